@@ -395,6 +395,113 @@ qevict_status qevict_last_attend_bytes(qevict_cache *c, int32_t layer, int64_t *
  * After it, synchronising the cache's stream also covers every retier call. */
 qevict_status qevict_join_routing(qevict_cache *c);
 
+/* ---- Prompts and sequences that keep every token -------------------------
+ *
+ * The calls below hold no handle: every buffer is the caller's and is passed
+ * to each call, together with the stream (hipStream_t, NULL = default stream)
+ * its work is enqueued on.  They run on the current device, to which stream
+ * and buffers belong, allocate nothing, never synchronise and may be captured
+ * into a HIP graph (lengths and tables are device arrays, read when the work
+ * runs).  Packed rows: sequence s is rows cu_tokens[s] .. cu_tokens[s + 1] - 1
+ * (device int32, n + 1 entries that do not decrease, 0 <= entries <=
+ * total_tokens; entries outside that are taken as the nearest bound), rows
+ * outside every sequence are neither read nor written.  A packed tensor is
+ * addressed as base + row * token_stride + head * head_stride (in elements,
+ * multiples of 8, not negative; a row's d channels are contiguous and 16-byte
+ * aligned), so slices of a fused projection and [H, tokens, d] tensors both
+ * fit.  Written tensors must not overlap themselves or another argument. */
+
+/* Causal attention of whole prompts (Sec. 4.1 attention, one query per prompt
+ * token; the pass whose keys and values qevict_prefill_assign or
+ * qevict_block_store then takes): inside each sequence token i attends to
+ * tokens 0 .. i with softmax(q k^T * scale), query head h on KV head
+ * h / (H_q / H_kv).
+ *   q [total, H_q, d], k, v [total, H_kv, d] bf16 packed, out like q
+ * A value that is not finite reaches the rows that attend to it and no other.
+ * H_q % H_kv == 0; d == 128; total_tokens * H_q <= 2^30. */
+typedef struct {
+  int32_t abi_version;
+  int32_t num_seqs;          /* sequences in cu_tokens, >= 1 */
+  int32_t total_tokens;      /* rows of the packed tensors   */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;          /* 128 */
+  float softmax_scale;       /* 0 selects 1/sqrt(head_dim) */
+  int64_t q_token_stride, q_head_stride;
+  int64_t k_token_stride, k_head_stride;
+  int64_t v_token_stride, v_head_stride;
+  int64_t out_token_stride, out_head_stride;
+} qevict_prompt_config;
+qevict_status qevict_prompt_attend(const qevict_prompt_config *cfg, const uint16_t *q,
+                                   const uint16_t *k, const uint16_t *v, const int32_t *cu_tokens,
+                                   uint16_t *out, void *hip_stream);
+
+/* The 8-bit block cache: a paged cache for sequences of different lengths that
+ * keep every token, at half the bytes of bf16.  Tokens are grouped in blocks
+ * of 64.  A complete block of one KV head is int8 codes with one scale for its
+ * keys and one for its values; the open block of a sequence (its last
+ * length % 64 tokens) is bf16.  A block is quantized once, when its last token
+ * arrives (Sec. 4.3, write-once codes):
+ *   s = max(fl32(max |x| / 127), 2^-100),  c = round-half-even(x / s), exact,
+ * and every reader takes s * c, so |x - s c| <= s / 2 (up to the rounding of
+ * s).  A block that holds a value that is not finite gets the scale NaN.
+ * One layer: */
+#define QEVICT_BLOCK_TOKENS 64
+typedef struct {
+  int8_t *k_codes;           /* [num_pages, H_kv, 64, d]                                    */
+  int8_t *v_codes;           /* [num_pages, H_kv, d, 64]: a channel's tokens together       */
+  float *k_scale;            /* [num_pages, H_kv]                                           */
+  float *v_scale;            /* [num_pages, H_kv]                                           */
+  uint16_t *k_tail;          /* [B, H_kv, 64, d] bf16, token p in row p % 64                */
+  uint16_t *v_tail;          /* [B, H_kv, 64, d] bf16                                       */
+  const int32_t *table;      /* [B, ceil(max_context / 64)] page of each block; an entry    */
+                             /* outside 0 .. num_pages - 1 holds no page: the block's       */
+                             /* tokens take no part in attention and are not stored         */
+  const int32_t *lens;       /* [B] tokens held; negative: no sequence in this place        */
+} qevict_block_layer;
+typedef struct {
+  int32_t abi_version;
+  int32_t batch;             /* B places                                                    */
+  int32_t num_q_heads;       /* H_q                                                         */
+  int32_t num_kv_heads;      /* H_kv; H_q % H_kv == 0 and H_q / H_kv <= 16                  */
+  int32_t head_dim;          /* 128                                                         */
+  int32_t max_context;       /* largest sequence length                                     */
+  int32_t num_pages;
+  float softmax_scale;       /* 0 selects 1/sqrt(head_dim)                                  */
+} qevict_block_config;
+
+/* Stores packed prompts k, v [total, H_kv, d] bf16: sequence s (its rows by
+ * cu_tokens, B + 1 entries; at most max_context of them are stored) becomes
+ * place s's tokens 0 .. n - 1, complete blocks into the pages of its table row
+ * and the rest into its tail.  A place without rows keeps what it holds, and
+ * lens is the caller's to set.  A page that is written belongs to one place. */
+qevict_status qevict_block_store(const qevict_block_config *cfg, const qevict_block_layer *layer,
+                                 const uint16_t *k, int64_t k_token_stride, int64_t k_head_stride,
+                                 const uint16_t *v, int64_t v_token_stride, int64_t v_head_stride,
+                                 const int32_t *cu_tokens, int32_t total_tokens, void *hip_stream);
+
+/* The reverse (for a tier or another cache that takes bf16, as
+ * qevict_prefill_assign does): writes tokens 0 .. n - 1 of every place, n the
+ * rows cu_tokens gives it, at most lens[s]; rows past that are left as they
+ * were.  A token of a complete block is its s * c rounded to fp32 and then to
+ * bf16, zero where the table holds no page; the open block is copied. */
+qevict_status qevict_block_fetch(const qevict_block_config *cfg, const qevict_block_layer *layer,
+                                 uint16_t *k, int64_t k_token_stride, int64_t k_head_stride,
+                                 uint16_t *v, int64_t v_token_stride, int64_t v_head_stride,
+                                 const int32_t *cu_tokens, int32_t total_tokens, void *hip_stream);
+
+/* One decode step (Sec. 4.1 decode attention): appends the new token of every
+ * place at position lens[s], attends with it over the place's complete blocks
+ * (codes expanded in registers) and its open block, itself included, and
+ * quantizes the block if the token filled it.  lens is read, not advanced: the
+ * caller adds 1 to it after the last layer of the step.  A place whose length
+ * is negative, or max_context and more, is skipped (its row of out stays).
+ *   q [B, H_q, d], k_new, v_new [B, H_kv, d] bf16, contiguous, 16-byte aligned
+ *   out [B, H_q, d] bf16 */
+qevict_status qevict_block_attend(const qevict_block_config *cfg, const qevict_block_layer *layer,
+                                  const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
+                                  uint16_t *out, void *hip_stream);
+
 const char *qevict_status_string(qevict_status s);
 const char *qevict_last_error(void);
 

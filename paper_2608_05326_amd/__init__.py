@@ -6,7 +6,8 @@ bf16 and quantized windows with per-window mass accumulation, TopK re-tiering
 and the quantize / promote migrations.  ``qevict`` is the ctypes binding.
 """
 from .qevict import (  # noqa: F401
-    Cache, Config, QEvictError, RetierStats, load_library, workspace_size, SYMBOLS,
+    BlockCache, BlockConfig, Cache, Config, QEvictError, RetierStats, load_library, prompt_attend,
+    workspace_size, SYMBOLS, BLOCK_TOKENS,
     OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_BAD_STATE, ERR_NONFINITE,
     ERR_CAPACITY, ERR_DEVICE,
     TIER_UNUSED, TIER_OPEN, TIER_FULL, TIER_QUANT, TIER_EVICTED,

@@ -15,7 +15,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libqevict.so")
-SOURCES = ["runtime.cpp", "attend.hip", "retier.hip", "migrate.hip", "prefill_scores.hip"]
+SOURCES = ["runtime.cpp", "attend.hip", "retier.hip", "migrate.hip", "prefill_scores.hip",
+           "prompt_attend.hip", "block_cache.hip"]
 ARCH = "gfx950"
 FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -56,7 +57,7 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(OUT_DIR, os.path.splitext(src)[0] + ".o")
         objs.append(obj)
         cmds.append([hipcc, "-c", "-x", "hip", os.path.join(CSRC, src), "-o", obj] + FLAGS)
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         for err in ex.map(_run, cmds):
             if verbose and err.strip():
                 print(err, file=sys.stderr)

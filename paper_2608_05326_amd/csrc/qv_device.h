@@ -137,6 +137,47 @@ struct ObsArgs {            // initial window scores from the observation querie
   float* scores;            // [B][n_w]
 };
 
+struct PromptArgs {         // causal attention of packed prompts
+  const uint16_t* q;        // rows [total] x heads, strides in elements
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;   // row and head strides
+  const int32_t* cu;        // [n_seqs + 1] first row of each prompt, then the end of the last
+  int32_t n_seqs, total, H_kv, gqa;
+  float scale_log2;
+};
+
+struct BlockArgs {          // one layer of an 8-bit block cache
+  int8_t* k_codes;          // [n_pages][H_kv][64][d]
+  int8_t* v_codes;          // [n_pages][H_kv][d][64]
+  float* k_scale;           // [n_pages][H_kv]
+  float* v_scale;
+  uint16_t* k_tail;         // [B][H_kv][64][d] bf16
+  uint16_t* v_tail;
+  const int32_t* table;     // [B][n_cols] page of each block
+  const int32_t* lens;      // [B] tokens held
+  int32_t B, H_q, H_kv, gqa, n_pages, n_cols, max_context;
+  float scale_log2;
+};
+
+struct PackedRows {         // packed keys and values of a store (in) or a fetch (out)
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  int64_t k_st, k_sh, v_st, v_sh;
+  const int32_t* cu;        // [B + 1]
+  int32_t total;
+};
+
+struct BlockStep {          // a decode step on the block cache
+  const uint16_t* q;        // [B][H_q][d]
+  const uint16_t* k_new;    // [B][H_kv][d]
+  const uint16_t* v_new;
+  uint16_t* out;            // [B][H_q][d]
+};
+
 struct ScorePowArgs {       // p-norm ranking: prompt scores raised to the power p
   const float* in;
   float* out;

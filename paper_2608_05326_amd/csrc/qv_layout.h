@@ -56,6 +56,7 @@ namespace qv {
 
 constexpr int kHeadDim = 128;
 constexpr int kMaxGqa = 16;
+constexpr int kBlockTokens = 64;    // tokens of a block of the 8-bit cache
 constexpr int kMaxCand = 4096;      // candidates per routing event (one workgroup sorts them)
 constexpr int kMaxSplits = 256;     // split-K factor of the attention pass
 constexpr int kAttnThreads = 256;

@@ -41,10 +41,17 @@ hipError_t launch_key_norm_init(const KeyNormArgs& a, hipStream_t st);
 hipError_t launch_score_pow(const ScorePowArgs& a, hipStream_t st);
 hipError_t launch_prefill_scores(const ObsArgs& a, hipStream_t st);
 hipError_t static_obs_scratch(void** ptr, const char** what);
+int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv);
+hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st);
+int64_t block_packed_groups(int64_t total, int n_seqs, int H_kv);
+hipError_t launch_block_store(const BlockArgs& a, const PackedRows& r, hipStream_t st);
+hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream_t st);
+hipError_t launch_block_attend(const BlockArgs& a, const BlockStep& s, hipStream_t st);
 }  // namespace qv
 
 using namespace qv;
 static_assert(kScorePnorm == QEVICT_SCORE_PNORM, "score mode numbering");
+static_assert(kBlockTokens == QEVICT_BLOCK_TOKENS, "block size");
 static_assert(kStaticObsScratchBytes == QEVICT_STATIC_SCRATCH_BYTES, "fixed scratch size");
 
 namespace {
@@ -1347,6 +1354,197 @@ qevict_status qevict_last_attend_bytes(qevict_cache* c, int32_t layer, int64_t* 
   }
   *bytes = total;
   return QEVICT_OK;
+}
+
+// ---- packed prompts and the 8-bit block cache (no handle) ----
+
+// Largest grid of 256-thread workgroups (work-items of a dimension are counted in 32 bits).
+static constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 1;
+
+static qevict_status check_heads(int32_t abi, int32_t hq, int32_t hkv, int32_t d, float scale) {
+  if (abi != QEVICT_ABI_VERSION)
+    return fail(QEVICT_ERR_UNSUPPORTED, "abi_version %d, library implements %d", abi, QEVICT_ABI_VERSION);
+  if (hq < 1 || hkv < 1) return fail(QEVICT_ERR_INVALID_ARG, "head counts must be positive");
+  if (hq % hkv) return fail(QEVICT_ERR_INVALID_ARG, "num_q_heads %% num_kv_heads != 0");
+  if (d != kHeadDim) return fail(QEVICT_ERR_UNSUPPORTED, "head_dim must be 128");
+  if (!(scale >= 0.f) || std::isinf(scale)) return fail(QEVICT_ERR_INVALID_ARG, "softmax_scale");
+  return QEVICT_OK;
+}
+
+static float scale_log2_of(float scale) {
+  return (scale > 0.f ? scale : 1.f / std::sqrt((float)kHeadDim)) * 1.44269504088896340736f;
+}
+
+// A packed tensor of `tokens` x `heads` rows: strides the kernels' 16-byte accesses can
+// follow and, for a written one, rows that do not overlap.
+static qevict_status check_rows(const char* name, const void* p, int64_t tokens, int heads, int64_t st, int64_t sh,
+                                bool written) {
+  if (!p) return fail(QEVICT_ERR_INVALID_ARG, "%s is NULL", name);
+  if ((uintptr_t)p & 15) return fail(QEVICT_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+  if (st < 0 || sh < 0 || st % 8 || sh % 8)
+    return fail(QEVICT_ERR_INVALID_ARG, "%s: strides must be non-negative multiples of 8 elements", name);
+  const int64_t limit = (int64_t)1 << 58;   // offsets in bytes stay within 63 bits
+  if ((tokens > 1 && st > limit / tokens) || (heads > 1 && sh > limit / heads))
+    return fail(QEVICT_ERR_INVALID_ARG, "%s: strides too large", name);
+  if (written) {
+    const bool lone_t = tokens == 1, lone_h = heads == 1;
+    if ((!lone_t && st < kHeadDim) || (!lone_h && sh < kHeadDim) ||
+        (!lone_t && !lone_h && st < (heads - 1) * sh + kHeadDim && sh < (tokens - 1) * st + kHeadDim))
+      return fail(QEVICT_ERR_INVALID_ARG, "%s: rows overlap", name);
+  }
+  return QEVICT_OK;
+}
+
+qevict_status qevict_prompt_attend(const qevict_prompt_config* cfg, const uint16_t* q, const uint16_t* k,
+                                   const uint16_t* v, const int32_t* cu_tokens, uint16_t* out, void* hip_stream) {
+  if (!cfg) return fail(QEVICT_ERR_INVALID_ARG, "config is NULL");
+  qevict_status s =
+      check_heads(cfg->abi_version, cfg->num_q_heads, cfg->num_kv_heads, cfg->head_dim, cfg->softmax_scale);
+  if (s) return s;
+  if (cfg->num_seqs < 1) return fail(QEVICT_ERR_INVALID_ARG, "num_seqs must be positive");
+  if (cfg->total_tokens < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (cfg->total_tokens == 0) return QEVICT_OK;
+  if (!cu_tokens || ((uintptr_t)cu_tokens & 3)) return fail(QEVICT_ERR_INVALID_ARG, "cu_tokens");
+  const int64_t n = cfg->total_tokens;
+  const int hq = cfg->num_q_heads, hkv = cfg->num_kv_heads;
+  if ((s = check_rows("q", q, n, hq, cfg->q_token_stride, cfg->q_head_stride, false)) ||
+      (s = check_rows("k", k, n, hkv, cfg->k_token_stride, cfg->k_head_stride, false)) ||
+      (s = check_rows("v", v, n, hkv, cfg->v_token_stride, cfg->v_head_stride, false)) ||
+      (s = check_rows("out", out, n, hq, cfg->out_token_stride, cfg->out_head_stride, true)))
+    return s;
+  if (n * hq > ((int64_t)1 << 30) || prompt_attend_groups(n, cfg->num_seqs, hq / hkv, hkv) > kMaxGroups)
+    return fail(QEVICT_ERR_UNSUPPORTED, "prompts too large for one call");
+  PromptArgs a;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.out = out;
+  a.q_st = cfg->q_token_stride;
+  a.q_sh = cfg->q_head_stride;
+  a.k_st = cfg->k_token_stride;
+  a.k_sh = cfg->k_head_stride;
+  a.v_st = cfg->v_token_stride;
+  a.v_sh = cfg->v_head_stride;
+  a.o_st = cfg->out_token_stride;
+  a.o_sh = cfg->out_head_stride;
+  a.cu = cu_tokens;
+  a.n_seqs = cfg->num_seqs;
+  a.total = cfg->total_tokens;
+  a.H_kv = hkv;
+  a.gqa = hq / hkv;
+  a.scale_log2 = scale_log2_of(cfg->softmax_scale);
+  hipError_t e = launch_prompt_attend(a, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "prompt_attend launch");
+}
+
+static qevict_status block_args(const qevict_block_config* cfg, const qevict_block_layer* layer, BlockArgs* a) {
+  if (!cfg || !layer) return fail(QEVICT_ERR_INVALID_ARG, "config or layer is NULL");
+  qevict_status s =
+      check_heads(cfg->abi_version, cfg->num_q_heads, cfg->num_kv_heads, cfg->head_dim, cfg->softmax_scale);
+  if (s) return s;
+  if (cfg->num_q_heads / cfg->num_kv_heads > kMaxGqa)
+    return fail(QEVICT_ERR_UNSUPPORTED, "at most 16 query heads per KV head");
+  if (cfg->batch < 1 || cfg->max_context < 1 || cfg->num_pages < 0)
+    return fail(QEVICT_ERR_INVALID_ARG, "batch and max_context must be positive, num_pages not negative");
+  if (cfg->max_context > ((int32_t)1 << 30) || (int64_t)cfg->batch * cfg->num_kv_heads > kMaxGroups)
+    return fail(QEVICT_ERR_UNSUPPORTED, "max_context or batch too large");
+  if (cfg->num_pages && (!layer->k_codes || !layer->v_codes || !layer->k_scale || !layer->v_scale))
+    return fail(QEVICT_ERR_INVALID_ARG, "null page pointer");
+  if (!layer->k_tail || !layer->v_tail || !layer->table || !layer->lens)
+    return fail(QEVICT_ERR_INVALID_ARG, "null tail, table or length pointer");
+  if (((uintptr_t)layer->k_codes | (uintptr_t)layer->v_codes | (uintptr_t)layer->k_tail |
+       (uintptr_t)layer->v_tail) & 15)
+    return fail(QEVICT_ERR_INVALID_ARG, "codes and tails must be 16-byte aligned");
+  if (((uintptr_t)layer->k_scale | (uintptr_t)layer->v_scale | (uintptr_t)layer->table |
+       (uintptr_t)layer->lens) & 3)
+    return fail(QEVICT_ERR_INVALID_ARG, "scales, table and lengths must be 4-byte aligned");
+  a->k_codes = layer->k_codes;
+  a->v_codes = layer->v_codes;
+  a->k_scale = layer->k_scale;
+  a->v_scale = layer->v_scale;
+  a->k_tail = layer->k_tail;
+  a->v_tail = layer->v_tail;
+  a->table = layer->table;
+  a->lens = layer->lens;
+  a->B = cfg->batch;
+  a->H_q = cfg->num_q_heads;
+  a->H_kv = cfg->num_kv_heads;
+  a->gqa = a->H_q / a->H_kv;
+  a->n_pages = cfg->num_pages;
+  a->n_cols = ceil_div(cfg->max_context, kBlockTokens);
+  a->max_context = cfg->max_context;
+  a->scale_log2 = scale_log2_of(cfg->softmax_scale);
+  return QEVICT_OK;
+}
+
+static qevict_status packed_rows(const BlockArgs& a, const uint16_t* k, int64_t k_st, int64_t k_sh, const uint16_t* v,
+                                 int64_t v_st, int64_t v_sh, const int32_t* cu, int32_t total, bool written,
+                                 PackedRows* r) {
+  if (!cu || ((uintptr_t)cu & 3)) return fail(QEVICT_ERR_INVALID_ARG, "cu_tokens");
+  qevict_status s;
+  if ((s = check_rows("k", k, total, a.H_kv, k_st, k_sh, written)) ||
+      (s = check_rows("v", v, total, a.H_kv, v_st, v_sh, written)))
+    return s;
+  if (block_packed_groups(total, a.B, a.H_kv) > kMaxGroups)
+    return fail(QEVICT_ERR_UNSUPPORTED, "sequences too large for one call");
+  r->k = k;
+  r->v = v;
+  r->k_out = written ? const_cast<uint16_t*>(k) : nullptr;
+  r->v_out = written ? const_cast<uint16_t*>(v) : nullptr;
+  r->k_st = k_st;
+  r->k_sh = k_sh;
+  r->v_st = v_st;
+  r->v_sh = v_sh;
+  r->cu = cu;
+  r->total = total;
+  return QEVICT_OK;
+}
+
+qevict_status qevict_block_store(const qevict_block_config* cfg, const qevict_block_layer* layer, const uint16_t* k,
+                                 int64_t k_token_stride, int64_t k_head_stride, const uint16_t* v,
+                                 int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu_tokens,
+                                 int32_t total_tokens, void* hip_stream) {
+  BlockArgs a;
+  PackedRows r;
+  qevict_status s = block_args(cfg, layer, &a);
+  if (s) return s;
+  if (total_tokens < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (total_tokens == 0) return QEVICT_OK;
+  if ((s = packed_rows(a, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, cu_tokens,
+                       total_tokens, false, &r)))
+    return s;
+  hipError_t e = launch_block_store(a, r, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_store launch");
+}
+
+qevict_status qevict_block_fetch(const qevict_block_config* cfg, const qevict_block_layer* layer, uint16_t* k,
+                                 int64_t k_token_stride, int64_t k_head_stride, uint16_t* v, int64_t v_token_stride,
+                                 int64_t v_head_stride, const int32_t* cu_tokens, int32_t total_tokens,
+                                 void* hip_stream) {
+  BlockArgs a;
+  PackedRows r;
+  qevict_status s = block_args(cfg, layer, &a);
+  if (s) return s;
+  if (total_tokens < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (total_tokens == 0) return QEVICT_OK;
+  if ((s = packed_rows(a, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, cu_tokens,
+                       total_tokens, true, &r)))
+    return s;
+  hipError_t e = launch_block_fetch(a, r, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_fetch launch");
+}
+
+qevict_status qevict_block_attend(const qevict_block_config* cfg, const qevict_block_layer* layer, const uint16_t* q,
+                                  const uint16_t* k_new, const uint16_t* v_new, uint16_t* out, void* hip_stream) {
+  BlockArgs a;
+  qevict_status s = block_args(cfg, layer, &a);
+  if (s) return s;
+  if (!q || !k_new || !v_new || !out) return fail(QEVICT_ERR_INVALID_ARG, "null pointer");
+  if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15)
+    return fail(QEVICT_ERR_INVALID_ARG, "q, k_new, v_new and out must be 16-byte aligned");
+  BlockStep step = {q, k_new, v_new, out};
+  hipError_t e = launch_block_attend(a, step, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_attend launch");
 }
 
 }  // extern "C"

@@ -28,6 +28,7 @@ FLAG_NO_PROMOTION, FLAG_DEBUG_MASSES, FLAG_ASYNC_ROUTING = 0x1, 0x2, 0x4
 FLAG_ROUTING_QUEUE_WAIT, FLAG_ROUTING_DEVICE_WAIT = 0x8, 0x10
 KERNEL_ATTEND, KERNEL_MERGE, KERNEL_RETIER, KERNEL_MIGRATE = range(4)
 SCORE_CUMULATIVE, SCORE_DECAY, SCORE_KEY_NORM, SCORE_PNORM = 0, 1, 2, 3
+BLOCK_TOKENS = 64
 
 # exported symbols declared in include/qevict.h
 SYMBOLS = (
@@ -38,7 +39,8 @@ SYMBOLS = (
     "qevict_profile_enable", "qevict_profile_read", "qevict_last_attend_bytes", "qevict_join_routing",
     "qevict_status_string", "qevict_last_error", "qevict_prefill_scores_scratch_size",
     "qevict_prefill_scores", "qevict_capacities_for_budget", "qevict_memory_report",
-    "qevict_prefill_scores_noalloc",
+    "qevict_prefill_scores_noalloc", "qevict_prompt_attend", "qevict_block_store", "qevict_block_fetch",
+    "qevict_block_attend",
 )
 
 
@@ -56,6 +58,25 @@ class _Config(ctypes.Structure):
         ("flags", ctypes.c_uint32), ("softmax_scale", ctypes.c_float), ("num_splits", ctypes.c_int32),
         ("score_mode", ctypes.c_int32), ("score_decay", ctypes.c_float), ("score_p", ctypes.c_float),
         ("rope_base", ctypes.c_float)]
+
+
+class _PromptConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "abi_version", "num_seqs", "total_tokens", "num_q_heads", "num_kv_heads", "head_dim")] + [
+        ("softmax_scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in (
+            "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride",
+            "v_head_stride", "out_token_stride", "out_head_stride")]
+
+
+class _BlockConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "abi_version", "batch", "num_q_heads", "num_kv_heads", "head_dim", "max_context", "num_pages")] + [
+        ("softmax_scale", ctypes.c_float)]
+
+
+class _BlockLayer(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in (
+        "k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "table", "lens")]
 
 
 class MemoryReport(ctypes.Structure):
@@ -153,6 +174,10 @@ def load_library(path: str | None = None):
         "qevict_capacities_for_budget": [P(_Config), i64, i32, P(i32), P(i32)],
         "qevict_memory_report": [vp, i32, i32, P(MemoryReport)],
         "qevict_prefill_scores_noalloc": [vp, vp, i32, vp, i32, vp],
+        "qevict_prompt_attend": [P(_PromptConfig), vp, vp, vp, vp, vp, vp],
+        "qevict_block_store": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, i32, vp],
+        "qevict_block_fetch": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, i32, vp],
+        "qevict_block_attend": [P(_BlockConfig), P(_BlockLayer), vp, vp, vp, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -413,3 +438,206 @@ class Cache:
         n = ctypes.c_int64()
         self._c(self.lib.qevict_last_attend_bytes(self.handle, layer, ctypes.byref(n)))
         return n.value
+
+
+# ------------------------------------------- prompts and the 8-bit block cache
+def _rows(t, torch, device, name, heads=None, tokens=None):
+    """Address and (token, head) strides of a packed bf16 tensor [tokens, heads, d]."""
+    if not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or \
+            (tokens is not None and t.shape[0] != tokens):
+        raise ValueError(f"{name} must be [{'T' if tokens is None else tokens}, "
+                         f"{'H' if heads is None else heads}, d], got shape {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a row must be contiguous")
+    # the stride of a dimension of size 1 is never used (and may be anything)
+    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if t.shape[0] > 1 else 0, \
+        t.stride(1) if t.shape[1] > 1 else 0
+
+
+def _int32(t, torch, device, name, shape):
+    if not t.is_cuda or t.device != device or t.dtype != torch.int32 or not t.is_contiguous() or \
+            tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+class _OnDevice:
+    """The device current for a call (a kernel runs on the current device)."""
+
+    def __init__(self, torch, device):
+        self.torch, self.index = torch, device.index
+
+    def __enter__(self):
+        self.before = self.torch.cuda.current_device()
+        if self.before != self.index:
+            self.torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            self.torch.cuda.set_device(self.before)
+
+
+def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stream=None):
+    """Causal attention of packed prompts: prompt s is rows cu_tokens[s] ..
+    cu_tokens[s + 1] - 1, each token attends to the tokens of its prompt up to itself.
+    q: bf16 [T, H_q, d]; k, v: bf16 [T, H_kv, d]; any strides that are multiples of 8
+    elements with the channels contiguous (slices of a fused projection, transposed
+    [H, T, d] tensors).  cu_tokens: int32 [n + 1] on the device.  Returns out, bf16
+    [T, H_q, d]; rows behind the last prompt are left as they were (undefined in an out
+    that is allocated here).  Runs on `stream`, by default torch's current one."""
+    import torch
+    lib = load_library()
+    dev = q.device
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q and k must be [T, H, d], got shapes {tuple(q.shape)} and {tuple(k.shape)}")
+    T, hq, d = q.shape
+    hkv = k.shape[1]
+    if out is None:
+        out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=dev)
+    qp, q_st, q_sh = _rows(q, torch, dev, "q")
+    kp, k_st, k_sh = _rows(k, torch, dev, "k", hkv, T)
+    vp, v_st, v_sh = _rows(v, torch, dev, "v", hkv, T)
+    op, o_st, o_sh = _rows(out, torch, dev, "out", hq, T)
+    if not k.shape[2] == v.shape[2] == out.shape[2] == d:
+        raise ValueError("q, k, v and out must have the same head dimension")
+    n = cu_tokens.numel() - 1
+    cu = _int32(cu_tokens, torch, dev, "cu_tokens", (n + 1,))
+    c = _PromptConfig(ABI_VERSION, n, T, hq, hkv, d, softmax_scale, q_st, q_sh, k_st, k_sh, v_st, v_sh,
+                      o_st, o_sh)
+    with _OnDevice(torch, dev):
+        st = (stream or torch.cuda.current_stream(dev)).cuda_stream
+        _check(lib, lib.qevict_prompt_attend(ctypes.byref(c), qp, kp, vp, cu, op, ctypes.c_void_p(st)))
+    return out
+
+
+@dataclasses.dataclass
+class BlockConfig:
+    batch: int
+    num_q_heads: int
+    num_kv_heads: int
+    max_context: int
+    num_pages: int = 0           # 0: a page for every block of every place
+    num_layers: int = 1
+    head_dim: int = 128
+    softmax_scale: float = 0.0
+
+
+class BlockCache:
+    """8-bit paged cache of sequences of different lengths (every token is kept; int8
+    codes with one scale per 64-token block and KV head, the open block in bf16).
+
+    Its state is plain tensors that the program may read, fill and share:
+      k_codes [L, pages, H_kv, 64, d], v_codes [L, pages, H_kv, d, 64]   int8
+      k_scale, v_scale [L, pages, H_kv]                                  float32
+      k_tail, v_tail [L, batch, H_kv, 64, d]                             bf16, open blocks
+      table [batch, ceil(max_context / 64)]  int32  page of each block, the same in all layers
+      lens [batch]                           int32  tokens held; negative: no sequence
+    An entry of table outside 0 .. pages - 1 means that the block has no page: its tokens
+    take no part.  With num_pages = 0 place s owns pages s * n .. s * n + n - 1, n the
+    columns of the table; otherwise the table starts at -1 and the program assigns pages
+    (before the block they are for is complete).  lens starts at -1: the program sets it after
+    storing a prompt and advances it after each step (advance()).
+
+    Assigning to one of them copies into it.  Calls run on torch's current stream unless the cache was given one."""
+
+    def __init__(self, cfg: BlockConfig, device="cuda", stream=None):
+        import torch
+
+        self.torch = torch
+        self.lib = load_library()
+        self.cfg = cfg
+        dev = torch.device(device)
+        if dev.type != "cuda":
+            raise ValueError(f"a block cache needs a GPU, got device {dev}")
+        if cfg.batch < 1 or cfg.max_context < 1 or cfg.num_layers < 1 or cfg.num_kv_heads < 1 or \
+                cfg.num_pages < 0:
+            raise ValueError("batch, max_context, num_layers and num_kv_heads must be positive")
+        if dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        self.device = dev
+        self.stream = stream
+        L, B, h, d, n = cfg.num_layers, cfg.batch, cfg.num_kv_heads, cfg.head_dim, BLOCK_TOKENS
+        cols = -(-cfg.max_context // n)
+        pages = cfg.num_pages or B * cols
+        self.num_pages = pages
+        z = torch.zeros
+        self._state = dict(
+            k_codes=z((L, pages, h, n, d), dtype=torch.int8, device=dev),
+            v_codes=z((L, pages, h, d, n), dtype=torch.int8, device=dev),
+            k_scale=z((L, pages, h), dtype=torch.float32, device=dev),
+            v_scale=z((L, pages, h), dtype=torch.float32, device=dev),
+            k_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
+            v_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
+            table=torch.full((B, cols), -1, dtype=torch.int32, device=dev),
+            lens=torch.full((B,), -1, dtype=torch.int32, device=dev))
+        if not cfg.num_pages:
+            self.table.copy_(torch.arange(pages, dtype=torch.int32).view(B, cols))
+        self._c = _BlockConfig(ABI_VERSION, B, cfg.num_q_heads, h, d, cfg.max_context, pages, cfg.softmax_scale)
+        self._layers = [_BlockLayer(*[
+            (t if name in ("table", "lens") else t[i]).data_ptr() for name, t in self._state.items()])
+            for i in range(L)]
+
+    def _layer(self, layer: int):
+        if not 0 <= layer < self.cfg.num_layers:
+            raise ValueError(f"layer {layer} out of range")
+        return self._layers[layer]
+
+    def _call(self, fn, layer, *args):
+        with _OnDevice(self.torch, self.device):
+            st = (self.stream or self.torch.cuda.current_stream(self.device)).cuda_stream
+            _check(self.lib, fn(ctypes.byref(self._c), ctypes.byref(self._layer(layer)), *args,
+                                ctypes.c_void_p(st)))
+
+    def _packed(self, k, v, cu_tokens):
+        t, h = self.torch, self.cfg.num_kv_heads
+        kr = _rows(k, t, self.device, "k", h)
+        vr = _rows(v, t, self.device, "v", h, k.shape[0])
+        if k.shape[2] != self.cfg.head_dim or v.shape[2] != self.cfg.head_dim:
+            raise ValueError(f"k and v must have {self.cfg.head_dim} channels")
+        return (*kr, *vr, _int32(cu_tokens, t, self.device, "cu_tokens", (self.cfg.batch + 1,)), k.shape[0])
+
+    def store(self, layer: int, k, v, cu_tokens):
+        """Stores packed prompts: rows cu_tokens[s] .. cu_tokens[s + 1] - 1 of k, v (bf16
+        [T, H_kv, d], strides as in prompt_attend) become the tokens of place s; a place
+        without rows keeps what it holds."""
+        self._call(self.lib.qevict_block_store, layer, *self._packed(k, v, cu_tokens))
+
+    def fetch(self, layer: int, k, v, cu_tokens):
+        """Writes the tokens of every place (at most lens[s] of them) to its rows of k, v
+        (bf16 [T, H_kv, d]); other rows are left as they were."""
+        self._call(self.lib.qevict_block_fetch, layer, *self._packed(k, v, cu_tokens))
+
+    def attend(self, layer: int, q, k_new, v_new, out):
+        """One decode step: appends token lens[s] of every place and attends with it.
+        q: bf16 [batch, H_q, d]; k_new, v_new: bf16 [batch, H_kv, d]; out: bf16 like q."""
+        t, c = self.torch, self.cfg
+        qs, ks = (c.batch, c.num_q_heads, c.head_dim), (c.batch, c.num_kv_heads, c.head_dim)
+        for x, name in ((q, "q"), (k_new, "k_new"), (v_new, "v_new"), (out, "out")):
+            if x.device != self.device:
+                raise ValueError(f"{name} must be on {self.device}, got {x.device}")
+        self._call(self.lib.qevict_block_attend, layer, _ptr(q, t.bfloat16, "q", qs),
+                   _ptr(k_new, t.bfloat16, "k_new", ks), _ptr(v_new, t.bfloat16, "v_new", ks),
+                   _ptr(out, t.bfloat16, "out", qs))
+
+    def advance(self):
+        """After a step's last layer: lens + 1 where a place holds a sequence that has room."""
+        self.lens += ((self.lens >= 0) & (self.lens < self.cfg.max_context)).to(self.lens.dtype)
+
+
+def _state_tensor(name):
+    def get(self):
+        return self._state[name]
+
+    def put(self, value):   # assignment writes into the tensor the kernels read
+        if value is not self._state[name]:
+            self._state[name].copy_(value)
+    return property(get, put)
+
+
+for _name, _ in _BlockLayer._fields_:
+    setattr(BlockCache, _name, _state_tensor(_name))
