@@ -497,10 +497,17 @@ qevict_status qevict_block_fetch(const qevict_block_config *cfg, const qevict_bl
  * caller adds 1 to it after the last layer of the step.  A place whose length
  * is negative, or max_context and more, is skipped (its row of out stays).
  *   q [B, H_q, d], k_new, v_new [B, H_kv, d] bf16, contiguous, 16-byte aligned
- *   out [B, H_q, d] bf16 */
+ *   out [B, H_q, d] bf16
+ *   workspace  device memory of qevict_block_workspace_size bytes, 256-byte
+ *              aligned, overwritten: steps that may overlap (on two streams, in
+ *              two graphs) need one each, as they need layers of their own
+ * The sums run in an order that depends on the lengths only: a step is
+ * bitwise repeatable. */
+qevict_status qevict_block_workspace_size(const qevict_block_config *cfg, size_t *bytes);
 qevict_status qevict_block_attend(const qevict_block_config *cfg, const qevict_block_layer *layer,
                                   const uint16_t *q, const uint16_t *k_new, const uint16_t *v_new,
-                                  uint16_t *out, void *hip_stream);
+                                  uint16_t *out, void *workspace, size_t workspace_bytes,
+                                  void *hip_stream);
 
 const char *qevict_status_string(qevict_status s);
 const char *qevict_last_error(void);

@@ -9,7 +9,8 @@
 //
 //   k_block_store   packed prompts -> pages and tails
 //   k_block_fetch   pages and tails -> packed bf16 rows
-//   k_block_attend  one decode token per sequence: append, attend, close a full block
+//   k_block_attend, k_block_merge  one decode token per sequence: append, attend, close a
+//                   full block
 //
 // Page layout, one KV head: keys [64][128] (a token's channels together), values [128][64]
 // (a channel's tokens together): each is the order in which the matrix instruction of its
@@ -277,9 +278,15 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 }
 
 // ------------------------------------------------------------------ decode attention
-// One token per sequence.  A workgroup of four waves takes one (sequence, KV head): wave w
-// takes blocks w, w + 4, ..., the tail is wave 0's last one.  With 16x16x32 MFMAs, the G
-// query heads of the KV head as columns (padded to 16):
+// One token per sequence, in two launches.  The items of a (sequence, KV head) pair are
+// its complete blocks, then its open block; the items of all pairs, in pair order, are cut
+// into equal parts, one per workgroup, whatever the lengths are (they are read on the
+// device).  A workgroup goes through the pairs its part touches (segments); its four waves
+// take a segment's items in turn and are joined in LDS.  A segment that is a whole pair is
+// written out; the others leave (maximum, sum, output) rows that k_block_merge joins.
+//
+// A wave's products, by 16x16x32 MFMAs with the G query heads of the KV head as columns
+// (padded to 16):
 //   S^T = K q^T   (A = 16 keys; a lane holds 4 keys of ONE head per tile)
 //   O^T = V^T P^T (A = 16 channels; the same lane owns 32 channels of that head)
 // Row r of key tile tt is token 16 (r / 4) + 4 tt + r % 4 of the block, so that lane group
@@ -289,6 +296,7 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // (exact: bf16 has 8 bits; entries 2^-38 below the head's largest round).
 namespace {
 constexpr float kLazyD = 8.f;
+constexpr int kParts = 512;      // workgroups of a step: two per compute unit
 
 __device__ __forceinline__ f32x4 mfma_f16(f16x8 x, f16x8 y, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
@@ -333,200 +341,348 @@ __device__ __forceinline__ void raise(Running& st, float mt) {
   }
 }
 
+// Items of a place: its complete blocks and the open one; none without a sequence or room.
+__device__ __forceinline__ int items_of(int len, int max_context) {
+  return len < 0 || len >= max_context ? 0 : len / kBlk + 1;
+}
+
+// inclusive sum over the wave's lanes
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(x, d, 64);
+    if (lane >= d) x += o;
+  }
+  return x;
+}
+
+// Items of all places (of one KV head); with a place, *before receives those of the places
+// before it.  At most 2^31 / H_kv (checked on the host).
+__device__ __forceinline__ int count_items(const BlockArgs& a, int place, int* before) {
+  const int lane = threadIdx.x & 63;
+  int sum = 0;
+  for (int s0 = 0; s0 < a.B; s0 += 64) {
+    const int n = s0 + lane < a.B ? items_of(a.lens[s0 + lane], a.max_context) : 0;
+    const int incl = wave_scan(n, lane);
+    if (place >= s0 && place < s0 + 64)
+      *before = sum + __builtin_amdgcn_readlane(incl, place - s0) - __builtin_amdgcn_readlane(n, place - s0);
+    sum += __builtin_amdgcn_readlane(incl, 63);
+  }
+  return sum;
+}
+
 constexpr int kTailRow = 2 * kHeadDim;
+constexpr int kJoinRow = kHeadDim + 4;
 }  // namespace
 
 __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, BlockStep s) {
-  __shared__ __attribute__((aligned(16))) uint8_t stail[kBlk * kTailRow];   // the tail's values
-  __shared__ __attribute__((aligned(16))) float so[4][16][kHeadDim + 4];
+  __shared__ __attribute__((aligned(16))) uint8_t stail[kBlk * kTailRow];   // the open block's values
   __shared__ float sml[4][16][2];
-  __shared__ CloseLds sm;
-  const int g = blockIdx.x, b = blockIdx.y;
+  extern __shared__ __attribute__((aligned(16))) float so[];                // [4][gqa][kJoinRow]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, qd = lane >> 4;
-  const int pos = a.lens[b];                     // position of the new token
-  if (pos < 0 || pos >= a.max_context) return;   // no sequence in this place
-  const int n_blk = pos / kBlk, n_tail = pos % kBlk + 1;
 
-  const int hr = min(r, a.gqa - 1);   // columns past the last head repeat it
-  const uint16_t* qp = s.q + ((int64_t)b * a.H_q + g * a.gqa + hr) * kHeadDim;
-  const uint16_t* kn = s.k_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
-  const uint16_t* vn = s.v_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
-  uint16_t* kt = a.k_tail + ((int64_t)b * a.H_kv + g) * kCodes;
-  uint16_t* vt = a.v_tail + ((int64_t)b * a.H_kv + g) * kCodes;
+  // ---- this workgroup's part of the items
+  const int64_t total = (int64_t)count_items(a, -1, nullptr) * a.H_kv;
+  const int parts = (int)min((int64_t)gridDim.x, total), part = blockIdx.x;
+  if (part >= parts) return;
+  const int begin = (int)(total * part / parts), end = (int)(total * (part + 1) / parts);
 
-  Running st;
-  st.m = -INFINITY;
-  st.l = 0.f;
+  int base = 0;   // items before the 64 places of this round
+  for (int s0 = 0; s0 < a.B && base < end; s0 += 64) {
+    const int len = s0 + lane < a.B ? a.lens[s0 + lane] : -1;
+    const int n = items_of(len, a.max_context) * a.H_kv;
+    const int incl = base + wave_scan(n, lane);
+    // places of the round that the part touches
+    uint64_t mine = __ballot(n > 0 && incl > begin && incl - n < end);
+    base = __builtin_amdgcn_readlane(incl, 63);
+    for (; mine; mine &= mine - 1) {
+      const int w = __builtin_ctzll(mine), b = s0 + w;
+      const int pos = __builtin_amdgcn_readlane(len, w);   // position of the new token
+      const int n_blk = pos / kBlk, n_tail = pos % kBlk + 1, per = n_blk + 1;
+      const int first = __builtin_amdgcn_readlane(incl, w) - per * a.H_kv;
+      const int lo = max(begin - first, 0), hi = min(end - first, per * a.H_kv);
+      for (int g = lo / per; g * per < hi; ++g) {
+        // ---- segment: items [i0, i1) of pair (b, g)
+        const int i0 = max(lo - g * per, 0), i1 = min(hi - g * per, per);
+        const int hr = min(r, a.gqa - 1);   // columns past the last head repeat it
+        const uint16_t* qp = s.q + ((int64_t)b * a.H_q + g * a.gqa + hr) * kHeadDim;
+        Running st;
+        st.m = -INFINITY;
+        st.l = 0.f;
 #pragma unroll
-  for (int ct = 0; ct < 8; ++ct) st.o[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        for (int ct = 0; ct < 8; ++ct) st.o[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
-  if (wave < n_blk) {
-    // query operand: k-step (p, e) covers channels 64 p + 16 qd + 8 e + j
-    u32x4 qw[4];
+        const int b_end = min(i1, n_blk);
+        if (i0 + wave < b_end) {
+          // query operand: k-step (p, e) covers channels 64 p + 16 qd + 8 e + j
+          u32x4 qw[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 64 * (i >> 1) + 16 * qd + 8 * (i & 1));
-    uint32_t am = 0;
+          for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 64 * (i >> 1) + 16 * qd + 8 * (i & 1));
+          uint32_t am = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) am = amax_bits(qw[i], am);
-    am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
-    am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
-    // 2^(14 - e) for a largest magnitude in [2^e, 2^(e + 1)); ldexp takes what its factors
-    // cannot hold in one
-    const int ex = (int)(am >> 23) - 127;
-    f16x8 qf[4];
+          for (int i = 0; i < 4; ++i) am = amax_bits(qw[i], am);
+          am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
+          am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+          // 2^(14 - ex) for a largest magnitude in [2^ex, 2^(ex + 1))
+          const int ex = (int)(am >> 23) - 127;
+          f16x8 qf[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        qf[i][2 * j] = (_Float16)ldexpf(lo_f32(qw[i][j]), 14 - ex);
-        qf[i][2 * j + 1] = (_Float16)ldexpf(hi_f32(qw[i][j]), 14 - ex);
-      }
-    const float qs = ldexpf(a.scale_log2, ex - 14);   // log2 units per (q' c s)
+            for (int j = 0; j < 4; ++j) {
+              qf[i][2 * j] = (_Float16)ldexpf(lo_f32(qw[i][j]), 14 - ex);
+              qf[i][2 * j + 1] = (_Float16)ldexpf(hi_f32(qw[i][j]), 14 - ex);
+            }
+          const float qs = ldexpf(a.scale_log2, ex - 14);   // log2 units per (q' c s)
 
-    for (int blk = wave; blk < n_blk; blk += 4) {
-      const int page = page_of(a, b, blk);
-      if (page < 0) continue;   // dropped: its tokens take no part
-      const int64_t e = (int64_t)page * a.H_kv + g;
-      const int8_t* kc = a.k_codes + e * kCodes;
-      const int8_t* vc = a.v_codes + e * kCodes;
-      const float sc = a.k_scale[e] * qs, vs = a.v_scale[e];
-      f32x4 acc[4];
+          for (int blk0 = i0 + wave; blk0 < b_end; blk0 += 256) {
+            // pages and scales of the wave's next 64 blocks, one per lane; a dropped block's
+            // tokens take no part
+            const int blk = blk0 + 4 * lane;
+            const int page = blk < b_end ? page_of(a, b, blk) : -1;
+            const int64_t e = (int64_t)max(page, 0) * a.H_kv + g;
+            float ks_l = 0.f, vs_l = 0.f;
+            if (page >= 0) {
+              ks_l = a.k_scale[e];
+              vs_l = a.v_scale[e];
+            }
+            uint64_t live = __ballot(page >= 0);
+            if (!live) continue;
+            const int row = (16 * (r >> 2) + (r & 3)) * kHeadDim + 16 * qd;   // + 4 tt rows
+            u32x4 kb[8], vb[8];
+            auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + g) * kCodes; };
+            auto load_k = [&](int j) {
+              const int8_t* kc = a.k_codes + entry(j) + row;
 #pragma unroll
-      for (int tt = 0; tt < 4; ++tt) {
-        acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        const int8_t* row = kc + (16 * (r >> 2) + 4 * tt + (r & 3)) * kHeadDim + 16 * qd;
+              for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 4 * (i >> 1) * kHeadDim + 64 * (i & 1));
+            };
+            load_k(__builtin_ctzll(live));
+            while (live) {
+              const int j = __builtin_ctzll(live);
+              live &= live - 1;
+              const int8_t* vc = a.v_codes + entry(j) + r * kBlk + 16 * qd;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const u32x4 x = *(const u32x4*)(row + 64 * p);
-          acc[tt] = mfma_f16(codes_f16(x[0], x[1]), qf[2 * p], acc[tt]);
-          acc[tt] = mfma_f16(codes_f16(x[2], x[3]), qf[2 * p + 1], acc[tt]);
+              for (int ct = 0; ct < 8; ++ct) vb[ct] = *(const u32x4*)(vc + 16 * ct * kBlk);
+              const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)) * qs;
+              const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
+              f32x4 acc[4];
+#pragma unroll
+              for (int tt = 0; tt < 4; ++tt) {
+                acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                  const u32x4 x = kb[2 * tt + p];
+                  acc[tt] = mfma_f16(codes_f16(x[0], x[1]), qf[2 * p], acc[tt]);
+                  acc[tt] = mfma_f16(codes_f16(x[2], x[3]), qf[2 * p + 1], acc[tt]);
+                }
+              }
+              if (live) load_k(__builtin_ctzll(live));
+              float mt = -INFINITY;
+#pragma unroll
+              for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  acc[tt][i] *= sc;
+                  mt = fmaxf(mt, acc[tt][i]);
+                }
+              raise(st, rows_max(mt));
+              const float mu = st.m > -INFINITY ? st.m : 0.f;
+              f16x8 p[2];
+#pragma unroll
+              for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu);
+                  st.l += x;
+                  p[tt >> 1][4 * (tt & 1) + i] = (_Float16)x;
+                }
+#pragma unroll
+              for (int ct = 0; ct < 8; ++ct) {
+                const u32x4 x = vb[ct];
+                f32x4 y = {0.f, 0.f, 0.f, 0.f};
+                y = mfma_f16(codes_f16(x[0], x[1]), p[0], y);
+                y = mfma_f16(codes_f16(x[2], x[3]), p[1], y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.o[ct][i] = fmaf(y[i], vs, st.o[ct][i]);
+              }
+            }
+          }
         }
-      }
-      float mt = -INFINITY;
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[tt][i] *= sc;
-          mt = fmaxf(mt, acc[tt][i]);
-        }
-      raise(st, rows_max(mt));
-      const float mu = st.m > -INFINITY ? st.m : 0.f;
-      f16x8 p[2];
-#pragma unroll
-      for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu);
-          st.l += x;
-          p[tt >> 1][4 * (tt & 1) + i] = (_Float16)x;
-        }
-#pragma unroll
-      for (int ct = 0; ct < 8; ++ct) {
-        const u32x4 x = *(const u32x4*)(vc + (16 * ct + r) * kBlk + 16 * qd);
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
-        y = mfma_f16(codes_f16(x[0], x[1]), p[0], y);
-        y = mfma_f16(codes_f16(x[2], x[3]), p[1], y);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st.o[ct][i] = fmaf(y[i], vs, st.o[ct][i]);
-      }
-    }
-  }
 
-  if (wave == 0) {
-    // the tail, in bf16: row n_tail - 1 is the new token, which this wave stores
-    const u32x4 z = {0, 0, 0, 0};
-    if (lane < 32) {
-      const uint16_t* src = lane < 16 ? kn : vn;
-      uint16_t* dst = (lane < 16 ? kt : vt) + (n_tail - 1) * kHeadDim;
-      *(u32x4*)(dst + 8 * r) = *(const u32x4*)(src + 8 * r);
-    }
+        if (i1 == per && wave == ((n_blk - i0) & 3)) {
+          // the open block, in bf16: row n_tail - 1 is the new token, which this wave stores
+          const uint16_t* kn = s.k_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
+          const uint16_t* vn = s.v_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
+          uint16_t* kt = a.k_tail + ((int64_t)b * a.H_kv + g) * kCodes;
+          uint16_t* vt = a.v_tail + ((int64_t)b * a.H_kv + g) * kCodes;
+          const u32x4 z = {0, 0, 0, 0};
+          if (lane < 32) {
+            const uint16_t* src = lane < 16 ? kn : vn;
+            uint16_t* dst = (lane < 16 ? kt : vt) + (n_tail - 1) * kHeadDim;
+            *(u32x4*)(dst + 8 * r) = *(const u32x4*)(src + 8 * r);
+          }
 #pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-      const int t = 4 * i + qd;
-      const u32x4 x = t < n_tail - 1 ? *(const u32x4*)(vt + t * kHeadDim + 8 * r)
-                                     : (t == n_tail - 1 ? *(const u32x4*)(vn + 8 * r) : z);
-      *(u32x4*)(stail + t * kTailRow + 16 * r) = x;
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    u32x4 qw[4];
+          for (int i = 0; i < 16; ++i) {
+            const int t = 4 * i + qd;
+            const u32x4 x = t < n_tail - 1 ? *(const u32x4*)(vt + t * kHeadDim + 8 * r)
+                                           : (t == n_tail - 1 ? *(const u32x4*)(vn + 8 * r) : z);
+            *(u32x4*)(stail + t * kTailRow + 16 * r) = x;
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          u32x4 qw[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 32 * i + 8 * qd);
-    f32x4 acc[4];
-    float mt = -INFINITY;
+          for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 32 * i + 8 * qd);
+          f32x4 acc[4];
+          float mt = -INFINITY;
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt) {
-      acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-      const int t = 16 * (r >> 2) + 4 * tt + (r & 3);
-      const uint16_t* row = t < n_tail - 1 ? kt + t * kHeadDim : kn;
+          for (int tt = 0; tt < 4; ++tt) {
+            acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            const int t = 16 * (r >> 2) + 4 * tt + (r & 3);
+            const uint16_t* row = t < n_tail - 1 ? kt + t * kHeadDim : kn;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[tt] = mfma_bf(*(const u32x4*)(row + 32 * i + 8 * qd), qw[i], acc[tt]);
+            for (int i = 0; i < 4; ++i) acc[tt] = mfma_bf(*(const u32x4*)(row + 32 * i + 8 * qd), qw[i], acc[tt]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        acc[tt][i] = 16 * qd + 4 * tt + i < n_tail ? acc[tt][i] * a.scale_log2 : -INFINITY;
-        mt = fmaxf(mt, acc[tt][i]);
-      }
-    }
-    raise(st, rows_max(mt));
-    const float mu = st.m > -INFINITY ? st.m : 0.f;
-    u32x4 p[2];
+            for (int i = 0; i < 4; ++i) {
+              acc[tt][i] = 16 * qd + 4 * tt + i < n_tail ? acc[tt][i] * a.scale_log2 : -INFINITY;
+              mt = fmaxf(mt, acc[tt][i]);
+            }
+          }
+          raise(st, rows_max(mt));
+          const float mu = st.m > -INFINITY ? st.m : 0.f;
+          u32x4 p[2];
 #pragma unroll
-    for (int tt = 0; tt < 4; ++tt)
+          for (int tt = 0; tt < 4; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu), y = __builtin_amdgcn_exp2f(acc[tt][i + 1] - mu);
-        st.l += x + y;
-        const bf16x2 h = {(__bf16)x, (__bf16)y};
-        p[tt >> 1][2 * (tt & 1) + (i >> 1)] = __builtin_bit_cast(uint32_t, h);
-      }
+            for (int i = 0; i < 4; i += 2) {
+              const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu), y = __builtin_amdgcn_exp2f(acc[tt][i + 1] - mu);
+              st.l += x + y;
+              const bf16x2 h = {(__bf16)x, (__bf16)y};
+              p[tt >> 1][2 * (tt & 1) + (i >> 1)] = __builtin_bit_cast(uint32_t, h);
+            }
 #pragma unroll
-    for (int ct = 0; ct < 8; ++ct)
+          for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {   // tokens 16 qd + 8 e + j
-        const uint8_t* src = stail + (16 * qd + 8 * e + (r >> 2)) * kTailRow + 32 * ct + 8 * (r & 3);
-        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src));
-        const u32x2 y =
-            __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 4 * kTailRow)));
-        st.o[ct] = mfma_bf((u32x4){x[0], x[1], y[0], y[1]}, p[e], st.o[ct]);
-      }
-  }
+            for (int e = 0; e < 2; ++e) {   // tokens 16 qd + 8 e + j
+              const uint8_t* src = stail + (16 * qd + 8 * e + (r >> 2)) * kTailRow + 32 * ct + 8 * (r & 3);
+              const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src));
+              const u32x2 y =
+                  __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 4 * kTailRow)));
+              st.o[ct] = mfma_bf((u32x4){x[0], x[1], y[0], y[1]}, p[e], st.o[ct]);
+            }
+        }
 
-  // ---- join the four waves
-  const float l = rows_sum(st.l);
-  if (qd == 0) {
-    sml[wave][r][0] = st.m;
-    sml[wave][r][1] = l;
-  }
+        // ---- join the four waves
+        const float l = rows_sum(st.l);
+        if (r < a.gqa) {
+          if (qd == 0) {
+            sml[wave][r][0] = st.m;
+            sml[wave][r][1] = l;
+          }
+          float* row = so + (wave * a.gqa + r) * kJoinRow + 4 * qd;
 #pragma unroll
-  for (int ct = 0; ct < 8; ++ct) *(f32x4*)&so[wave][r][16 * ct + 4 * qd] = st.o[ct];
-  __syncthreads();
-  for (int e = tid; e < a.gqa * (kHeadDim / 2); e += kThreads) {
-    const int h = e / (kHeadDim / 2), c = 2 * (e % (kHeadDim / 2));
-    float M = -INFINITY;
+          for (int ct = 0; ct < 8; ++ct) *(f32x4*)(row + 16 * ct) = st.o[ct];
+        }
+        __syncthreads();
+        const bool whole = i0 == 0 && i1 == per;
+        const int64_t slot = (int64_t)part + (int64_t)b * a.H_kv + g;   // both grow: no two segments share one
+        for (int e = tid; e < a.gqa * (kHeadDim / 4); e += kThreads) {
+          const int h = e / (kHeadDim / 4), c = 4 * (e % (kHeadDim / 4));
+          float M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, sml[w][h][0]);
-    const float mu = M > -INFINITY ? M : 0.f;
-    float L = 0.f, x = 0.f, y = 0.f;
+          for (int v = 0; v < 4; ++v) M = fmaxf(M, sml[v][h][0]);
+          const float mu = M > -INFINITY ? M : 0.f;
+          float L = 0.f;
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = __builtin_amdgcn_exp2f(sml[w][h][0] - mu);
-      L = fmaf(f, sml[w][h][1], L);
-      x = fmaf(f, so[w][h][c], x);
-      y = fmaf(f, so[w][h][c + 1], y);
+          for (int v = 0; v < 4; ++v) {
+            const float f = __builtin_amdgcn_exp2f(sml[v][h][0] - mu);
+            L = fmaf(f, sml[v][h][1], L);
+            const f32x4 y = *(const f32x4*)(so + (v * a.gqa + h) * kJoinRow + c);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
+          }
+          if (whole) {
+            const bf16x2 v0 = {(__bf16)(x[0] / L), (__bf16)(x[1] / L)}, v1 = {(__bf16)(x[2] / L), (__bf16)(x[3] / L)};
+            *(u32x2*)(s.out + ((int64_t)b * a.H_q + g * a.gqa + h) * kHeadDim + c) =
+                (u32x2){__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1)};
+          } else {
+            *(f32x4*)(s.part_o + (slot * a.gqa + h) * kHeadDim + c) = x;
+            if (c == 0) s.part_ml[slot * a.gqa + h] = make_float2(M, L);
+          }
+        }
+        __syncthreads();
+      }
     }
-    const bf16x2 v = {(__bf16)(x / L), (__bf16)(y / L)};
-    *(bf16x2*)(s.out + ((int64_t)b * a.H_q + g * a.gqa + h) * kHeadDim + c) = v;
   }
+}
 
-  if (n_tail == kBlk) {   // the token filled its block
-    const int page = page_of(a, b, n_blk);
+// Joins the parts of the pairs that more than one workgroup served, one workgroup per
+// (place, query head): eight groups of 32 lanes take the parts in turn.  The workgroups past
+// those quantize the blocks that the step's token filled, one per (place, KV head).
+__global__ __launch_bounds__(kThreads) void k_block_merge(BlockArgs a, BlockStep s, int n_parts) {
+  __shared__ f32x4 sx[8][kHeadDim / 4];
+  __shared__ float2 sml[8];
+  const int tid = threadIdx.x;
+  if (blockIdx.x >= a.B * a.H_q) {
+    __shared__ CloseLds sm;
+    const int pair = blockIdx.x - a.B * a.H_q, b = pair / a.H_kv, g = pair % a.H_kv;
+    const int pos = a.lens[b];
+    if (pos < 0 || pos >= a.max_context || pos % kBlk != kBlk - 1) return;
+    const int page = page_of(a, b, pos / kBlk);
     if (page < 0) return;
+    const uint16_t* kt = a.k_tail + (int64_t)pair * kCodes;
+    const uint16_t* vt = a.v_tail + (int64_t)pair * kCodes;
     const int64_t e = (int64_t)page * a.H_kv + g;
-    close_block([&](int t) { return t < kBlk - 1 ? kt + t * kHeadDim : kn; },
-                [&](int t) { return t < kBlk - 1 ? vt + t * kHeadDim : vn; }, a.k_codes + e * kCodes,
-                a.v_codes + e * kCodes, a.k_scale + e, a.v_scale + e, sm);
+    close_block([&](int t) { return kt + t * kHeadDim; }, [&](int t) { return vt + t * kHeadDim; },
+                a.k_codes + e * kCodes, a.v_codes + e * kCodes, a.k_scale + e, a.v_scale + e, sm);
+    return;
   }
+  const int b = blockIdx.x / a.H_q, head = blockIdx.x % a.H_q, g = head / a.gqa;
+  const int per = items_of(a.lens[b], a.max_context);
+  if (per == 0) return;
+  int before;
+  const int64_t total = (int64_t)count_items(a, b, &before) * a.H_kv;
+  const int64_t parts = min((int64_t)n_parts, total);
+  const int64_t first = (int64_t)before * a.H_kv + (int64_t)g * per;
+  // the part of item i is the largest p with floor(total p / parts) <= i
+  const int p0 = (int)(((first + 1) * parts - 1) / total), p1 = (int)(((first + per) * parts - 1) / total);
+  if (p0 == p1) return;   // written by the attention pass
+  const int64_t row0 = ((int64_t)p0 + (int64_t)b * a.H_kv + g) * a.gqa + head % a.gqa;
+  const int n = p1 - p0 + 1, grp = tid >> 5, c = tid & 31;
+  float M = -INFINITY, L = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int i = grp; i < n; i += 8) {
+    const int64_t row = row0 + (int64_t)i * a.gqa;
+    const float2 ml = s.part_ml[row];
+    const f32x4 y = *(const f32x4*)(s.part_o + row * kHeadDim + 4 * c);
+    const float mn = fmaxf(M, ml.x), mu = mn > -INFINITY ? mn : 0.f;
+    const float f0 = __builtin_amdgcn_exp2f(M - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
+    M = mn;
+    L = fmaf(f1, ml.y, f0 * L);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = fmaf(f1, y[j], f0 * x[j]);
+  }
+  sx[grp][c] = x;
+  if (c == 0) sml[grp] = make_float2(M, L);
+  __syncthreads();
+  if (grp) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) M = fmaxf(M, sml[i].x);
+  const float mu = M > -INFINITY ? M : 0.f;
+  L = 0.f;
+  x = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float f = __builtin_amdgcn_exp2f(sml[i].x - mu);
+    L = fmaf(f, sml[i].y, L);
+    const f32x4 y = sx[i][c];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = fmaf(f, y[j], x[j]);
+  }
+  const bf16x2 v0 = {(__bf16)(x[0] / L), (__bf16)(x[1] / L)}, v1 = {(__bf16)(x[2] / L), (__bf16)(x[3] / L)};
+  *(u32x2*)(s.out + ((int64_t)b * a.H_q + head) * kHeadDim + 4 * c) =
+      (u32x2){__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1)};
 }
 
 // Workgroups of the packed kernels (an upper bound: every sequence may end inside a block).
@@ -542,8 +698,19 @@ hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream
   k_block_fetch<<<dim3((uint32_t)n), kThreads, 0, st>>>(a, r);
   return hipGetLastError();
 }
-hipError_t launch_block_attend(const BlockArgs& a, const BlockStep& s, hipStream_t st) {
-  k_block_attend<<<dim3(a.H_kv, a.B), kThreads, 0, st>>>(a, s);
+
+// Partial rows of a step: at most one segment per (workgroup, pair) step in item order.
+static int64_t part_rows(int64_t B, int H_kv, int gqa) { return (kParts + B * H_kv) * gqa; }
+int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa) {
+  return part_rows(B, H_kv, gqa) * (int64_t)(sizeof(float2) + kHeadDim * sizeof(float));
+}
+
+hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace, hipStream_t st) {
+  s.part_o = (float*)workspace;
+  s.part_ml = (float2*)(s.part_o + part_rows(a.B, a.H_kv, a.gqa) * kHeadDim);
+  k_block_attend<<<dim3(kParts), kThreads, (size_t)4 * a.gqa * kJoinRow * sizeof(float), st>>>(a, s);
+  if (hipError_t e = hipGetLastError()) return e;
+  k_block_merge<<<dim3(a.B * (a.H_q + a.H_kv)), kThreads, 0, st>>>(a, s, kParts);
   return hipGetLastError();
 }
 

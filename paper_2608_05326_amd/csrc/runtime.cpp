@@ -46,7 +46,8 @@ hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st);
 int64_t block_packed_groups(int64_t total, int n_seqs, int H_kv);
 hipError_t launch_block_store(const BlockArgs& a, const PackedRows& r, hipStream_t st);
 hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream_t st);
-hipError_t launch_block_attend(const BlockArgs& a, const BlockStep& s, hipStream_t st);
+int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa);
+hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace, hipStream_t st);
 }  // namespace qv
 
 using namespace qv;
@@ -1437,8 +1438,8 @@ qevict_status qevict_prompt_attend(const qevict_prompt_config* cfg, const uint16
   return e == hipSuccess ? QEVICT_OK : hip_fail(e, "prompt_attend launch");
 }
 
-static qevict_status block_args(const qevict_block_config* cfg, const qevict_block_layer* layer, BlockArgs* a) {
-  if (!cfg || !layer) return fail(QEVICT_ERR_INVALID_ARG, "config or layer is NULL");
+static qevict_status check_block_config(const qevict_block_config* cfg) {
+  if (!cfg) return fail(QEVICT_ERR_INVALID_ARG, "config is NULL");
   qevict_status s =
       check_heads(cfg->abi_version, cfg->num_q_heads, cfg->num_kv_heads, cfg->head_dim, cfg->softmax_scale);
   if (s) return s;
@@ -1446,8 +1447,18 @@ static qevict_status block_args(const qevict_block_config* cfg, const qevict_blo
     return fail(QEVICT_ERR_UNSUPPORTED, "at most 16 query heads per KV head");
   if (cfg->batch < 1 || cfg->max_context < 1 || cfg->num_pages < 0)
     return fail(QEVICT_ERR_INVALID_ARG, "batch and max_context must be positive, num_pages not negative");
-  if (cfg->max_context > ((int32_t)1 << 30) || (int64_t)cfg->batch * cfg->num_kv_heads > kMaxGroups)
+  // the items of a step (blocks of all places and KV heads) are counted in 32 bits
+  if (cfg->max_context > ((int32_t)1 << 30) ||
+      (int64_t)cfg->batch * (cfg->num_q_heads + cfg->num_kv_heads) > kMaxGroups ||
+      (int64_t)cfg->batch * cfg->num_kv_heads > INT32_MAX / (cfg->max_context / kBlockTokens + 2))
     return fail(QEVICT_ERR_UNSUPPORTED, "max_context or batch too large");
+  return QEVICT_OK;
+}
+
+static qevict_status block_args(const qevict_block_config* cfg, const qevict_block_layer* layer, BlockArgs* a) {
+  qevict_status s = check_block_config(cfg);
+  if (s) return s;
+  if (!layer) return fail(QEVICT_ERR_INVALID_ARG, "layer is NULL");
   if (cfg->num_pages && (!layer->k_codes || !layer->v_codes || !layer->k_scale || !layer->v_scale))
     return fail(QEVICT_ERR_INVALID_ARG, "null page pointer");
   if (!layer->k_tail || !layer->v_tail || !layer->table || !layer->lens)
@@ -1534,16 +1545,30 @@ qevict_status qevict_block_fetch(const qevict_block_config* cfg, const qevict_bl
   return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_fetch launch");
 }
 
+qevict_status qevict_block_workspace_size(const qevict_block_config* cfg, size_t* bytes) {
+  qevict_status s = check_block_config(cfg);
+  if (s) return s;
+  if (!bytes) return fail(QEVICT_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = (size_t)block_workspace_bytes(cfg->batch, cfg->num_kv_heads, cfg->num_q_heads / cfg->num_kv_heads);
+  return QEVICT_OK;
+}
+
 qevict_status qevict_block_attend(const qevict_block_config* cfg, const qevict_block_layer* layer, const uint16_t* q,
-                                  const uint16_t* k_new, const uint16_t* v_new, uint16_t* out, void* hip_stream) {
+                                  const uint16_t* k_new, const uint16_t* v_new, uint16_t* out, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream) {
   BlockArgs a;
   qevict_status s = block_args(cfg, layer, &a);
   if (s) return s;
   if (!q || !k_new || !v_new || !out) return fail(QEVICT_ERR_INVALID_ARG, "null pointer");
   if (((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)out) & 15)
     return fail(QEVICT_ERR_INVALID_ARG, "q, k_new, v_new and out must be 16-byte aligned");
-  BlockStep step = {q, k_new, v_new, out};
-  hipError_t e = launch_block_attend(a, step, (hipStream_t)hip_stream);
+  if (!workspace || ((uintptr_t)workspace & 255))
+    return fail(QEVICT_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+  const int64_t need = block_workspace_bytes(a.B, a.H_kv, a.gqa);
+  if (workspace_bytes < (size_t)need)
+    return fail(QEVICT_ERR_WORKSPACE, "workspace has %zu bytes, needs %lld", workspace_bytes, (long long)need);
+  BlockStep step = {q, k_new, v_new, out, nullptr, nullptr};
+  hipError_t e = launch_block_attend(a, step, workspace, (hipStream_t)hip_stream);
   return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_attend launch");
 }
 

@@ -40,7 +40,7 @@ SYMBOLS = (
     "qevict_status_string", "qevict_last_error", "qevict_prefill_scores_scratch_size",
     "qevict_prefill_scores", "qevict_capacities_for_budget", "qevict_memory_report",
     "qevict_prefill_scores_noalloc", "qevict_prompt_attend", "qevict_block_store", "qevict_block_fetch",
-    "qevict_block_attend",
+    "qevict_block_workspace_size", "qevict_block_attend",
 )
 
 
@@ -177,7 +177,8 @@ def load_library(path: str | None = None):
         "qevict_prompt_attend": [P(_PromptConfig), vp, vp, vp, vp, vp, vp],
         "qevict_block_store": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, i32, vp],
         "qevict_block_fetch": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, i32, vp],
-        "qevict_block_attend": [P(_BlockConfig), P(_BlockLayer), vp, vp, vp, vp, vp],
+        "qevict_block_workspace_size": [P(_BlockConfig), P(ctypes.c_size_t)],
+        "qevict_block_attend": [P(_BlockConfig), P(_BlockLayer), vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -543,7 +544,8 @@ class BlockCache:
     (before the block they are for is complete).  lens starts at -1: the program sets it after
     storing a prompt and advances it after each step (advance()).
 
-    Assigning to one of them copies into it.  Calls run on torch's current stream unless the cache was given one."""
+    Assigning to one of them copies into it.  Steps of one cache share its workspace and open
+    blocks: they run one after the other.  Calls run on torch's current stream unless the cache was given one."""
 
     def __init__(self, cfg: BlockConfig, device="cuda", stream=None):
         import torch
@@ -565,6 +567,9 @@ class BlockCache:
         cols = -(-cfg.max_context // n)
         pages = cfg.num_pages or B * cols
         self.num_pages = pages
+        self._c = _BlockConfig(ABI_VERSION, B, cfg.num_q_heads, h, d, cfg.max_context, pages, cfg.softmax_scale)
+        need = ctypes.c_size_t()
+        _check(self.lib, self.lib.qevict_block_workspace_size(ctypes.byref(self._c), ctypes.byref(need)))
         z = torch.zeros
         self._state = dict(
             k_codes=z((L, pages, h, n, d), dtype=torch.int8, device=dev),
@@ -577,7 +582,7 @@ class BlockCache:
             lens=torch.full((B,), -1, dtype=torch.int32, device=dev))
         if not cfg.num_pages:
             self.table.copy_(torch.arange(pages, dtype=torch.int32).view(B, cols))
-        self._c = _BlockConfig(ABI_VERSION, B, cfg.num_q_heads, h, d, cfg.max_context, pages, cfg.softmax_scale)
+        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
         self._layers = [_BlockLayer(*[
             (t if name in ("table", "lens") else t[i]).data_ptr() for name, t in self._state.items()])
             for i in range(L)]
@@ -622,7 +627,8 @@ class BlockCache:
                 raise ValueError(f"{name} must be on {self.device}, got {x.device}")
         self._call(self.lib.qevict_block_attend, layer, _ptr(q, t.bfloat16, "q", qs),
                    _ptr(k_new, t.bfloat16, "k_new", ks), _ptr(v_new, t.bfloat16, "v_new", ks),
-                   _ptr(out, t.bfloat16, "out", qs))
+                   _ptr(out, t.bfloat16, "out", qs), ctypes.c_void_p(self.workspace.data_ptr()),
+                   self.workspace.numel())
 
     def advance(self):
         """After a step's last layer: lens + 1 where a place holds a sequence that has room."""

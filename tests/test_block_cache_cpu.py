@@ -61,9 +61,10 @@ def _block(call, cfg=None, layer=None, **kw):
     for n, x in (layer or {}).items():
         setattr(p, n, x)
     if call == "attend":
-        a = dict(q=P, k=P, v=P, out=P)
+        a = dict(q=P, k=P, v=P, out=P, ws=P, size=1 << 40)
         a.update(kw)
-        return lib.qevict_block_attend(ctypes.byref(c), ctypes.byref(p), a["q"], a["k"], a["v"], a["out"], None)
+        return lib.qevict_block_attend(ctypes.byref(c), ctypes.byref(p), a["q"], a["k"], a["v"], a["out"],
+                                       a["ws"], a["size"], None)
     a = dict(k=P, k_st=256, k_sh=128, v=P, v_st=256, v_sh=128, cu=P, total=100)
     a.update(kw)
     fn = lib.qevict_block_store if call == "store" else lib.qevict_block_fetch
@@ -113,7 +114,22 @@ def test_fetch_refuses_rows_that_overlap_and_attend_its_tensors():
     assert _block("fetch", v_sh=0) == m.ERR_INVALID_ARG
     for kw in (dict(q=None), dict(k=ODD), dict(v=ODD), dict(out=ctypes.c_void_p((1 << 20) + 2))):
         assert _block("attend", **kw) == m.ERR_INVALID_ARG
+    for kw in (dict(ws=None), dict(ws=ODD), dict(size=0), dict(size=1000)):
+        assert _block("attend", **kw) == m.ERR_WORKSPACE
     assert _block("store", total=0, k=None, v=None, cu=None) == m.OK
+
+
+def test_workspace_size():
+    lib = qv.load_library()
+    c = m._BlockConfig(qv.qevict.ABI_VERSION, 2, 8, 2, 128, 1000, 40, 0.0)
+    n = ctypes.c_size_t()
+    assert lib.qevict_block_workspace_size(ctypes.byref(c), ctypes.byref(n)) == m.OK
+    # a partial row of 128 values, maximum and sum per head of a (part or pair): 4 heads a pair
+    assert n.value % (4 * 130 * 4) == 0 and n.value // (4 * 130 * 4) > 2 * 2
+    assert _block("attend", size=n.value - 1) == m.ERR_WORKSPACE
+    c.batch = 0
+    assert lib.qevict_block_workspace_size(ctypes.byref(c), ctypes.byref(n)) == m.ERR_INVALID_ARG
+    assert lib.qevict_block_workspace_size(None, ctypes.byref(n)) == m.ERR_INVALID_ARG
 
 
 def test_a_block_cache_needs_a_gpu():
