@@ -15,8 +15,6 @@
 // Page layout, one KV head: keys [64][128] (a token's channels together), values [128][64]
 // (a channel's tokens together): each is the order in which the matrix instruction of its
 // product reads it, 16 bytes a lane.
-#include <algorithm>
-
 #include "qv_device.h"
 
 namespace qv {
@@ -62,83 +60,66 @@ __device__ __forceinline__ uint32_t amax_bits(u32x4 x, uint32_t m) {
   return m;
 }
 
-// Quantizes one complete block of one KV head into its page (all 256 threads).  row(r) is
-// the address of token r's keys (values: vrow).  sm: 8 KiB + 512 B of LDS + 8 words.
+// Quantizes the keys (VALUES: the values) of one complete block of one KV head into its
+// page (all 256 threads).  row(t) is the address of token t's channels.
 struct CloseLds {
   uint32_t vt[kHeadDim][kBlk / 4 + 1];   // value codes, four tokens a word
-  uint32_t amax[2][kThreads / 64];
+  uint32_t amax[kThreads / 64];
 };
-template <class KRow, class VRow>
-__device__ __forceinline__ void close_block(KRow krow, VRow vrow, int8_t* kc, int8_t* vc, float* ks, float* vs,
-                                            CloseLds& sm) {
+template <bool VALUES, class Row>
+__device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale, CloseLds& sm) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int c = tid & 15, m = tid >> 4;   // 8-channel chunk, group of four tokens
-  u32x4 xk[4], xv[4];
+  u32x4 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    xk[i] = *(const u32x4*)(krow(4 * m + i) + 8 * c);
-    xv[i] = *(const u32x4*)(vrow(4 * m + i) + 8 * c);
-  }
-  uint32_t ak = 0, av = 0;
+  for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(row(4 * m + i) + 8 * c);
+  uint32_t am = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    ak = amax_bits(xk[i], ak);
-    av = amax_bits(xv[i], av);
-  }
+  for (int i = 0; i < 4; ++i) am = amax_bits(x[i], am);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    ak = max(ak, (uint32_t)__shfl_xor((int)ak, d, 64));
-    av = max(av, (uint32_t)__shfl_xor((int)av, d, 64));
-  }
-  if (lane == 0) {
-    sm.amax[0][wave] = ak;
-    sm.amax[1][wave] = av;
-  }
+  for (int d = 1; d < 64; d <<= 1) am = max(am, (uint32_t)__shfl_xor((int)am, d, 64));
+  if (lane == 0) sm.amax[wave] = am;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
-    ak = max(ak, sm.amax[0][w]);
-    av = max(av, sm.amax[1][w]);
-  }
-  const float sk = block_scale(ak), sv = block_scale(av);
-  const bool fk = sk == sk, fv = sv == sv;
-  const float ik = 1.f / sk, iv = 1.f / sv;
-  if (tid == 0) {
-    *ks = sk;
-    *vs = sv;
-  }
+  for (int w = 0; w < kThreads / 64; ++w) am = max(am, sm.amax[w]);
+  const float s = block_scale(am), inv = 1.f / s;
+  const bool finite = s == s;
+  if (tid == 0) *scale = s;
+  if constexpr (!VALUES) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t w[2] = {0, 0};
-    if (fk) {
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w[2] = {0, 0};
+      if (finite) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        w[j >> 1] |= (uint32_t)(uint8_t)code_of(lo_f32(xk[i][j]), sk, ik) << (16 * (j & 1));
-        w[j >> 1] |= (uint32_t)(uint8_t)code_of(hi_f32(xk[i][j]), sk, ik) << (16 * (j & 1) + 8);
+        for (int j = 0; j < 4; ++j) {
+          w[j >> 1] |= (uint32_t)(uint8_t)code_of(lo_f32(x[i][j]), s, inv) << (16 * (j & 1));
+          w[j >> 1] |= (uint32_t)(uint8_t)code_of(hi_f32(x[i][j]), s, inv) << (16 * (j & 1) + 8);
+        }
       }
+      *(u32x2*)(codes + (4 * m + i) * kHeadDim + 8 * c) = (u32x2){w[0], w[1]};
     }
-    *(u32x2*)(kc + (4 * m + i) * kHeadDim + 8 * c) = (u32x2){w[0], w[1]};
-  }
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    uint32_t w = 0;
-    if (fv) {
+    for (int j = 0; j < 8; ++j) {
+      uint32_t w = 0;
+      if (finite) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = xv[i][j >> 1];
-        w |= (uint32_t)(uint8_t)code_of(j & 1 ? hi_f32(x) : lo_f32(x), sv, iv) << (8 * i);
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t y = x[i][j >> 1];
+          w |= (uint32_t)(uint8_t)code_of(j & 1 ? hi_f32(y) : lo_f32(y), s, inv) << (8 * i);
+        }
       }
+      sm.vt[8 * c + j][m] = w;
     }
-    sm.vt[8 * c + j][m] = w;
-  }
-  __syncthreads();
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {   // 16 bytes a thread: channel e / 4, tokens 16 (e % 4) ..
-    const int e = tid + kThreads * i;
-    u32x4 x;
+    for (int i = 0; i < 2; ++i) {   // 16 bytes a thread: channel e / 4, tokens 16 (e % 4) ..
+      const int e = tid + kThreads * i;
+      u32x4 y;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = sm.vt[e >> 2][4 * (e & 3) + j];
-    *(u32x4*)(vc + 16 * e) = x;
+      for (int j = 0; j < 4; ++j) y[j] = sm.vt[e >> 2][4 * (e & 3) + j];
+      *(u32x4*)(codes + 16 * e) = y;
+    }
   }
 }
 
@@ -187,30 +168,29 @@ __device__ __forceinline__ int page_of(const BlockArgs& a, int seq, int blk) {
 }
 }  // namespace
 
-// Packed prompts into the cache, one workgroup per (block, KV head).
+// Packed prompts into the cache, one workgroup per (block, KV head, keys or values).
 __global__ __launch_bounds__(kThreads) void k_block_store(BlockArgs a, PackedRows r) {
   __shared__ CloseLds sm;
-  const int g = blockIdx.x % a.H_kv;
+  const bool values = blockIdx.x & 1;
+  const int g = (blockIdx.x >> 1) % a.H_kv;
   PackedBlock w;
-  if (!find_block(r.cu, a.B, r.total, blockIdx.x / a.H_kv, &w)) return;
+  if (!find_block(r.cu, a.B, r.total, (blockIdx.x >> 1) / a.H_kv, &w)) return;
   const int t0 = w.blk * kBlk, n = min(kBlk, min(w.len, a.max_context) - t0);
   if (n <= 0) return;
-  const uint16_t* k = r.k + (int64_t)(w.start + t0) * r.k_st + g * r.k_sh;
-  const uint16_t* v = r.v + (int64_t)(w.start + t0) * r.v_st + g * r.v_sh;
+  const int64_t st = values ? r.v_st : r.k_st;
+  const uint16_t* x = (values ? r.v + g * r.v_sh : r.k + g * r.k_sh) + (int64_t)(w.start + t0) * st;
   if (n == kBlk) {
     const int page = page_of(a, w.seq, w.blk);
     if (page < 0) return;
     const int64_t e = (int64_t)page * a.H_kv + g;
-    close_block([&](int t) { return k + t * r.k_st; }, [&](int t) { return v + t * r.v_st; },
-                a.k_codes + e * kCodes, a.v_codes + e * kCodes, a.k_scale + e, a.v_scale + e, sm);
+    auto row = [&](int t) { return x + t * st; };
+    if (values) close_block<true>(row, a.v_codes + e * kCodes, a.v_scale + e, sm);
+    else close_block<false>(row, a.k_codes + e * kCodes, a.k_scale + e, sm);
     return;
   }
-  const int64_t tail = ((int64_t)w.seq * a.H_kv + g) * kCodes;
-  for (int e = threadIdx.x; e < n * 16; e += kThreads) {
-    const int t = e >> 4, c = 8 * (e & 15);
-    *(u32x4*)(a.k_tail + tail + t * kHeadDim + c) = *(const u32x4*)(k + t * r.k_st + c);
-    *(u32x4*)(a.v_tail + tail + t * kHeadDim + c) = *(const u32x4*)(v + t * r.v_st + c);
-  }
+  uint16_t* tail = (values ? a.v_tail : a.k_tail) + ((int64_t)w.seq * a.H_kv + g) * kCodes;
+  for (int e = threadIdx.x; e < n * 16; e += kThreads)
+    *(u32x4*)(tail + 8 * e) = *(const u32x4*)(x + (e >> 4) * st + 8 * (e & 15));
 }
 
 // The cache back into packed bf16 rows: a token of a complete block is bf16(fl32(c s)), a
@@ -278,11 +258,12 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 }
 
 // ------------------------------------------------------------------ decode attention
-// One token per sequence, in two launches.  The items of a (sequence, KV head) pair are
-// its complete blocks, then its open block; the items of all pairs, in pair order, are cut
-// into equal parts, one per workgroup, whatever the lengths are (they are read on the
-// device).  A workgroup goes through the pairs its part touches (segments); its four waves
-// take a segment's items in turn and are joined in LDS.  A segment that is a whole pair is
+// One token per sequence, in two launches.  In the first, one workgroup per (sequence, KV
+// head) pair takes the open block, and a pair's complete blocks too if they are few; the
+// blocks of all other pairs, in pair order, are cut into equal parts, one per further
+// workgroup, whatever the lengths are (they are read on the device).  Such a workgroup goes
+// through the pairs its part touches (segments); the four waves of a workgroup take a
+// segment's blocks in turn and are joined in LDS.  A pair that one workgroup served is
 // written out; the others leave (maximum, sum, output) rows that k_block_merge joins.
 //
 // A wave's products, by 16x16x32 MFMAs with the G query heads of the KV head as columns
@@ -296,7 +277,14 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // (exact: bf16 has 8 bits; entries 2^-38 below the head's largest round).
 namespace {
 constexpr float kLazyD = 8.f;
-constexpr int kParts = 512;      // workgroups of a step: two per compute unit
+// Two workgroups fit a compute unit (213 registers; at 168, for three, the loop spills):
+// 480 parts leave room for the pairs' own workgroups of a small batch beside them.  8 KV
+// heads: one sequence of 32K 22.2 us a step with 480 parts, 23.1 with 512, 28 with 768.
+constexpr int kParts = 480;
+// A pair of at most kSmall complete blocks (two rounds of four waves) is one workgroup's,
+// and a segment counts as kSegCost blocks beside its own: without either, a part of many
+// short sequences outlasts the others (32 ragged places, 985 MB: 329 -> 191 us).
+constexpr int kSmall = 8, kSegCost = 4;
 
 __device__ __forceinline__ f32x4 mfma_f16(f16x8 x, f16x8 y, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
@@ -341,9 +329,15 @@ __device__ __forceinline__ void raise(Running& st, float mt) {
   }
 }
 
-// Items of a place: its complete blocks and the open one; none without a sequence or room.
+// Complete blocks of a place that holds a sequence with room for a token, else -1.
+__device__ __forceinline__ int blocks_of(int len, int max_context) {
+  return len < 0 || len >= max_context ? -1 : len / kBlk;
+}
+// Items of one of its pairs in the parts: the blocks of a pair that is not small, and what
+// the segment costs (items that hold nothing).
 __device__ __forceinline__ int items_of(int len, int max_context) {
-  return len < 0 || len >= max_context ? 0 : len / kBlk + 1;
+  const int n = blocks_of(len, max_context);
+  return n > kSmall ? n + kSegCost : 0;
 }
 
 // inclusive sum over the wave's lanes
@@ -356,13 +350,25 @@ __device__ __forceinline__ int wave_scan(int x, int lane) {
   return x;
 }
 
-// Items of all places (of one KV head); with a place, *before receives those of the places
-// before it.  At most 2^31 / H_kv (checked on the host).
-__device__ __forceinline__ int count_items(const BlockArgs& a, int place, int* before) {
+// Page of block blk0 + 4 lane, -1 past `end` or without one.
+__device__ __forceinline__ int lane_page(const BlockArgs& a, int b, int blk0, int end) {
+  const int blk = blk0 + 4 * (threadIdx.x & 63);
+  return blk < end ? page_of(a, b, blk) : -1;
+}
+
+// Length in place s0 + lane (-1 past the last).
+__device__ __forceinline__ int lane_len(const BlockArgs& a, int s0) {
+  const int s = s0 + (threadIdx.x & 63);
+  return s < a.B ? a.lens[s] : -1;
+}
+
+// Items of all places (of one KV head), at most 2^31 / H_kv (checked on the host), and
+// those of the places before `place`.  len0: lane_len of the first 64 places.
+__device__ __forceinline__ int count_items(const BlockArgs& a, int len0, int place, int* before) {
   const int lane = threadIdx.x & 63;
   int sum = 0;
   for (int s0 = 0; s0 < a.B; s0 += 64) {
-    const int n = s0 + lane < a.B ? items_of(a.lens[s0 + lane], a.max_context) : 0;
+    const int n = items_of(s0 ? lane_len(a, s0) : len0, a.max_context);
     const int incl = wave_scan(n, lane);
     if (place >= s0 && place < s0 + 64)
       *before = sum + __builtin_amdgcn_readlane(incl, place - s0) - __builtin_amdgcn_readlane(n, place - s0);
@@ -370,6 +376,9 @@ __device__ __forceinline__ int count_items(const BlockArgs& a, int place, int* b
   }
   return sum;
 }
+
+// Items of a part: equal parts but for the last.
+__device__ __forceinline__ int part_items(int total) { return (int)(((uint32_t)total + kParts - 1) / kParts); }
 
 constexpr int kTailRow = 2 * kHeadDim;
 constexpr int kJoinRow = kHeadDim + 4;
@@ -381,287 +390,330 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
   extern __shared__ __attribute__((aligned(16))) float so[];                // [4][gqa][kJoinRow]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, qd = lane >> 4;
+  const int n_pairs = a.B * a.H_kv;
 
-  // ---- this workgroup's part of the items
-  const int64_t total = (int64_t)count_items(a, -1, nullptr) * a.H_kv;
-  const int parts = (int)min((int64_t)gridDim.x, total), part = blockIdx.x;
-  if (part >= parts) return;
-  const int begin = (int)(total * part / parts), end = (int)(total * (part + 1) / parts);
+  // One segment: blocks [i0, i1) of pair (b, g), and the open block with n_tail > 0 tokens
+  // (the new one included); `whole` when that is all of the pair.
+  auto segment = [&](int b, int g, int i0, int i1, int n_tail, bool whole, int64_t slot) {
+    const int hr = min(r, a.gqa - 1);   // columns past the last head repeat it
+    const uint16_t* qp = s.q + ((int64_t)b * a.H_q + g * a.gqa + hr) * kHeadDim;
+    Running st;
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < 8; ++ct) st.o[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
 
+    if (16 * wave < n_tail) {
+      // tokens 16 wave .. + 15 of the open block, in bf16 (16x16x16 MFMA for the values: a
+      // lane's four logits are the four tokens it wants); the new token is the last, and
+      // the wave that meets it stores it
+      const int64_t tail = ((int64_t)b * a.H_kv + g) * kCodes;
+      const uint16_t* kn = s.k_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
+      const uint16_t* vn = s.v_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
+      const int t0 = 16 * wave, last = n_tail - 1;
+      u32x4 qw[4], kk[4], vv[4];
+      const uint16_t* krow = t0 + r < last ? a.k_tail + tail + (t0 + r) * kHeadDim : kn;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        qw[i] = *(const u32x4*)(qp + 32 * i + 8 * qd);
+        kk[i] = *(const u32x4*)(krow + 32 * i + 8 * qd);
+        const int t = t0 + 4 * i + qd;
+        vv[i] = *(const u32x4*)((t < last ? a.v_tail + tail + t * kHeadDim : vn) + 8 * r);
+        if (t > last) vv[i] = (u32x4){0, 0, 0, 0};
+      }
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        acc = mfma_bf(kk[i], qw[i], acc);
+        *(u32x4*)(stail + (t0 + 4 * i + qd) * kTailRow + 16 * r) = vv[i];
+        if (t0 + 4 * i + qd == last) *(u32x4*)(a.v_tail + tail + last * kHeadDim + 8 * r) = vv[i];
+        if (t0 + r == last) *(u32x4*)(a.k_tail + tail + last * kHeadDim + 32 * i + 8 * qd) = kk[i];
+      }
+      float mt = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        acc[i] = t0 + 4 * qd + i <= last ? acc[i] * a.scale_log2 : -INFINITY;
+        mt = fmaxf(mt, acc[i]);
+      }
+      st.m = rows_max(mt);
+      const float mu = st.m > -INFINITY ? st.m : 0.f;
+      s16x4 p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = __builtin_amdgcn_exp2f(acc[i] - mu);
+        st.l += x;
+        p[i] = __builtin_bit_cast(short, (__bf16)x);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's rows are in LDS
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(stail + (t0 + 4 * qd + (r >> 2)) * kTailRow + 32 * ct + 8 * (r & 3)));
+        st.o[ct] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, p, st.o[ct], 0, 0, 0);
+      }
+    }
+
+    if (i0 + wave < i1) {
+      // pages and scales of the wave's next 64 blocks, one per lane (a dropped block's
+      // tokens take no part), then the first one's keys: the query is read and scaled
+      // while they are on their way
+      int page = lane_page(a, b, i0 + wave, i1);
+      u32x4 qw[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 64 * (i >> 1) + 16 * qd + 8 * (i & 1));
+      const int row = (16 * (r >> 2) + (r & 3)) * kHeadDim + 16 * qd;   // + 4 tt rows
+      u32x4 kb[8], vb[8];
+      float ks_l, vs_l;
+      uint64_t live;
+      auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + g) * kCodes; };
+      auto load_k = [&](int j) {
+        const int8_t* kc = a.k_codes + entry(j) + row;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 4 * (i >> 1) * kHeadDim + 64 * (i & 1));
+      };
+      auto start = [&]() {
+        live = __ballot(page >= 0);
+        if (live) load_k(__builtin_ctzll(live));
+        const int64_t e = (int64_t)max(page, 0) * a.H_kv + g;
+        ks_l = vs_l = 0.f;
+        if (page >= 0) {
+          ks_l = a.k_scale[e];
+          vs_l = a.v_scale[e];
+        }
+      };
+      start();
+      // query operand: k-step (p, e) covers channels 64 p + 16 qd + 8 e + j
+      uint32_t am = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) am = amax_bits(qw[i], am);
+      am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
+      am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+      // 2^(14 - ex) for a largest magnitude in [2^ex, 2^(ex + 1))
+      const int ex = (int)(am >> 23) - 127;
+      f16x8 qf[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          qf[i][2 * j] = (_Float16)ldexpf(lo_f32(qw[i][j]), 14 - ex);
+          qf[i][2 * j + 1] = (_Float16)ldexpf(hi_f32(qw[i][j]), 14 - ex);
+        }
+      const float qs = ldexpf(a.scale_log2, ex - 14);   // log2 units per (q' c s)
+
+      for (int blk0 = i0 + wave;;) {
+        while (live) {
+          const int j = __builtin_ctzll(live);
+          live &= live - 1;
+          const int8_t* vc = a.v_codes + entry(j) + r * kBlk + 16 * qd;
+#pragma unroll
+          for (int ct = 0; ct < 8; ++ct) vb[ct] = *(const u32x4*)(vc + 16 * ct * kBlk);
+          const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)) * qs;
+          const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
+          f32x4 acc[4];
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt) {
+            acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+              const u32x4 x = kb[2 * tt + p];
+              acc[tt] = mfma_f16(codes_f16(x[0], x[1]), qf[2 * p], acc[tt]);
+              acc[tt] = mfma_f16(codes_f16(x[2], x[3]), qf[2 * p + 1], acc[tt]);
+            }
+          }
+          if (live) load_k(__builtin_ctzll(live));
+          float mt = -INFINITY;
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              acc[tt][i] *= sc;
+              mt = fmaxf(mt, acc[tt][i]);
+            }
+          raise(st, rows_max(mt));
+          const float mu = st.m > -INFINITY ? st.m : 0.f;
+          f16x8 p[2];
+#pragma unroll
+          for (int tt = 0; tt < 4; ++tt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu);
+              st.l += x;
+              p[tt >> 1][4 * (tt & 1) + i] = (_Float16)x;
+            }
+#pragma unroll
+          for (int ct = 0; ct < 8; ++ct) {
+            const u32x4 x = vb[ct];
+            f32x4 y = {0.f, 0.f, 0.f, 0.f};
+            y = mfma_f16(codes_f16(x[0], x[1]), p[0], y);
+            y = mfma_f16(codes_f16(x[2], x[3]), p[1], y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st.o[ct][i] = fmaf(y[i], vs, st.o[ct][i]);
+          }
+        }
+        blk0 += 256;
+        if (blk0 >= i1) break;
+        page = lane_page(a, b, blk0, i1);
+        start();
+      }
+    }
+
+    // ---- join the four waves
+    const float l = rows_sum(st.l);
+    if (r < a.gqa) {
+      if (qd == 0) {
+        sml[wave][r][0] = st.m;
+        sml[wave][r][1] = l;
+      }
+      float* row = so + (wave * a.gqa + r) * kJoinRow + 4 * qd;
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) *(f32x4*)(row + 16 * ct) = st.o[ct];
+    }
+    __syncthreads();
+    for (int e = tid; e < a.gqa * (kHeadDim / 4); e += kThreads) {
+      const int h = e / (kHeadDim / 4), c = 4 * (e % (kHeadDim / 4));
+      float M = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) M = fmaxf(M, sml[v][h][0]);
+      const float mu = M > -INFINITY ? M : 0.f;
+      float L = 0.f;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const float f = __builtin_amdgcn_exp2f(sml[v][h][0] - mu);
+        L = fmaf(f, sml[v][h][1], L);
+        const f32x4 y = *(const f32x4*)(so + (v * a.gqa + h) * kJoinRow + c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
+      }
+      if (whole) {
+        const bf16x2 v0 = {(__bf16)(x[0] / L), (__bf16)(x[1] / L)}, v1 = {(__bf16)(x[2] / L), (__bf16)(x[3] / L)};
+        *(u32x2*)(s.out + ((int64_t)b * a.H_q + g * a.gqa + h) * kHeadDim + c) =
+            (u32x2){__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1)};
+      } else {
+        *(f32x4*)(s.part_o + (slot * a.gqa + h) * kHeadDim + c) = x;
+        if (c == 0) s.part_ml[slot * a.gqa + h] = make_float2(M, L);
+      }
+    }
+    __syncthreads();
+  };
+
+  // ---- this workgroup's pair, or its part of the items
+  const bool own_pair = (int)blockIdx.x < n_pairs;
+  const int part = blockIdx.x - n_pairs;
+  int begin = 0, end = INT32_MAX, s_begin = 0, s_end = a.B;
+  if (own_pair) {
+    s_begin = (int)(blockIdx.x / a.H_kv) & ~63;
+    s_end = s_begin + 1;
+  }
+  const int len0 = lane_len(a, s_begin + touch_kernargs<sizeof(BlockArgs) + sizeof(BlockStep)>());
+  if (!own_pair) {
+    int before;
+    const int total = count_items(a, len0, -1, &before) * a.H_kv;
+    const int size = part_items(total);
+    if ((int64_t)part * size >= total) return;
+    begin = part * size;
+    end = min(begin + size, total);
+  }
   int base = 0;   // items before the 64 places of this round
-  for (int s0 = 0; s0 < a.B && base < end; s0 += 64) {
-    const int len = s0 + lane < a.B ? a.lens[s0 + lane] : -1;
+  for (int s0 = s_begin; s0 < s_end && base < end; s0 += 64) {
+    const int len = s0 == s_begin ? len0 : lane_len(a, s0);
     const int n = items_of(len, a.max_context) * a.H_kv;
     const int incl = base + wave_scan(n, lane);
-    // places of the round that the part touches
-    uint64_t mine = __ballot(n > 0 && incl > begin && incl - n < end);
+    // places of the round that the workgroup serves
+    uint64_t mine = own_pair ? (uint64_t)1 << ((blockIdx.x / a.H_kv) & 63)
+                             : __ballot(n > 0 && incl > begin && incl - n < end);
     base = __builtin_amdgcn_readlane(incl, 63);
     for (; mine; mine &= mine - 1) {
       const int w = __builtin_ctzll(mine), b = s0 + w;
       const int pos = __builtin_amdgcn_readlane(len, w);   // position of the new token
-      const int n_blk = pos / kBlk, n_tail = pos % kBlk + 1, per = n_blk + 1;
+      const int n_blk = blocks_of(pos, a.max_context), per = n_blk + kSegCost;
+      if (n_blk < 0) return;
       const int first = __builtin_amdgcn_readlane(incl, w) - per * a.H_kv;
       const int lo = max(begin - first, 0), hi = min(end - first, per * a.H_kv);
-      for (int g = lo / per; g * per < hi; ++g) {
-        // ---- segment: items [i0, i1) of pair (b, g)
-        const int i0 = max(lo - g * per, 0), i1 = min(hi - g * per, per);
-        const int hr = min(r, a.gqa - 1);   // columns past the last head repeat it
-        const uint16_t* qp = s.q + ((int64_t)b * a.H_q + g * a.gqa + hr) * kHeadDim;
-        Running st;
-        st.m = -INFINITY;
-        st.l = 0.f;
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct) st.o[ct] = (f32x4){0.f, 0.f, 0.f, 0.f};
-
-        const int b_end = min(i1, n_blk);
-        if (i0 + wave < b_end) {
-          // query operand: k-step (p, e) covers channels 64 p + 16 qd + 8 e + j
-          u32x4 qw[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 64 * (i >> 1) + 16 * qd + 8 * (i & 1));
-          uint32_t am = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) am = amax_bits(qw[i], am);
-          am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
-          am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
-          // 2^(14 - ex) for a largest magnitude in [2^ex, 2^(ex + 1))
-          const int ex = (int)(am >> 23) - 127;
-          f16x8 qf[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              qf[i][2 * j] = (_Float16)ldexpf(lo_f32(qw[i][j]), 14 - ex);
-              qf[i][2 * j + 1] = (_Float16)ldexpf(hi_f32(qw[i][j]), 14 - ex);
-            }
-          const float qs = ldexpf(a.scale_log2, ex - 14);   // log2 units per (q' c s)
-
-          for (int blk0 = i0 + wave; blk0 < b_end; blk0 += 256) {
-            // pages and scales of the wave's next 64 blocks, one per lane; a dropped block's
-            // tokens take no part
-            const int blk = blk0 + 4 * lane;
-            const int page = blk < b_end ? page_of(a, b, blk) : -1;
-            const int64_t e = (int64_t)max(page, 0) * a.H_kv + g;
-            float ks_l = 0.f, vs_l = 0.f;
-            if (page >= 0) {
-              ks_l = a.k_scale[e];
-              vs_l = a.v_scale[e];
-            }
-            uint64_t live = __ballot(page >= 0);
-            if (!live) continue;
-            const int row = (16 * (r >> 2) + (r & 3)) * kHeadDim + 16 * qd;   // + 4 tt rows
-            u32x4 kb[8], vb[8];
-            auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + g) * kCodes; };
-            auto load_k = [&](int j) {
-              const int8_t* kc = a.k_codes + entry(j) + row;
-#pragma unroll
-              for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 4 * (i >> 1) * kHeadDim + 64 * (i & 1));
-            };
-            load_k(__builtin_ctzll(live));
-            while (live) {
-              const int j = __builtin_ctzll(live);
-              live &= live - 1;
-              const int8_t* vc = a.v_codes + entry(j) + r * kBlk + 16 * qd;
-#pragma unroll
-              for (int ct = 0; ct < 8; ++ct) vb[ct] = *(const u32x4*)(vc + 16 * ct * kBlk);
-              const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)) * qs;
-              const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
-              f32x4 acc[4];
-#pragma unroll
-              for (int tt = 0; tt < 4; ++tt) {
-                acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                  const u32x4 x = kb[2 * tt + p];
-                  acc[tt] = mfma_f16(codes_f16(x[0], x[1]), qf[2 * p], acc[tt]);
-                  acc[tt] = mfma_f16(codes_f16(x[2], x[3]), qf[2 * p + 1], acc[tt]);
-                }
-              }
-              if (live) load_k(__builtin_ctzll(live));
-              float mt = -INFINITY;
-#pragma unroll
-              for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  acc[tt][i] *= sc;
-                  mt = fmaxf(mt, acc[tt][i]);
-                }
-              raise(st, rows_max(mt));
-              const float mu = st.m > -INFINITY ? st.m : 0.f;
-              f16x8 p[2];
-#pragma unroll
-              for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu);
-                  st.l += x;
-                  p[tt >> 1][4 * (tt & 1) + i] = (_Float16)x;
-                }
-#pragma unroll
-              for (int ct = 0; ct < 8; ++ct) {
-                const u32x4 x = vb[ct];
-                f32x4 y = {0.f, 0.f, 0.f, 0.f};
-                y = mfma_f16(codes_f16(x[0], x[1]), p[0], y);
-                y = mfma_f16(codes_f16(x[2], x[3]), p[1], y);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.o[ct][i] = fmaf(y[i], vs, st.o[ct][i]);
-              }
-            }
-          }
+      const bool small = n_blk <= kSmall;
+      int g = own_pair ? (int)(blockIdx.x % a.H_kv) : lo / per;
+      const int g_end = own_pair ? g + 1 : (hi + per - 1) / per;
+      for (; g < g_end; ++g) {
+        int i0 = max(lo - g * per, 0), i1 = min(hi - g * per, n_blk);
+        if (own_pair) {
+          i0 = 0;
+          i1 = small ? n_blk : 0;
+        } else if (i0 >= i1) {
+          continue;
         }
-
-        if (i1 == per && wave == ((n_blk - i0) & 3)) {
-          // the open block, in bf16: row n_tail - 1 is the new token, which this wave stores
-          const uint16_t* kn = s.k_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
-          const uint16_t* vn = s.v_new + ((int64_t)b * a.H_kv + g) * kHeadDim;
-          uint16_t* kt = a.k_tail + ((int64_t)b * a.H_kv + g) * kCodes;
-          uint16_t* vt = a.v_tail + ((int64_t)b * a.H_kv + g) * kCodes;
-          const u32x4 z = {0, 0, 0, 0};
-          if (lane < 32) {
-            const uint16_t* src = lane < 16 ? kn : vn;
-            uint16_t* dst = (lane < 16 ? kt : vt) + (n_tail - 1) * kHeadDim;
-            *(u32x4*)(dst + 8 * r) = *(const u32x4*)(src + 8 * r);
-          }
-#pragma unroll 4
-          for (int i = 0; i < 16; ++i) {
-            const int t = 4 * i + qd;
-            const u32x4 x = t < n_tail - 1 ? *(const u32x4*)(vt + t * kHeadDim + 8 * r)
-                                           : (t == n_tail - 1 ? *(const u32x4*)(vn + 8 * r) : z);
-            *(u32x4*)(stail + t * kTailRow + 16 * r) = x;
-          }
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          u32x4 qw[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) qw[i] = *(const u32x4*)(qp + 32 * i + 8 * qd);
-          f32x4 acc[4];
-          float mt = -INFINITY;
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt) {
-            acc[tt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            const int t = 16 * (r >> 2) + 4 * tt + (r & 3);
-            const uint16_t* row = t < n_tail - 1 ? kt + t * kHeadDim : kn;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[tt] = mfma_bf(*(const u32x4*)(row + 32 * i + 8 * qd), qw[i], acc[tt]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              acc[tt][i] = 16 * qd + 4 * tt + i < n_tail ? acc[tt][i] * a.scale_log2 : -INFINITY;
-              mt = fmaxf(mt, acc[tt][i]);
-            }
-          }
-          raise(st, rows_max(mt));
-          const float mu = st.m > -INFINITY ? st.m : 0.f;
-          u32x4 p[2];
-#pragma unroll
-          for (int tt = 0; tt < 4; ++tt)
-#pragma unroll
-            for (int i = 0; i < 4; i += 2) {
-              const float x = __builtin_amdgcn_exp2f(acc[tt][i] - mu), y = __builtin_amdgcn_exp2f(acc[tt][i + 1] - mu);
-              st.l += x + y;
-              const bf16x2 h = {(__bf16)x, (__bf16)y};
-              p[tt >> 1][2 * (tt & 1) + (i >> 1)] = __builtin_bit_cast(uint32_t, h);
-            }
-#pragma unroll
-          for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {   // tokens 16 qd + 8 e + j
-              const uint8_t* src = stail + (16 * qd + 8 * e + (r >> 2)) * kTailRow + 32 * ct + 8 * (r & 3);
-              const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)src));
-              const u32x2 y =
-                  __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(src + 4 * kTailRow)));
-              st.o[ct] = mfma_bf((u32x4){x[0], x[1], y[0], y[1]}, p[e], st.o[ct]);
-            }
-        }
-
-        // ---- join the four waves
-        const float l = rows_sum(st.l);
-        if (r < a.gqa) {
-          if (qd == 0) {
-            sml[wave][r][0] = st.m;
-            sml[wave][r][1] = l;
-          }
-          float* row = so + (wave * a.gqa + r) * kJoinRow + 4 * qd;
-#pragma unroll
-          for (int ct = 0; ct < 8; ++ct) *(f32x4*)(row + 16 * ct) = st.o[ct];
-        }
-        __syncthreads();
-        const bool whole = i0 == 0 && i1 == per;
-        const int64_t slot = (int64_t)part + (int64_t)b * a.H_kv + g;   // both grow: no two segments share one
-        for (int e = tid; e < a.gqa * (kHeadDim / 4); e += kThreads) {
-          const int h = e / (kHeadDim / 4), c = 4 * (e % (kHeadDim / 4));
-          float M = -INFINITY;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) M = fmaxf(M, sml[v][h][0]);
-          const float mu = M > -INFINITY ? M : 0.f;
-          float L = 0.f;
-          f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float f = __builtin_amdgcn_exp2f(sml[v][h][0] - mu);
-            L = fmaf(f, sml[v][h][1], L);
-            const f32x4 y = *(const f32x4*)(so + (v * a.gqa + h) * kJoinRow + c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
-          }
-          if (whole) {
-            const bf16x2 v0 = {(__bf16)(x[0] / L), (__bf16)(x[1] / L)}, v1 = {(__bf16)(x[2] / L), (__bf16)(x[3] / L)};
-            *(u32x2*)(s.out + ((int64_t)b * a.H_q + g * a.gqa + h) * kHeadDim + c) =
-                (u32x2){__builtin_bit_cast(uint32_t, v0), __builtin_bit_cast(uint32_t, v1)};
-          } else {
-            *(f32x4*)(s.part_o + (slot * a.gqa + h) * kHeadDim + c) = x;
-            if (c == 0) s.part_ml[slot * a.gqa + h] = make_float2(M, L);
-          }
-        }
-        __syncthreads();
+        // (part and pair grow together: no two segments share a slot)
+        const int64_t slot = own_pair ? (int64_t)blockIdx.x : (int64_t)n_pairs + part + b * a.H_kv + g;
+        segment(b, g, i0, i1, own_pair ? pos % kBlk + 1 : 0, own_pair && small, slot);
       }
     }
   }
 }
 
 // Joins the parts of the pairs that more than one workgroup served, one workgroup per
-// (place, query head): eight groups of 32 lanes take the parts in turn.  The workgroups past
-// those quantize the blocks that the step's token filled, one per (place, KV head).
-__global__ __launch_bounds__(kThreads) void k_block_merge(BlockArgs a, BlockStep s, int n_parts) {
+// (place, query head): eight groups of 32 lanes take the parts in turn.  The workgroups
+// before those quantize the blocks that the step's token filled, one per (place, KV head,
+// keys or values).
+__global__ __launch_bounds__(kThreads) void k_block_merge(BlockArgs a, BlockStep s) {
   __shared__ f32x4 sx[8][kHeadDim / 4];
   __shared__ float2 sml[8];
   const int tid = threadIdx.x;
-  if (blockIdx.x >= a.B * a.H_q) {
+  const int n_close = 2 * a.B * a.H_kv;
+  if ((int)blockIdx.x < n_close) {
     __shared__ CloseLds sm;
-    const int pair = blockIdx.x - a.B * a.H_q, b = pair / a.H_kv, g = pair % a.H_kv;
+    const int pair = blockIdx.x >> 1, b = pair / a.H_kv, g = pair % a.H_kv;
     const int pos = a.lens[b];
     if (pos < 0 || pos >= a.max_context || pos % kBlk != kBlk - 1) return;
     const int page = page_of(a, b, pos / kBlk);
     if (page < 0) return;
-    const uint16_t* kt = a.k_tail + (int64_t)pair * kCodes;
-    const uint16_t* vt = a.v_tail + (int64_t)pair * kCodes;
+    const uint16_t* x = (blockIdx.x & 1 ? a.v_tail : a.k_tail) + (int64_t)pair * kCodes;
     const int64_t e = (int64_t)page * a.H_kv + g;
-    close_block([&](int t) { return kt + t * kHeadDim; }, [&](int t) { return vt + t * kHeadDim; },
-                a.k_codes + e * kCodes, a.v_codes + e * kCodes, a.k_scale + e, a.v_scale + e, sm);
+    auto row = [&](int t) { return x + t * kHeadDim; };
+    if (blockIdx.x & 1) close_block<true>(row, a.v_codes + e * kCodes, a.v_scale + e, sm);
+    else close_block<false>(row, a.k_codes + e * kCodes, a.k_scale + e, sm);
     return;
   }
-  const int b = blockIdx.x / a.H_q, head = blockIdx.x % a.H_q, g = head / a.gqa;
+  const int b = (blockIdx.x - n_close) / a.H_q, head = (blockIdx.x - n_close) % a.H_q, g = head / a.gqa;
   const int per = items_of(a.lens[b], a.max_context);
-  if (per == 0) return;
+  if (per == 0) return;   // no sequence, or written by the attention pass
   int before;
-  const int64_t total = (int64_t)count_items(a, b, &before) * a.H_kv;
-  const int64_t parts = min((int64_t)n_parts, total);
-  const int64_t first = (int64_t)before * a.H_kv + (int64_t)g * per;
-  // the part of item i is the largest p with floor(total p / parts) <= i
-  const int p0 = (int)(((first + 1) * parts - 1) / total), p1 = (int)(((first + per) * parts - 1) / total);
-  if (p0 == p1) return;   // written by the attention pass
-  const int64_t row0 = ((int64_t)p0 + (int64_t)b * a.H_kv + g) * a.gqa + head % a.gqa;
-  const int n = p1 - p0 + 1, grp = tid >> 5, c = tid & 31;
+  const int total = count_items(a, lane_len(a, 0), b, &before) * a.H_kv;
+  const int size = part_items(total);
+  const int first = before * a.H_kv + g * per;
+  const int p0 = first / size, p1 = (first + per - kSegCost - 1) / size;
+  const int pair = b * a.H_kv + g, h = head % a.gqa;
+  // row 0 is the open block's, the others the parts'
+  const int64_t row0 = (int64_t)pair * a.gqa + h, row1 = ((int64_t)a.B * a.H_kv + p0 + pair - 1) * a.gqa + h;
+  const int n = p1 - p0 + 2, grp = tid >> 5, c = tid & 31;
   float M = -INFINITY, L = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int i = grp; i < n; i += 8) {
-    const int64_t row = row0 + (int64_t)i * a.gqa;
-    const float2 ml = s.part_ml[row];
-    const f32x4 y = *(const f32x4*)(s.part_o + row * kHeadDim + 4 * c);
-    const float mn = fmaxf(M, ml.x), mu = mn > -INFINITY ? mn : 0.f;
-    const float f0 = __builtin_amdgcn_exp2f(M - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
-    M = mn;
-    L = fmaf(f1, ml.y, f0 * L);
+  for (int i0 = grp; i0 < n; i0 += 64) {
+    // a round of eight rows, all loads first (rows past the last repeat it, with no weight)
+    float2 ml[8];
+    f32x4 y[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = fmaf(f1, y[j], f0 * x[j]);
+    for (int k = 0; k < 8; ++k) {
+      const int i = min(i0 + 8 * k, n - 1);
+      const int64_t row = i ? row1 + (int64_t)i * a.gqa : row0;
+      ml[k] = s.part_ml[row];
+      y[k] = *(const f32x4*)(s.part_o + row * kHeadDim + 4 * c);
+    }
+    float mn = M;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+    const float mu = mn > -INFINITY ? mn : 0.f;
+    const float f0 = __builtin_amdgcn_exp2f(M - mu);
+    M = mn;
+    L *= f0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= f0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (i0 + 8 * k >= n) break;
+      const float f = __builtin_amdgcn_exp2f(ml[k].x - mu);
+      L = fmaf(f, ml[k].y, L);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = fmaf(f, y[k][j], x[j]);
+    }
   }
   sx[grp][c] = x;
   if (c == 0) sml[grp] = make_float2(M, L);
@@ -690,7 +742,7 @@ int64_t block_packed_groups(int64_t total, int n_seqs, int H_kv) { return (total
 
 hipError_t launch_block_store(const BlockArgs& a, const PackedRows& r, hipStream_t st) {
   const int64_t n = block_packed_groups(r.total, a.B, a.H_kv);
-  k_block_store<<<dim3((uint32_t)n), kThreads, 0, st>>>(a, r);
+  k_block_store<<<dim3((uint32_t)(2 * n)), kThreads, 0, st>>>(a, r);
   return hipGetLastError();
 }
 hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream_t st) {
@@ -699,8 +751,9 @@ hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream
   return hipGetLastError();
 }
 
-// Partial rows of a step: at most one segment per (workgroup, pair) step in item order.
-static int64_t part_rows(int64_t B, int H_kv, int gqa) { return (kParts + B * H_kv) * gqa; }
+// Partial rows of a step: one segment per pair, and one per step from (part, pair) to the
+// next in item order.
+static int64_t part_rows(int64_t B, int H_kv, int gqa) { return (kParts + 2 * B * H_kv) * gqa; }
 int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa) {
   return part_rows(B, H_kv, gqa) * (int64_t)(sizeof(float2) + kHeadDim * sizeof(float));
 }
@@ -708,9 +761,9 @@ int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa) {
 hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace, hipStream_t st) {
   s.part_o = (float*)workspace;
   s.part_ml = (float2*)(s.part_o + part_rows(a.B, a.H_kv, a.gqa) * kHeadDim);
-  k_block_attend<<<dim3(kParts), kThreads, (size_t)4 * a.gqa * kJoinRow * sizeof(float), st>>>(a, s);
+  k_block_attend<<<dim3(a.B * a.H_kv + kParts), kThreads, (size_t)4 * a.gqa * kJoinRow * sizeof(float), st>>>(a, s);
   if (hipError_t e = hipGetLastError()) return e;
-  k_block_merge<<<dim3(a.B * (a.H_q + a.H_kv)), kThreads, 0, st>>>(a, s, kParts);
+  k_block_merge<<<dim3(a.B * (a.H_q + 2 * a.H_kv)), kThreads, 0, st>>>(a, s);
   return hipGetLastError();
 }
 

@@ -176,8 +176,8 @@ struct BlockStep {          // a decode step on the block cache
   const uint16_t* k_new;    // [B][H_kv][d]
   const uint16_t* v_new;
   uint16_t* out;            // [B][H_q][d]
-  float* part_o;            // [kParts + B H_kv][gqa][d] partial output rows
-  float2* part_ml;          // [kParts + B H_kv][gqa] (maximum in log2 units, sum)
+  float* part_o;            // [kParts + 2 B H_kv][gqa][d] partial output rows
+  float2* part_ml;          // [kParts + 2 B H_kv][gqa] (maximum in log2 units, sum)
 };
 
 struct ScorePowArgs {       // p-norm ranking: prompt scores raised to the power p

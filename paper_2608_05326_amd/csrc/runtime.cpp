@@ -1449,8 +1449,8 @@ static qevict_status check_block_config(const qevict_block_config* cfg) {
     return fail(QEVICT_ERR_INVALID_ARG, "batch and max_context must be positive, num_pages not negative");
   // the items of a step (blocks of all places and KV heads) are counted in 32 bits
   if (cfg->max_context > ((int32_t)1 << 30) ||
-      (int64_t)cfg->batch * (cfg->num_q_heads + cfg->num_kv_heads) > kMaxGroups ||
-      (int64_t)cfg->batch * cfg->num_kv_heads > INT32_MAX / (cfg->max_context / kBlockTokens + 2))
+      (int64_t)cfg->batch * (cfg->num_q_heads + 2 * cfg->num_kv_heads) > kMaxGroups ||
+      (int64_t)cfg->batch * cfg->num_kv_heads > INT32_MAX / (cfg->max_context / kBlockTokens + 16))
     return fail(QEVICT_ERR_UNSUPPORTED, "max_context or batch too large");
   return QEVICT_OK;
 }
@@ -1496,7 +1496,7 @@ static qevict_status packed_rows(const BlockArgs& a, const uint16_t* k, int64_t 
   if ((s = check_rows("k", k, total, a.H_kv, k_st, k_sh, written)) ||
       (s = check_rows("v", v, total, a.H_kv, v_st, v_sh, written)))
     return s;
-  if (block_packed_groups(total, a.B, a.H_kv) > kMaxGroups)
+  if (2 * block_packed_groups(total, a.B, a.H_kv) > kMaxGroups)
     return fail(QEVICT_ERR_UNSUPPORTED, "sequences too large for one call");
   r->k = k;
   r->v = v;
