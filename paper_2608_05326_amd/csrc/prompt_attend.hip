@@ -62,14 +62,23 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ int swz_k(int key) { return key & 15; }
 __device__ __forceinline__ int swz_v(int key) { return ((key & 3) << 2) | ((key >> 2) & 3); }
 
+// 16 bytes a lane from global memory to LDS, in lane order from a row that is uniform
+__device__ __forceinline__ void dma16(const void* g, uint8_t* lds_row) {
+  __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)lds_row, 16, 0, 0);
+}
+
 __device__ __forceinline__ bool nonfinite_pair(uint32_t x) {
   return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
 }
 }  // namespace
 
 __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
-  __shared__ __attribute__((aligned(16))) uint8_t sk[kKeys * kRowBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t sv[kKeys * kRowBytes];
+  // two tiles of keys and values, in four arrays: reads of one tile do not wait for the
+  // loads of the next (the compiler tells arrays apart, not parts of one)
+  __shared__ __attribute__((aligned(16))) uint8_t sk0[kKeys * kRowBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t sv0[kKeys * kRowBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t sk1[kKeys * kRowBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t sv1[kKeys * kRowBytes];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
 
@@ -139,19 +148,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
   const int vsub = 8 * (lane & 1);
 
   const int n_tiles = pos_last / kKeys + 1;
-  for (int t = 0; t < n_tiles; ++t) {
-    const int key0 = t * kKeys;
-    __syncthreads();   // the previous tile is consumed
+  // Starts the loads of tile t straight into LDS: a wave's instruction fills four rows, its
+  // lanes in order, so the swizzle is applied to the chunk a lane fetches.
+  auto fetch = [&](int t, uint8_t* sk, uint8_t* sv) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 16 * wave + 4 * i + (lane >> 4);
-      const int64_t key = min(key0 + r, len - 1);   // keys past the prompt are masked
-      *(u32x4*)(sk + r * kRowBytes + 16 * ((lane & 15) ^ swz_k(r))) =
-          *(const u32x4*)(kp + key * a.k_st + 8 * (lane & 15));
-      *(u32x4*)(sv + r * kRowBytes + 16 * ((lane & 15) ^ swz_v(r))) =
-          *(const u32x4*)(vp + key * a.v_st + 8 * (lane & 15));
+      const int64_t key = min(t * kKeys + r, len - 1);   // keys past the prompt are masked
+      dma16(kp + key * a.k_st + 8 * ((lane & 15) ^ swz_k(r)), sk + (16 * wave + 4 * i) * kRowBytes);
+      dma16(vp + key * a.v_st + 8 * ((lane & 15) ^ swz_v(r)), sv + (16 * wave + 4 * i) * kRowBytes);
     }
-    __syncthreads();
+  };
+  auto compute = [&](int t, uint8_t* sk, uint8_t* sv) {
+    const int key0 = t * kKeys;
     // only tiles that reach past the workgroup's first position mask keys
     const bool edge = key0 + kKeys - 1 > pos_first;
     bool odd_values = false;
@@ -251,6 +260,19 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
           }
       }
     }
+  };
+  fetch(0, sk0, sv0);
+  for (int t = 0; t < n_tiles; t += 2) {
+    // a tile's loads have landed and the tile before is consumed: its arrays are free
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < n_tiles) fetch(t + 1, sk1, sv1);
+    compute(t, sk0, sv0);
+    if (t + 1 == n_tiles) break;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 2 < n_tiles) fetch(t + 2, sk0, sv0);
+    compute(t + 1, sk1, sv1);
   }
 
   const float inv = 1.f / half_sum(l);
