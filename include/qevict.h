@@ -418,7 +418,8 @@ qevict_status qevict_join_routing(qevict_cache *c);
  * h / (H_q / H_kv).
  *   q [total, H_q, d], k, v [total, H_kv, d] bf16 packed, out like q
  * A value that is not finite reaches the rows that attend to it and no other.
- * H_q % H_kv == 0; d == 128; total_tokens * H_q <= 2^30. */
+ * H_q % H_kv == 0; d == 128; total_tokens * H_q <= 2^30; token strides of k and
+ * v below 2^23. */
 typedef struct {
   int32_t abi_version;
   int32_t num_seqs;          /* sequences in cu_tokens, >= 1 */

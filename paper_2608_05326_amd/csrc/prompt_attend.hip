@@ -16,7 +16,7 @@
 // the first product's result to the second's operand without moving between lanes.
 // P enters the second product in bf16 (off by at most 2^-8 of itself, the size of the
 // output's own rounding); logits, maximum, sum and output are held in 32 bits.
-#include <algorithm>
+#include <cstdlib>
 
 #include "qv_device.h"
 
@@ -28,10 +28,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-constexpr int kRows = 128;      // (position, head) rows per workgroup
-constexpr int kKeys = 64;       // keys per tile
-constexpr int kThreads = 256;
 constexpr int kRowBytes = 2 * kHeadDim;
+constexpr int kAhead = 3;       // steps that key operands are read ahead
 // the running maximum is raised (and the output rescaled) only when a tile exceeds it by
 // this many powers of two: P stays below 256
 constexpr float kLazy = 8.f;
@@ -72,7 +70,14 @@ __device__ __forceinline__ bool nonfinite_pair(uint32_t x) {
 }
 }  // namespace
 
-__global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
+// RS row sets of 32 rows, KG waves a row set: with one, a wave takes all keys of a 64-key
+// tile; with more, each takes 32 keys of a tile of 32 KG (they are joined at the end).
+template <int RS, int KG>
+__global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a) {
+  constexpr int kThreads = 64 * RS * KG, kWaves = RS * KG;
+  constexpr int kRows = 32 * RS;                 // (position, head) rows of the workgroup
+  constexpr int kKeys = KG == 1 ? 64 : 32 * KG;  // keys per tile
+  constexpr int KT = KG == 1 ? 2 : 1;            // 32-key tiles of a wave in it
   // two tiles of keys and values, in four arrays: reads of one tile do not wait for the
   // loads of the next (the compiler tells arrays apart, not parts of one)
   __shared__ __attribute__((aligned(16))) uint8_t sk0[kKeys * kRowBytes];
@@ -95,7 +100,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
       b = min(max(a.cu[s], 0), a.total);
       n = min(max(a.cu[s + 1], b), a.total) - b;
     }
-    const int tiles = (int)(((int64_t)n * a.gqa + kRows - 1) / kRows);
+    const int tiles = (n * a.gqa + kRows - 1) / kRows;
     int incl = tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -115,16 +120,52 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
     }
   }
   if (!found) return;
-  const int64_t n_rows = (int64_t)len * a.gqa;
-  const int64_t row0 = (int64_t)tile * kRows;
+  const int n_rows = len * a.gqa, row0 = tile * kRows;   // at most 2^30 (checked on the host)
+  const int rw = wave % RS, kg = wave / RS, kw = 32 * kg;   // the wave's row set and first key
+  const int pos_first = row0 / a.gqa, pos_last = min(row0 + kRows - 1, n_rows - 1) / a.gqa;   // of the workgroup
+  const int n_tiles = pos_last / kKeys + 1;
+
+  const uint16_t* kp = a.k + (int64_t)start * a.k_st + g * a.k_sh;
+  const uint16_t* vp = a.v + (int64_t)start * a.v_st + g * a.v_sh;
+  // Starts the loads of tile t straight into LDS: a wave's instruction fills four rows, its
+  // lanes in order, so the swizzle is applied to the chunk a lane fetches.  Byte offsets in a
+  // tile fit 32 bits (checked on the host).
+  constexpr int kLoads = kKeys / 4 / kWaves;
+  const int fr = kKeys / kWaves * wave + (lane >> 4);
+  uint32_t koff[kLoads], voff[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int r = fr + 4 * i;
+    koff[i] = (uint32_t)r * (uint32_t)(2 * a.k_st) + 16 * ((lane & 15) ^ swz_k(r));
+    voff[i] = (uint32_t)r * (uint32_t)(2 * a.v_st) + 16 * ((lane & 15) ^ swz_v(r));
+  }
+  auto fetch = [&](int t, uint8_t* sk, uint8_t* sv) {
+    const uint8_t* kt = (const uint8_t*)(kp + (int64_t)t * kKeys * a.k_st);
+    const uint8_t* vt = (const uint8_t*)(vp + (int64_t)t * kKeys * a.v_st);
+    uint8_t* const dk = sk + kKeys / kWaves * wave * kRowBytes;
+    uint8_t* const dv = sv + kKeys / kWaves * wave * kRowBytes;
+    const int past = t * kKeys + kKeys - len;   // keys past the prompt repeat its last (they are masked)
+    if (past <= 0) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        dma16(kt + koff[i], dk + 4 * i * kRowBytes);
+        dma16(vt + voff[i], dv + 4 * i * kRowBytes);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const uint32_t back = max(fr + 4 * i - (kKeys - 1 - past), 0);
+        dma16(kt + (koff[i] - back * (uint32_t)(2 * a.k_st)), dk + 4 * i * kRowBytes);
+        dma16(vt + (voff[i] - back * (uint32_t)(2 * a.v_st)), dv + 4 * i * kRowBytes);
+      }
+    }
+  };
+  fetch(0, sk0, sv0);
 
   // this lane's row (rows past the prompt's last repeat it and are not stored)
-  const int64_t row = row0 + wave * 32 + lr;
-  const int64_t rowc = min(row, n_rows - 1);
-  const int pos = (int)(rowc / a.gqa), head = g * a.gqa + (int)(rowc % a.gqa);
-  const int pos_first = (int)(row0 / a.gqa);   // of the workgroup
-  const int pos_last = (int)(min(row0 + kRows - 1, n_rows - 1) / a.gqa);
-
+  const int row = row0 + rw * 32 + lr;
+  const int rowc = min(row, n_rows - 1);
+  const int pos = rowc / a.gqa, head = g * a.gqa + rowc % a.gqa;
   u32x4 q[8];
   {
     const uint16_t* p = a.q + (start + pos) * a.q_st + head * a.q_sh + 8 * lh;
@@ -139,26 +180,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
   float m = -INFINITY, l = 0.f;
   const float sc = a.scale_log2;
 
-  const uint16_t* kp = a.k + (int64_t)start * a.k_st + g * a.k_sh;
-  const uint16_t* vp = a.v + (int64_t)start * a.v_st + g * a.v_sh;
-  // LDS addresses: A operand row lr of a 32-key tile is key krow of it
-  const int krow = 16 * (lr >> 4) + 8 * ((lr >> 2) & 1) + 4 * ((lr >> 3) & 1) + (lr & 3);
-  const int vkey = 8 * lh + ((lane >> 2) & 3);                 // + 4 j
-  const int vchunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);   // + 4 c
-  const int vsub = 8 * (lane & 1);
-
-  const int n_tiles = pos_last / kKeys + 1;
-  // Starts the loads of tile t straight into LDS: a wave's instruction fills four rows, its
-  // lanes in order, so the swizzle is applied to the chunk a lane fetches.
-  auto fetch = [&](int t, uint8_t* sk, uint8_t* sv) {
+  // LDS offsets: A operand row lr of a 32-key tile is key krow of it; the swizzles leave
+  // k-step ks at kbase ^ 32 ks (keys) and channels 32 c .. at vbase[] ^ 64 c (values of keys
+  // 8 lh .. + 3 and + 4 .. + 7)
+  const int krow = kw + 16 * (lr >> 4) + 8 * ((lr >> 2) & 1) + 4 * ((lr >> 3) & 1) + (lr & 3);
+  const int kbase = krow * kRowBytes + 16 * (lh ^ swz_k(krow));
+  int vbase[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = 16 * wave + 4 * i + (lane >> 4);
-      const int64_t key = min(t * kKeys + r, len - 1);   // keys past the prompt are masked
-      dma16(kp + key * a.k_st + 8 * ((lane & 15) ^ swz_k(r)), sk + (16 * wave + 4 * i) * kRowBytes);
-      dma16(vp + key * a.v_st + 8 * ((lane & 15) ^ swz_v(r)), sv + (16 * wave + 4 * i) * kRowBytes);
-    }
-  };
+  for (int j = 0; j < 2; ++j) {
+    const int key = kw + 8 * lh + 4 * j + ((lane >> 2) & 3);
+    vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
+  }
+
   auto compute = [&](int t, uint8_t* sk, uint8_t* sv) {
     const int key0 = t * kKeys;
     // only tiles that reach past the workgroup's first position mask keys
@@ -167,7 +200,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
     if (edge) {
       // a masked key's value must not reach a row through 0 * infinity: values that are
       // not finite leave the tile here and are added to the rows that see them below
-      for (int i = 0; i < 4; ++i) {
+#pragma unroll 1
+      for (int i = 0; i < kKeys * 16 / kThreads; ++i) {
         u32x4* p = (u32x4*)sv + tid + kThreads * i;
         u32x4 x = *p;
         bool bad = false;
@@ -186,31 +220,54 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
       odd_values = __syncthreads_or(odd_values);
     }
 
-    f32x16 s[2];
+    if (KG > 1 && key0 + kw > pos_last) return;   // masked for all rows
+    // the operands of either product are read ahead of it: a read takes longer than the
+    // products of one step
+    u32x4 kk[kAhead][KT];
+    auto read_k = [&](int ks) {
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < KT; ++kt)
+        kk[ks % kAhead][kt] = *(const u32x4*)(sk + (kbase ^ (32 * ks)) + 32 * kt * kRowBytes);
+    };
+    u32x4 vv[2][4];
+    auto read_v = [&](int ks) {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                      sv + (vbase[0] ^ (64 * c)) + 16 * ks * kRowBytes)));
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                      sv + (vbase[1] ^ (64 * c)) + 16 * ks * kRowBytes)));
+        vv[ks & 1][c] = (u32x4){x[0], x[1], y[0], y[1]};
+      }
+    };
+    f32x16 s[KT];
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
+    for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const int key = 32 * kt + krow;
-        const u32x4 kk = *(const u32x4*)(sk + key * kRowBytes + 16 * ((2 * ks + lh) ^ swz_k(key)));
-        s[kt] = mfma32(kk, q[ks], s[kt]);
-      }
-    // s[kt][i]: raw logit of key key0 + 32 kt + 16 (i / 8) + 8 lh + i % 8 for this lane's row
+    for (int ks = 0; ks < 8; ++ks) {
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) s[kt] = mfma32(kk[ks % kAhead][kt], q[ks], s[kt]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (ks + kAhead < 8) read_k(ks + kAhead);
+      else if (ks + kAhead == 8) read_v(0);
+    }
+    // s[kt][i]: raw logit of key key0 + kw + 32 kt + 16 (i / 8) + 8 lh + i % 8 for this lane's row
     if (edge) {
-      const int rel = pos - key0 - 8 * lh;
+      const int rel = pos - key0 - kw - 8 * lh;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) s[kt][i] = -INFINITY;
     }
     float mt = -INFINITY;
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mt = fmaxf(mt, s[kt][i]);
     mt = half_max(mt) * sc;
@@ -225,9 +282,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
         for (int i = 0; i < 16; ++i) o[c][i] *= al;
     }
     const float mu = m > -INFINITY ? m : 0.f;
-    u32x4 p[4];
+    u32x4 p[2 * KT];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
         const float e0 = __builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -mu));
@@ -236,20 +293,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
         p[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(e0, e1);
       }
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
+    for (int ks = 0; ks < 2 * KT; ++ks) {
+      if (ks + 1 < 2 * KT) read_v(ks + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int k0 = 16 * ks + vkey;
-        const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(sv + k0 * kRowBytes + 16 * ((4 * c + vchunk) ^ swz_v(k0)) + vsub));
-        const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(sv + (k0 + 4) * kRowBytes + 16 * ((4 * c + vchunk) ^ swz_v(k0 + 4)) + vsub));
-        const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
-        o[c] = mfma32((u32x4){y0[0], y0[1], y1[0], y1[1]}, p[ks], o[c]);
-      }
+      for (int c = 0; c < 4; ++c) o[c] = mfma32(vv[ks & 1][c], p[ks], o[c]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     // o[c][i]: channel 32 c + 8 (i / 4) + 4 lh + i % 4 of this lane's row
     if (odd_values) {
-      for (int r = 0; r < kKeys && key0 + r <= pos; ++r) {
+      for (int r = kw; r < kw + 32 * KT && key0 + r <= pos; ++r) {
         const uint16_t* vr = vp + (int64_t)(key0 + r) * a.v_st + 4 * lh;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -261,7 +314,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
       }
     }
   };
-  fetch(0, sk0, sv0);
   for (int t = 0; t < n_tiles; t += 2) {
     // a tile's loads have landed and the tile before is consumed: its arrays are free
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -275,7 +327,45 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
     compute(t + 1, sk1, sv1);
   }
 
-  const float inv = 1.f / half_sum(l);
+  l = half_sum(l);
+  if constexpr (KG > 1) {
+    // the first wave of a row set takes in the others' maxima, sums and outputs (16 KB a
+    // wave, in the tiles' arrays)
+    __shared__ float2 sml[kWaves][64];
+    constexpr int kPer = kKeys * kRowBytes / 16384;   // waves per array
+    static_assert((KG - 1) * RS <= 4 * kPer, "room for the waves' outputs");
+    auto rows_of = [&](int w) {
+      w -= RS;
+      uint8_t* const arr = w / kPer == 0 ? sk0 : w / kPer == 1 ? sv0 : w / kPer == 2 ? sk1 : sv1;
+      return (float*)(arr + w % kPer * 16384) + lane;
+    };
+    __syncthreads();   // the tiles are consumed
+    if (kg) {
+      sml[wave][lane] = make_float2(m, l);
+      float* so = rows_of(wave);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) so[64 * (16 * c + i)] = o[c][i];
+    }
+    __syncthreads();
+    if (kg) return;
+#pragma unroll
+    for (int j = 1; j < KG; ++j) {
+      const float2 ml = sml[wave + j * RS][lane];
+      const float* so = rows_of(wave + j * RS);
+      const float mn = fmaxf(m, ml.x), mu = mn > -INFINITY ? mn : 0.f;
+      const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
+      m = mn;
+      l = fmaf(f1, ml.y, f0 * l);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] = fmaf(f1, so[64 * (16 * c + i)], f0 * o[c][i]);
+    }
+  }
+
+  const float inv = 1.f / l;
   uint16_t* op = a.out + (start + pos) * a.o_st + head * a.o_sh;
 #pragma unroll
   for (int c = 0; c < 4; ++c)
@@ -295,14 +385,21 @@ __global__ __launch_bounds__(kThreads, 2) void k_prompt_attend(PromptArgs a) {
 }
 
 // Workgroups of a launch (an upper bound: every prompt's last tile may be a partial one).
+static int64_t groups_of(int64_t total, int n_seqs, int gqa, int H_kv, int rows) {
+  return (total * gqa / rows + n_seqs) * H_kv;
+}
 int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv) {
-  return (total * gqa / kRows + n_seqs) * H_kv;
+  return groups_of(total, n_seqs, gqa, H_kv, 32);
 }
 
 hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st) {
-  const int64_t n = prompt_attend_groups(a.total, a.n_seqs, a.gqa, a.H_kv);
-  if (n == 0) return hipSuccess;
-  k_prompt_attend<<<dim3((uint32_t)n), kThreads, 0, st>>>(a);
+  auto n = [&](int rows) { return groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, rows); };
+  static const int mode = getenv("QV_SPLIT") ? atoi(getenv("QV_SPLIT")) : 0;
+  int split = mode ? mode : n(128) >= 512 ? 1 : 4;
+  if (split == 1) k_prompt_attend<4, 1><<<dim3((uint32_t)n(128)), 256, 0, st>>>(a);
+  else if (split == 2) k_prompt_attend<2, 2><<<dim3((uint32_t)n(64)), 256, 0, st>>>(a);
+  else if (split == 4) k_prompt_attend<2, 4><<<dim3((uint32_t)n(64)), 512, 0, st>>>(a);
+  else if (split == 8) k_prompt_attend<4, 2><<<dim3((uint32_t)n(128)), 512, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -1415,6 +1415,8 @@ qevict_status qevict_prompt_attend(const qevict_prompt_config* cfg, const uint16
     return s;
   if (n * hq > ((int64_t)1 << 30) || prompt_attend_groups(n, cfg->num_seqs, hq / hkv, hkv) > kMaxGroups)
     return fail(QEVICT_ERR_UNSUPPORTED, "prompts too large for one call");
+  if (cfg->k_token_stride >= (1 << 23) || cfg->v_token_stride >= (1 << 23))   // 32-bit offsets in a tile
+    return fail(QEVICT_ERR_UNSUPPORTED, "token strides of k and v must be below 2^23");
   PromptArgs a;
   a.q = q;
   a.k = k;

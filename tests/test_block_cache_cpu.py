@@ -42,6 +42,8 @@ def _prompt(q=P, k=P, v=P, cu=P, out=P, **kw):
     (dict(out_head_stride=0), m.ERR_INVALID_ARG),
     (dict(total_tokens=1 << 28, out_token_stride=1024), m.ERR_UNSUPPORTED),
     (dict(num_seqs=1 << 30), m.ERR_UNSUPPORTED),
+    (dict(k_token_stride=1 << 23), m.ERR_UNSUPPORTED),
+    (dict(v_token_stride=1 << 24), m.ERR_UNSUPPORTED),
 ])
 def test_prompt_attend_refuses(kw, status):
     assert _prompt(**kw) == status
