@@ -16,7 +16,7 @@
 // the first product's result to the second's operand without moving between lanes.
 // P enters the second product in bf16 (off by at most 2^-8 of itself, the size of the
 // output's own rounding); logits, maximum, sum and output are held in 32 bits.
-#include <cstdlib>
+#include <algorithm>
 
 #include "qv_device.h"
 
@@ -389,17 +389,28 @@ static int64_t groups_of(int64_t total, int n_seqs, int gqa, int H_kv, int rows)
   return (total * gqa / rows + n_seqs) * H_kv;
 }
 int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv) {
-  return groups_of(total, n_seqs, gqa, H_kv, 32);
+  return groups_of(total, n_seqs, gqa, H_kv, 64);
+}
+
+// Which form: 128 rows and four waves that take all keys, two such workgroups to a compute
+// unit, or 64 rows and eight waves, four to a row set, one to a unit.  The second ends its
+// longest row sooner but pays its start and join for half as many rows.  Estimated from the
+// prompts' mean length t, a launch takes the larger of its longest workgroup and its sum
+// over the chip, in microseconds (measured on one prompt of 2067 tokens and 8 heads: 47 and
+// 30; 4096: 88 and 65; 8192: 201 and 218; on 1024 tokens of 32/8 heads: 27 and 29; on 32
+// prompts of 100 tokens: 23 and 57).
+static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
+  const float t = (float)a.total / a.n_seqs;
+  const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.74f + 5.f) / 512);
+  const float eight = std::max(t / 128 * 1.35f + 8.f, n64 * (t / 256 * 1.35f + 8.f) / 256);
+  return eight < four;
 }
 
 hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st) {
-  auto n = [&](int rows) { return groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, rows); };
-  static const int mode = getenv("QV_SPLIT") ? atoi(getenv("QV_SPLIT")) : 0;
-  int split = mode ? mode : n(128) >= 512 ? 1 : 4;
-  if (split == 1) k_prompt_attend<4, 1><<<dim3((uint32_t)n(128)), 256, 0, st>>>(a);
-  else if (split == 2) k_prompt_attend<2, 2><<<dim3((uint32_t)n(64)), 256, 0, st>>>(a);
-  else if (split == 4) k_prompt_attend<2, 4><<<dim3((uint32_t)n(64)), 512, 0, st>>>(a);
-  else if (split == 8) k_prompt_attend<4, 2><<<dim3((uint32_t)n(128)), 512, 0, st>>>(a);
+  const int64_t n128 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 128);
+  const int64_t n64 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 64);
+  if (eight_waves(a, n128, n64)) k_prompt_attend<2, 4><<<dim3((uint32_t)n64), 512, 0, st>>>(a);
+  else k_prompt_attend<4, 1><<<dim3((uint32_t)n128), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -442,45 +442,50 @@ class Cache:
 
 
 # ------------------------------------------- prompts and the 8-bit block cache
-def _rows(t, torch, device, name, heads=None, tokens=None):
-    """Address and (token, head) strides of a packed bf16 tensor [tokens, heads, d]."""
-    if not t.is_cuda or t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
-    if t.dtype != torch.bfloat16:
+# (these calls cost the GPU a few microseconds when they are small, so their marshalling
+# asks each tensor for its shape, strides and device index once)
+def _rows(t, torch, index, name, heads=None, tokens=None, dim=None):
+    """Address and (token, head) strides of a packed bf16 tensor [tokens, heads, d] on
+    device `index`."""
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must be on device cuda:{index}, got {t.device}")
+    if t.dtype is not torch.bfloat16:
         raise ValueError(f"{name} must be torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or \
-            (tokens is not None and t.shape[0] != tokens):
+    sh = t.shape
+    if len(sh) != 3 or (heads is not None and sh[1] != heads) or (tokens is not None and sh[0] != tokens) or \
+            (dim is not None and sh[2] != dim):
         raise ValueError(f"{name} must be [{'T' if tokens is None else tokens}, "
-                         f"{'H' if heads is None else heads}, d], got shape {tuple(t.shape)}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+                         f"{'H' if heads is None else heads}, {'d' if dim is None else dim}], "
+                         f"got shape {tuple(sh)}")
+    st = t.stride()
+    if st[2] != 1 and sh[2] > 1:
         raise ValueError(f"{name}: the channels of a row must be contiguous")
     # the stride of a dimension of size 1 is never used (and may be anything)
-    return ctypes.c_void_p(t.data_ptr()), t.stride(0) if t.shape[0] > 1 else 0, \
-        t.stride(1) if t.shape[1] > 1 else 0
+    return t.data_ptr(), st[0] if sh[0] > 1 else 0, st[1] if sh[1] > 1 else 0
 
 
-def _int32(t, torch, device, name, shape):
-    if not t.is_cuda or t.device != device or t.dtype != torch.int32 or not t.is_contiguous() or \
-            tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {shape} on {device}, "
+def _int32(t, torch, index, name, n):
+    if t.get_device() != index or t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] != n or \
+            not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} entries on device cuda:{index}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
-class _OnDevice:
-    """The device current for a call (a kernel runs on the current device)."""
-
-    def __init__(self, torch, device):
-        self.torch, self.index = torch, device.index
-
-    def __enter__(self):
-        self.before = self.torch.cuda.current_device()
-        if self.before != self.index:
-            self.torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            self.torch.cuda.set_device(self.before)
+def _launch(lib, torch, index, stream, fn, *args):
+    """A handle-free call with the device of its tensors current (kernels run on the
+    current device), on `stream` or torch's current one there."""
+    before = torch.cuda.current_device()
+    if before != index:
+        torch.cuda.set_device(index)
+    try:
+        st = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(index)
+        status = fn(*args, st)
+    finally:
+        if before != index:
+            torch.cuda.set_device(before)
+    if status != OK:
+        _check(lib, status)
 
 
 def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stream=None):
@@ -491,28 +496,22 @@ def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stre
     [H, T, d] tensors).  cu_tokens: int32 [n + 1] on the device.  Returns out, bf16
     [T, H_q, d]; rows behind the last prompt are left as they were (undefined in an out
     that is allocated here).  Runs on `stream`, by default torch's current one."""
-    import torch
     lib = load_library()
-    dev = q.device
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError(f"q and k must be [T, H, d], got shapes {tuple(q.shape)} and {tuple(k.shape)}")
+    import torch
+    index = q.get_device()
+    qp, q_st, q_sh = _rows(q, torch, index, "q")
     T, hq, d = q.shape
+    kp, k_st, k_sh = _rows(k, torch, index, "k", None, T, d)
     hkv = k.shape[1]
+    vp, v_st, v_sh = _rows(v, torch, index, "v", hkv, T, d)
     if out is None:
-        out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=dev)
-    qp, q_st, q_sh = _rows(q, torch, dev, "q")
-    kp, k_st, k_sh = _rows(k, torch, dev, "k", hkv, T)
-    vp, v_st, v_sh = _rows(v, torch, dev, "v", hkv, T)
-    op, o_st, o_sh = _rows(out, torch, dev, "out", hq, T)
-    if not k.shape[2] == v.shape[2] == out.shape[2] == d:
-        raise ValueError("q, k, v and out must have the same head dimension")
+        out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=q.device)
+    op, o_st, o_sh = _rows(out, torch, index, "out", hq, T, d)
     n = cu_tokens.numel() - 1
-    cu = _int32(cu_tokens, torch, dev, "cu_tokens", (n + 1,))
+    cu = _int32(cu_tokens, torch, index, "cu_tokens", n + 1)
     c = _PromptConfig(ABI_VERSION, n, T, hq, hkv, d, softmax_scale, q_st, q_sh, k_st, k_sh, v_st, v_sh,
                       o_st, o_sh)
-    with _OnDevice(torch, dev):
-        st = (stream or torch.cuda.current_stream(dev)).cuda_stream
-        _check(lib, lib.qevict_prompt_attend(ctypes.byref(c), qp, kp, vp, cu, op, ctypes.c_void_p(st)))
+    _launch(lib, torch, index, stream, lib.qevict_prompt_attend, ctypes.byref(c), qp, kp, vp, cu, op)
     return out
 
 
@@ -587,24 +586,17 @@ class BlockCache:
             (t if name in ("table", "lens") else t[i]).data_ptr() for name, t in self._state.items()])
             for i in range(L)]
 
-    def _layer(self, layer: int):
+    def _call(self, fn, layer: int, *args):
         if not 0 <= layer < self.cfg.num_layers:
             raise ValueError(f"layer {layer} out of range")
-        return self._layers[layer]
-
-    def _call(self, fn, layer, *args):
-        with _OnDevice(self.torch, self.device):
-            st = (self.stream or self.torch.cuda.current_stream(self.device)).cuda_stream
-            _check(self.lib, fn(ctypes.byref(self._c), ctypes.byref(self._layer(layer)), *args,
-                                ctypes.c_void_p(st)))
+        _launch(self.lib, self.torch, self.device.index, self.stream, fn, ctypes.byref(self._c),
+                ctypes.byref(self._layers[layer]), *args)
 
     def _packed(self, k, v, cu_tokens):
-        t, h = self.torch, self.cfg.num_kv_heads
-        kr = _rows(k, t, self.device, "k", h)
-        vr = _rows(v, t, self.device, "v", h, k.shape[0])
-        if k.shape[2] != self.cfg.head_dim or v.shape[2] != self.cfg.head_dim:
-            raise ValueError(f"k and v must have {self.cfg.head_dim} channels")
-        return (*kr, *vr, _int32(cu_tokens, t, self.device, "cu_tokens", (self.cfg.batch + 1,)), k.shape[0])
+        t, c, i = self.torch, self.cfg, self.device.index
+        kr = _rows(k, t, i, "k", c.num_kv_heads, None, c.head_dim)
+        vr = _rows(v, t, i, "v", c.num_kv_heads, k.shape[0], c.head_dim)
+        return (*kr, *vr, _int32(cu_tokens, t, i, "cu_tokens", c.batch + 1), k.shape[0])
 
     def store(self, layer: int, k, v, cu_tokens):
         """Stores packed prompts: rows cu_tokens[s] .. cu_tokens[s + 1] - 1 of k, v (bf16
@@ -620,15 +612,16 @@ class BlockCache:
     def attend(self, layer: int, q, k_new, v_new, out):
         """One decode step: appends token lens[s] of every place and attends with it.
         q: bf16 [batch, H_q, d]; k_new, v_new: bf16 [batch, H_kv, d]; out: bf16 like q."""
-        t, c = self.torch, self.cfg
-        qs, ks = (c.batch, c.num_q_heads, c.head_dim), (c.batch, c.num_kv_heads, c.head_dim)
-        for x, name in ((q, "q"), (k_new, "k_new"), (v_new, "v_new"), (out, "out")):
-            if x.device != self.device:
-                raise ValueError(f"{name} must be on {self.device}, got {x.device}")
-        self._call(self.lib.qevict_block_attend, layer, _ptr(q, t.bfloat16, "q", qs),
-                   _ptr(k_new, t.bfloat16, "k_new", ks), _ptr(v_new, t.bfloat16, "v_new", ks),
-                   _ptr(out, t.bfloat16, "out", qs), ctypes.c_void_p(self.workspace.data_ptr()),
-                   self.workspace.numel())
+        p = []
+        for x, name, heads in ((q, "q", self.cfg.num_q_heads), (k_new, "k_new", self.cfg.num_kv_heads),
+                               (v_new, "v_new", self.cfg.num_kv_heads), (out, "out", self.cfg.num_q_heads)):
+            if x.get_device() != self.device.index or x.dtype is not self.torch.bfloat16 or \
+                    x.shape != (self.cfg.batch, heads, self.cfg.head_dim) or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous bf16 tensor of shape "
+                                 f"{(self.cfg.batch, heads, self.cfg.head_dim)} on {self.device}, got {x.dtype} "
+                                 f"{tuple(x.shape)} on {x.device}")
+            p.append(x.data_ptr())
+        self._call(self.lib.qevict_block_attend, layer, *p, self.workspace.data_ptr(), self.workspace.numel())
 
     def advance(self):
         """After a step's last layer: lens + 1 where a place holds a sequence that has room."""
