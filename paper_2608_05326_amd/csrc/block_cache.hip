@@ -39,26 +39,29 @@ __device__ __forceinline__ float block_scale(uint32_t amax) {
   return fmaxf(__fdiv_rn(__uint_as_float(amax), 127.f), kMinScale);
 }
 
-// round-half-even(x / s) for finite x: the product with the rounded reciprocal is within
-// one of it, and the signs of x - (c + 1/2) s and x - (c - 1/2) s (one fused operation
-// each, so exact) decide.  inv = 1 / s (s >= 2^-100: no overflow).
-__device__ __forceinline__ int code_of(float x, float s, float inv) {
-  float c = rintf(x * inv);
-  const float up = fmaf(-(c + 0.5f), s, x), dn = fmaf(-(c - 0.5f), s, x);
-  const bool odd = ((int)c & 1) != 0;
-  if (up > 0.f || (up == 0.f && odd)) c += 1.f;
-  else if (dn < 0.f || (dn == 0.f && odd)) c -= 1.f;
-  return (int)c;
+// round-half-even(x / s) for finite x.  The product with the rounded reciprocal is within
+// 2^-15 of x / s, so its nearest integer c is right or off by one.  The rest r = x - c s is
+// exact: c s and x are multiples of the last place of s (a smaller x has c = 0 and r = x)
+// and |r| <= s.  c moves towards r where |r| > s / 2, and an odd c where |r| = s / 2: at
+// s / 2 or at the float after it, compared as integers.  inv = 1 / s (s >= 2^-100: no
+// overflow), half = the bits of s / 2.
+__device__ __forceinline__ uint32_t code_byte(float x, float s, float inv, uint32_t half) {
+  const float c = rintf(x * inv), r = fmaf(-c, s, x);
+  const int ci = (int)c;
+  const uint32_t rb = __float_as_uint(r), from = half + (~ci & 1);
+  return (uint32_t)(ci + ((rb & 0x7FFFFFFFu) >= from ? (int)rb >> 31 | 1 : 0)) & 0xFFu;
 }
 
-__device__ __forceinline__ uint32_t amax_bits(u32x4 x, uint32_t m) {
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+// bf16 magnitudes as integers (NaN and infinity above all others), two at once
+__device__ __forceinline__ uint32_t amax_pair(u32x4 x, uint32_t m) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    m = max(m, (x[j] << 16) & 0x7FFF0000u);
-    m = max(m, x[j] & 0x7FFF0000u);
-  }
+  for (int j = 0; j < 4; ++j)
+    m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m),
+                                                              __builtin_bit_cast(u16x2, x[j] & 0x7FFF7FFFu)));
   return m;
 }
+__device__ __forceinline__ uint32_t amax_bits(uint32_t pair) { return max(pair << 16, pair & 0xFFFF0000u); }
 
 // Quantizes the keys (VALUES: the values) of one complete block of one KV head into its
 // page (all 256 threads).  row(t) is the address of token t's channels.
@@ -75,7 +78,8 @@ __device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale
   for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(row(4 * m + i) + 8 * c);
   uint32_t am = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) am = amax_bits(x[i], am);
+  for (int i = 0; i < 4; ++i) am = amax_pair(x[i], am);
+  am = amax_bits(am);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) am = max(am, (uint32_t)__shfl_xor((int)am, d, 64));
   if (lane == 0) sm.amax[wave] = am;
@@ -83,6 +87,7 @@ __device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) am = max(am, sm.amax[w]);
   const float s = block_scale(am), inv = 1.f / s;
+  const uint32_t half = __float_as_uint(0.5f * s);
   const bool finite = s == s;
   if (tid == 0) *scale = s;
   if constexpr (!VALUES) {
@@ -92,8 +97,8 @@ __device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale
       if (finite) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          w[j >> 1] |= (uint32_t)(uint8_t)code_of(lo_f32(x[i][j]), s, inv) << (16 * (j & 1));
-          w[j >> 1] |= (uint32_t)(uint8_t)code_of(hi_f32(x[i][j]), s, inv) << (16 * (j & 1) + 8);
+          w[j >> 1] |= code_byte(lo_f32(x[i][j]), s, inv, half) << (16 * (j & 1));
+          w[j >> 1] |= code_byte(hi_f32(x[i][j]), s, inv, half) << (16 * (j & 1) + 8);
         }
       }
       *(u32x2*)(codes + (4 * m + i) * kHeadDim + 8 * c) = (u32x2){w[0], w[1]};
@@ -106,7 +111,7 @@ __device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t y = x[i][j >> 1];
-          w |= (uint32_t)(uint8_t)code_of(j & 1 ? hi_f32(y) : lo_f32(y), s, inv) << (8 * i);
+          w |= code_byte(j & 1 ? hi_f32(y) : lo_f32(y), s, inv, half) << (8 * i);
         }
       }
       sm.vt[8 * c + j][m] = w;
@@ -485,7 +490,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
       // query operand: k-step (p, e) covers channels 64 p + 16 qd + 8 e + j
       uint32_t am = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) am = amax_bits(qw[i], am);
+      for (int i = 0; i < 4; ++i) am = amax_pair(qw[i], am);
+      am = amax_bits(am);
       am = max(am, (uint32_t)__shfl_xor((int)am, 16, 64));
       am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
       // 2^(14 - ex) for a largest magnitude in [2^ex, 2^(ex + 1))
