@@ -74,7 +74,7 @@ __device__ __forceinline__ bool nonfinite_pair(uint32_t x) {
 // tile; with more, each takes 32 keys of a tile of 32 KG (they are joined at the end).
 template <int RS, int KG>
 __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a) {
-  constexpr int kThreads = 64 * RS * KG, kWaves = RS * KG;
+  constexpr int kWaves = RS * KG;
   constexpr int kRows = 32 * RS;                 // (position, head) rows of the workgroup
   constexpr int kKeys = KG == 1 ? 64 : 32 * KG;  // keys per tile
   constexpr int KT = KG == 1 ? 2 : 1;            // 32-key tiles of a wave in it
@@ -84,6 +84,7 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   __shared__ __attribute__((aligned(16))) uint8_t sv0[kKeys * kRowBytes];
   __shared__ __attribute__((aligned(16))) uint8_t sk1[kKeys * kRowBytes];
   __shared__ __attribute__((aligned(16))) uint8_t sv1[kKeys * kRowBytes];
+  __shared__ int sodd[2][kWaves];   // a tile held values that are not finite
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
 
@@ -127,11 +128,11 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
 
   const uint16_t* kp = a.k + (int64_t)start * a.k_st + g * a.k_sh;
   const uint16_t* vp = a.v + (int64_t)start * a.v_st + g * a.v_sh;
-  // Starts the loads of tile t straight into LDS: a wave's instruction fills four rows, its
-  // lanes in order, so the swizzle is applied to the chunk a lane fetches.  Byte offsets in a
-  // tile fit 32 bits (checked on the host).
+  // Starts the loads of a tile straight into LDS: a wave's instruction fills four rows, its
+  // lanes in order, so the swizzle is applied to the chunk a lane fetches.  Byte offsets in
+  // a tile fit 32 bits (checked on the host).
   constexpr int kLoads = kKeys / 4 / kWaves;
-  const int fr = kKeys / kWaves * wave + (lane >> 4);
+  const int fr0 = kKeys / kWaves * wave, fr = fr0 + (lane >> 4);
   uint32_t koff[kLoads], voff[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i) {
@@ -139,33 +140,31 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     koff[i] = (uint32_t)r * (uint32_t)(2 * a.k_st) + 16 * ((lane & 15) ^ swz_k(r));
     voff[i] = (uint32_t)r * (uint32_t)(2 * a.v_st) + 16 * ((lane & 15) ^ swz_v(r));
   }
-  auto fetch = [&](int t, uint8_t* sk, uint8_t* sv) {
-    const uint8_t* kt = (const uint8_t*)(kp + (int64_t)t * kKeys * a.k_st);
-    const uint8_t* vt = (const uint8_t*)(vp + (int64_t)t * kKeys * a.v_st);
-    uint8_t* const dk = sk + kKeys / kWaves * wave * kRowBytes;
-    uint8_t* const dv = sv + kKeys / kWaves * wave * kRowBytes;
+  auto fetch = [&](int t, const uint16_t* base, int64_t stride, const uint32_t (&off)[kLoads], uint8_t* tile) __attribute__((always_inline)) {
+    if (t >= n_tiles) return;
+    const uint8_t* src = (const uint8_t*)(base + (int64_t)t * kKeys * stride);
+    uint8_t* const dst = tile + fr0 * kRowBytes;
     const int past = t * kKeys + kKeys - len;   // keys past the prompt repeat its last (they are masked)
     if (past <= 0) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        dma16(kt + koff[i], dk + 4 * i * kRowBytes);
-        dma16(vt + voff[i], dv + 4 * i * kRowBytes);
-      }
+      for (int i = 0; i < kLoads; ++i) dma16(src + off[i], dst + 4 * i * kRowBytes);
     } else {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         const uint32_t back = max(fr + 4 * i - (kKeys - 1 - past), 0);
-        dma16(kt + (koff[i] - back * (uint32_t)(2 * a.k_st)), dk + 4 * i * kRowBytes);
-        dma16(vt + (voff[i] - back * (uint32_t)(2 * a.v_st)), dv + 4 * i * kRowBytes);
+        dma16(src + (off[i] - back * (uint32_t)(2 * stride)), dst + 4 * i * kRowBytes);
       }
     }
   };
-  fetch(0, sk0, sv0);
+  fetch(0, kp, a.k_st, koff, sk0);
 
   // this lane's row (rows past the prompt's last repeat it and are not stored)
   const int row = row0 + rw * 32 + lr;
   const int rowc = min(row, n_rows - 1);
   const int pos = rowc / a.gqa, head = g * a.gqa + rowc % a.gqa;
+  // first and last position of the wave's rows, and the tiles in which it has keys to see
+  const int wpos0 = (row0 + rw * 32) / a.gqa, wpos1 = min(row0 + rw * 32 + 31, n_rows - 1) / a.gqa;
+  const int n_mine = row0 + rw * 32 < n_rows && wpos1 >= kw ? (wpos1 - kw) / kKeys + 1 : 0;
   u32x4 q[8];
   {
     const uint16_t* p = a.q + (start + pos) * a.q_st + head * a.q_sh + 8 * lh;
@@ -192,43 +191,14 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
   }
 
-  auto compute = [&](int t, uint8_t* sk, uint8_t* sv) {
-    const int key0 = t * kKeys;
-    // only tiles that reach past the workgroup's first position mask keys
-    const bool edge = key0 + kKeys - 1 > pos_first;
-    bool odd_values = false;
-    if (edge) {
-      // a masked key's value must not reach a row through 0 * infinity: values that are
-      // not finite leave the tile here and are added to the rows that see them below
-#pragma unroll 1
-      for (int i = 0; i < kKeys * 16 / kThreads; ++i) {
-        u32x4* p = (u32x4*)sv + tid + kThreads * i;
-        u32x4 x = *p;
-        bool bad = false;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= nonfinite_pair(x[j]);
-        if (bad) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
-            if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
-          }
-          *p = x;
-        }
-        odd_values |= bad;
-      }
-      odd_values = __syncthreads_or(odd_values);
-    }
+  // only tiles that reach past the workgroup's first position hold masked keys
+  auto edge = [&](int t) { return t * kKeys + kKeys - 1 > pos_first; };
+  f32x16 s[KT];
+  u32x4 p[2 * KT];
 
-    if (KG > 1 && key0 + kw > pos_last) return;   // masked for all rows
-    // the operands of either product are read ahead of it: a read takes longer than the
-    // products of one step
-    u32x4 kk[kAhead][KT];
-    auto read_k = [&](int ks) {
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-        kk[ks % kAhead][kt] = *(const u32x4*)(sk + (kbase ^ (32 * ks)) + 32 * kt * kRowBytes);
-    };
+  // o += V^T P^T of tile t.  Operands are read ahead of their products: a read takes longer
+  // than the products of one step.
+  auto values = [&](int t, const uint8_t* sv) __attribute__((always_inline)) {
     u32x4 vv[2][4];
     auto read_v = [&](int ks) {
 #pragma unroll
@@ -240,7 +210,42 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
         vv[ks & 1][c] = (u32x4){x[0], x[1], y[0], y[1]};
       }
     };
-    f32x16 s[KT];
+    read_v(0);
+#pragma unroll
+    for (int ks = 0; ks < 2 * KT; ++ks) {
+      if (ks + 1 < 2 * KT) read_v(ks + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = mfma32(vv[ks & 1][c], p[ks], o[c]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // o[c][i]: channel 32 c + 8 (i / 4) + 4 lh + i % 4 of this lane's row
+    if (edge(t)) {
+      int odd = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) odd |= sodd[t & 1][w];
+      if (__builtin_amdgcn_readfirstlane(odd)) {   // the values left out of the tile
+        for (int r = kw; r < kw + 32 * KT && t * kKeys + r <= pos; ++r) {
+          const uint16_t* vr = vp + (int64_t)(t * kKeys + r) * a.v_st + 4 * lh;
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint16_t x = vr[32 * c + 8 * (i >> 2) + (i & 3)];
+              if ((x & 0x7F80u) == 0x7F80u) o[c][i] += bf16_to_f32(x);
+            }
+        }
+      }
+    }
+  };
+  // s = K Q^T of tile t
+  auto logits = [&](const uint8_t* sk) __attribute__((always_inline)) {
+    u32x4 kk[kAhead][KT];
+    auto read_k = [&](int ks) {
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+        kk[ks % kAhead][kt] = *(const u32x4*)(sk + (kbase ^ (32 * ks)) + 32 * kt * kRowBytes);
+    };
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -254,11 +259,13 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
       for (int kt = 0; kt < KT; ++kt) s[kt] = mfma32(kk[ks % kAhead][kt], q[ks], s[kt]);
       __builtin_amdgcn_sched_barrier(0);
       if (ks + kAhead < 8) read_k(ks + kAhead);
-      else if (ks + kAhead == 8) read_v(0);
     }
-    // s[kt][i]: raw logit of key key0 + kw + 32 kt + 16 (i / 8) + 8 lh + i % 8 for this lane's row
-    if (edge) {
-      const int rel = pos - key0 - kw - 8 * lh;
+  };
+  // p = exp2(s - m), l and o kept relative to m
+  auto weights = [&](int t) __attribute__((always_inline)) {
+    // s[kt][i]: raw logit of key t kKeys + kw + 32 kt + 16 (i / 8) + 8 lh + i % 8 for this lane's row
+    if (t * kKeys + kw + 32 * KT - 1 > wpos0) {
+      const int rel = pos - t * kKeys - kw - 8 * lh;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -282,7 +289,6 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
         for (int i = 0; i < 16; ++i) o[c][i] *= al;
     }
     const float mu = m > -INFINITY ? m : 0.f;
-    u32x4 p[2 * KT];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -292,39 +298,61 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
         l += e0 + e1;
         p[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(e0, e1);
       }
+  };
+  // A masked key's value must not reach a row through 0 * infinity: values that are not
+  // finite leave an edge tile, in the rows this wave has loaded, and are added to the rows
+  // that see them after its products.
+  auto clean = [&](int t, uint8_t* sv) __attribute__((always_inline)) {
+    int odd = 0;
+#pragma unroll 1
+    for (int i = 0; i < kLoads; ++i) {
+      u32x4* const at = (u32x4*)(sv + (fr0 + 4 * i) * kRowBytes) + lane;
+      u32x4 x = *at;
+      bool bad = false;
 #pragma unroll
-    for (int ks = 0; ks < 2 * KT; ++ks) {
-      if (ks + 1 < 2 * KT) read_v(ks + 1);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 4; ++j) bad |= nonfinite_pair(x[j]);
+      if (bad) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) o[c] = mfma32(vv[ks & 1][c], p[ks], o[c]);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // o[c][i]: channel 32 c + 8 (i / 4) + 4 lh + i % 4 of this lane's row
-    if (odd_values) {
-      for (int r = kw; r < kw + 32 * KT && key0 + r <= pos; ++r) {
-        const uint16_t* vr = vp + (int64_t)(key0 + r) * a.v_st + 4 * lh;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint16_t x = vr[32 * c + 8 * (i >> 2) + (i & 3)];
-            if ((x & 0x7F80u) == 0x7F80u) o[c][i] += bf16_to_f32(x);
-          }
+        for (int j = 0; j < 4; ++j) {
+          if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
+          if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
+        }
+        *at = x;
+        odd = 1;
       }
     }
+    odd = __any(odd);
+    if (lane == 0) sodd[t & 1][wave] = odd;
   };
+  // loads landed and LDS writes done, for all waves
+  auto landed = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  // Tile t: the products of the values of the tile before and of its own keys, then its
+  // weights.  Meanwhile the next tile's keys and its own values arrive; the arrays they
+  // fill were last read in the products of the tile before.
+  auto step = [&](int t, uint8_t* sk, uint8_t* sv_before, uint8_t* sk_next, uint8_t* sv) __attribute__((always_inline)) {
+    fetch(t + 1, kp, a.k_st, koff, sk_next);
+    fetch(t, vp, a.v_st, voff, sv);
+    if (t > 0 && t - 1 < n_mine) values(t - 1, sv_before);
+    if (t < n_mine) logits(sk);
+    if (t < n_mine) weights(t);
+    if (edge(t)) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      clean(t, sv);
+    }
+    landed();
+  };
+  landed();
   for (int t = 0; t < n_tiles; t += 2) {
-    // a tile's loads have landed and the tile before is consumed: its arrays are free
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t + 1 < n_tiles) fetch(t + 1, sk1, sv1);
-    compute(t, sk0, sv0);
-    if (t + 1 == n_tiles) break;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (t + 2 < n_tiles) fetch(t + 2, sk0, sv0);
-    compute(t + 1, sk1, sv1);
+    step(t, sk0, sv1, sk1, sv0);
+    if (t + 1 < n_tiles) step(t + 1, sk1, sv0, sk0, sv1);
+  }
+  if (n_tiles - 1 < n_mine) {
+    if (n_tiles & 1) values(n_tiles - 1, sv0);
+    else values(n_tiles - 1, sv1);
   }
 
   l = half_sum(l);
@@ -396,9 +424,9 @@ int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv) {
 // unit, or 64 rows and eight waves, four to a row set, one to a unit.  The second ends its
 // longest row sooner but pays its start and join for half as many rows.  Estimated from the
 // prompts' mean length t, a launch takes the larger of its longest workgroup and its sum
-// over the chip, in microseconds (measured on one prompt of 2067 tokens and 8 heads: 47 and
-// 30; 4096: 88 and 65; 8192: 201 and 218; on 1024 tokens of 32/8 heads: 27 and 29; on 32
-// prompts of 100 tokens: 23 and 57).
+// over the chip, in microseconds (measured on one prompt of 2067 tokens and 8 heads: 46 and
+// 30; 4096: 87 and 64; 8192: 204 and 217; on 1024 tokens of 32/8 heads: 27 and 28; on 32
+// prompts of 100 tokens: 24 and 58).
 static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
   const float t = (float)a.total / a.n_seqs;
   const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.74f + 5.f) / 512);
