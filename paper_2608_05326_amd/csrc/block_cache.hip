@@ -128,43 +128,6 @@ __device__ __forceinline__ void close_block(Row row, int8_t* codes, float* scale
   }
 }
 
-// Where a workgroup of the packed kernels works: block `blk` of sequence `seq`, whose rows
-// start at `start` in the packed order and number `len`.
-struct PackedBlock {
-  int seq, blk, start, len;
-};
-// The idx-th block of the packed sequences (every sequence has ceil(len / 64)); false past
-// the last.  The same in every lane of every wave.
-__device__ __forceinline__ bool find_block(const int32_t* cu, int n_seqs, int total, int idx, PackedBlock* out) {
-  const int lane = threadIdx.x & 63;
-  for (int s0 = 0; s0 < n_seqs; s0 += 64) {
-    const int s = s0 + lane;
-    int b = 0, n = 0;
-    if (s < n_seqs) {
-      b = min(max(cu[s], 0), total);
-      n = min(max(cu[s + 1], b), total) - b;
-    }
-    const int blocks = n / kBlk + (n % kBlk != 0);
-    int incl = blocks;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(incl, d, 64);
-      if (lane >= d) incl += o;
-    }
-    const uint64_t past = __ballot(incl > idx);
-    if (past) {
-      const int w = __builtin_ctzll(past);
-      out->seq = s0 + w;
-      out->start = __builtin_amdgcn_readlane(b, w);
-      out->len = __builtin_amdgcn_readlane(n, w);
-      out->blk = idx - (__builtin_amdgcn_readlane(incl, w) - __builtin_amdgcn_readlane(blocks, w));
-      return true;
-    }
-    idx -= __builtin_amdgcn_readlane(incl, 63);
-  }
-  return false;
-}
-
 // Page of a sequence's block; -1 when the table holds none (dropped, or out of range).
 __device__ __forceinline__ int page_of(const BlockArgs& a, int seq, int blk) {
   if (blk >= a.n_cols) return -1;
@@ -178,14 +141,14 @@ __global__ __launch_bounds__(kThreads) void k_block_store(BlockArgs a, PackedRow
   __shared__ CloseLds sm;
   const bool values = blockIdx.x & 1;
   const int g = (blockIdx.x >> 1) % a.H_kv;
-  PackedBlock w;
-  if (!find_block(r.cu, a.B, r.total, (blockIdx.x >> 1) / a.H_kv, &w)) return;
-  const int t0 = w.blk * kBlk, n = min(kBlk, min(w.len, a.max_context) - t0);
+  PackedTile w;
+  if (!find_tile(r.cu, a.B, r.total, 1, kBlk, (blockIdx.x >> 1) / a.H_kv, &w)) return;
+  const int t0 = w.tile * kBlk, n = min(kBlk, min(w.len, a.max_context) - t0);
   if (n <= 0) return;
   const int64_t st = values ? r.v_st : r.k_st;
   const uint16_t* x = (values ? r.v + g * r.v_sh : r.k + g * r.k_sh) + (int64_t)(w.start + t0) * st;
   if (n == kBlk) {
-    const int page = page_of(a, w.seq, w.blk);
+    const int page = page_of(a, w.seq, w.tile);
     if (page < 0) return;
     const int64_t e = (int64_t)page * a.H_kv + g;
     auto row = [&](int t) { return x + t * st; };
@@ -204,14 +167,14 @@ __global__ __launch_bounds__(kThreads) void k_block_store(BlockArgs a, PackedRow
 __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRows r) {
   __shared__ uint32_t vt[kHeadDim][kBlk / 4 + 1];
   const int g = blockIdx.x % a.H_kv, tid = threadIdx.x;
-  PackedBlock w;
-  if (!find_block(r.cu, a.B, r.total, blockIdx.x / a.H_kv, &w)) return;
+  PackedTile w;
+  if (!find_tile(r.cu, a.B, r.total, 1, kBlk, blockIdx.x / a.H_kv, &w)) return;
   const int held = min(a.lens[w.seq], a.max_context);
-  const int t0 = w.blk * kBlk, n = min(min(kBlk, w.len - t0), held - t0);
+  const int t0 = w.tile * kBlk, n = min(min(kBlk, w.len - t0), held - t0);
   if (n <= 0) return;
   uint16_t* k = r.k_out + (int64_t)(w.start + t0) * r.k_st + g * r.k_sh;
   uint16_t* v = r.v_out + (int64_t)(w.start + t0) * r.v_st + g * r.v_sh;
-  if (w.blk >= held / kBlk) {
+  if (w.tile >= held / kBlk) {
     const int64_t tail = ((int64_t)w.seq * a.H_kv + g) * kCodes;
     for (int e = tid; e < n * 16; e += kThreads) {
       const int t = e >> 4, c = 8 * (e & 15);
@@ -220,7 +183,7 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
     }
     return;
   }
-  const int page = page_of(a, w.seq, w.blk);
+  const int page = page_of(a, w.seq, w.tile);
   const int64_t e0 = (int64_t)max(page, 0) * a.H_kv + g;
   const int c = tid & 15, m = tid >> 4;
   float sk = 0.f, sv = 0.f;
@@ -367,19 +330,24 @@ __device__ __forceinline__ int lane_len(const BlockArgs& a, int s0) {
   return s < a.B ? a.lens[s] : -1;
 }
 
-// Items of all places (of one KV head), at most 2^31 / H_kv (checked on the host), and
+// Items of all places (of one KV head), at most 2^30 / H_kv (checked on the host), and
 // those of the places before `place`.  len0: lane_len of the first 64 places.
 __device__ __forceinline__ int count_items(const BlockArgs& a, int len0, int place, int* before) {
   const int lane = threadIdx.x & 63;
-  int sum = 0;
-  for (int s0 = 0; s0 < a.B; s0 += 64) {
-    const int n = items_of(s0 ? lane_len(a, s0) : len0, a.max_context);
-    const int incl = wave_scan(n, lane);
-    if (place >= s0 && place < s0 + 64)
-      *before = sum + __builtin_amdgcn_readlane(incl, place - s0) - __builtin_amdgcn_readlane(n, place - s0);
-    sum += __builtin_amdgcn_readlane(incl, 63);
+  int sum = items_of(len0, a.max_context), pre = lane < place ? sum : 0;
+#pragma unroll 4
+  for (int s0 = 64; s0 < a.B; s0 += 64) {
+    const int n = items_of(lane_len(a, s0), a.max_context);
+    sum += n;
+    pre += s0 + lane < place ? n : 0;
   }
-  return sum;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    sum += __shfl_xor(sum, d, 64);
+    pre += __shfl_xor(pre, d, 64);
+  }
+  *before = __builtin_amdgcn_readfirstlane(pre);
+  return __builtin_amdgcn_readfirstlane(sum);
 }
 
 // Items of a part: equal parts but for the last.

@@ -88,39 +88,11 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
 
-  // ---- this workgroup's KV head, prompt and rows: tiles of all prompts are numbered in
-  // prompt order, the longest tile of a prompt first
-  const int g = blockIdx.x % a.H_kv;
-  int tile = blockIdx.x / a.H_kv;
-  int start = 0, len = 0;
-  bool found = false;
-  for (int s0 = 0; s0 < a.n_seqs && !found; s0 += 64) {
-    const int s = s0 + lane;
-    int b = 0, n = 0;
-    if (s < a.n_seqs) {
-      b = min(max(a.cu[s], 0), a.total);
-      n = min(max(a.cu[s + 1], b), a.total) - b;
-    }
-    const int tiles = (n * a.gqa + kRows - 1) / kRows;
-    int incl = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(incl, d, 64);
-      if (lane >= d) incl += o;
-    }
-    const uint64_t past = __ballot(incl > tile);
-    if (past) {
-      const int w = __builtin_ctzll(past);
-      start = __builtin_amdgcn_readlane(b, w);
-      len = __builtin_amdgcn_readlane(n, w);
-      // the tile's number inside its prompt, counted from the prompt's end
-      tile = __builtin_amdgcn_readlane(incl, w) - 1 - tile;
-      found = true;
-    } else {
-      tile -= __builtin_amdgcn_readlane(incl, 63);
-    }
-  }
-  if (!found) return;
+  // ---- this workgroup's KV head, prompt and rows, the longest tile of a prompt first
+  const int g = (int)(blockIdx.x % a.H_kv) + touch_kernargs<sizeof(PromptArgs)>();
+  PackedTile pt;
+  if (!find_tile(a.cu, a.n_seqs, a.total, a.gqa, kRows, blockIdx.x / a.H_kv, &pt)) return;
+  const int start = pt.start, len = pt.len, tile = pt.n_tiles - 1 - pt.tile;
   const int n_rows = len * a.gqa, row0 = tile * kRows;   // at most 2^30 (checked on the host)
   const int rw = wave % RS, kg = wave / RS, kw = 32 * kg;   // the wave's row set and first key
   const int pos_first = row0 / a.gqa, pos_last = min(row0 + kRows - 1, n_rows - 1) / a.gqa;   // of the workgroup
@@ -430,6 +402,7 @@ int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv) {
 static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
   const float t = (float)a.total / a.n_seqs;
   const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.74f + 5.f) / 512);
+  if (n64 >= 4096) return false;
   const float eight = std::max(t / 128 * 1.35f + 8.f, n64 * (t / 256 * 1.35f + 8.f) / 256);
   return eight < four;
 }

@@ -137,6 +137,39 @@ struct ObsArgs {            // initial window scores from the observation querie
   float* scores;            // [B][n_w]
 };
 
+// The packed sequence a workgroup serves, its tiles of `rows` rows numbered so that no
+// prefix sums are needed: sequence s has G = `per` rows a token and owns the numbers from
+// floor(cu[s] G / rows) + s on, never fewer than its tiles (a difference of floors plus one
+// is at least the ceiling of the difference), so a search over cu finds it, 64 entries a
+// step.  cu is read within [0, total]; false when tile `idx` is nobody's.  The same in
+// every lane.
+struct PackedTile {
+  int seq, start, len, tile, n_tiles;   // tile: the number inside the sequence, < n_tiles
+};
+__device__ __forceinline__ bool find_tile(const int32_t* cu, int n_seqs, int total, int per, int rows, int idx,
+                                          PackedTile* out) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = n_seqs;   // the sequence is one of [lo, lo + n)
+  for (;;) {
+    const int step = (n + 63) / 64, s = lo + min(lane * step, n - 1);
+    const int b = min(max(cu[s], 0), total), e = min(max(cu[s + 1], b), total);
+    const int base = (int)((int64_t)b * per / rows) + s;
+    const uint64_t below = __ballot(base <= idx && lane * step < n);
+    if (!below) return false;
+    const int w = 63 - __builtin_clzll(below);
+    if (step == 1) {
+      out->seq = lo + w;
+      out->start = __builtin_amdgcn_readlane(b, w);
+      out->len = __builtin_amdgcn_readlane(e, w) - out->start;
+      out->tile = idx - __builtin_amdgcn_readlane(base, w);
+      out->n_tiles = (int)(((int64_t)out->len * per + rows - 1) / rows);
+      return out->tile < out->n_tiles;
+    }
+    lo += w * step;
+    n = min(step, n - w * step);
+  }
+}
+
 struct PromptArgs {         // causal attention of packed prompts
   const uint16_t* q;        // rows [total] x heads, strides in elements
   const uint16_t* k;

@@ -1452,7 +1452,7 @@ static qevict_status check_block_config(const qevict_block_config* cfg) {
   // the items of a step (blocks of all places and KV heads) are counted in 32 bits
   if (cfg->max_context > ((int32_t)1 << 30) ||
       (int64_t)cfg->batch * (cfg->num_q_heads + 2 * cfg->num_kv_heads) > kMaxGroups ||
-      (int64_t)cfg->batch * cfg->num_kv_heads > INT32_MAX / (cfg->max_context / kBlockTokens + 16))
+      (int64_t)cfg->batch * cfg->num_kv_heads > ((int32_t)1 << 30) / (cfg->max_context / kBlockTokens + 16))
     return fail(QEVICT_ERR_UNSUPPORTED, "max_context or batch too large");
   return QEVICT_OK;
 }

@@ -244,6 +244,23 @@ def test_attend_longer(lens):
     _step(bc, lens, seed=4, scale=2.0)
 
 
+def test_many_places():
+    """300 places (more than a wave's 64 lanes count at once), some empty, a few long."""
+    rng = np.random.default_rng(7)
+    lens = rng.integers(-1, 40, 300)
+    lens[[5, 63, 64, 130, 299]] = [900, 640, 639, 1100, 575]
+    lens = lens.tolist()
+    bc, k, v = _make(lens, 2, 1, seed=34)
+    _step(bc, lens, seed=35)
+    import torch
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    pos = [max(t, 0) for t in lens]
+    bc.fetch(0, ko, vo, _cu(pos))
+    a = sum(pos[:130])
+    assert torch.equal(ko[a + 1088:a + 1100], k[a + 1088:a + 1100])   # place 130's open block
+    assert bool(((ko.float() - k.float()).abs() <= 0.05).all())       # scales: 5 / 127, half a step and a rounding
+
+
 def test_steps_across_block_ends():
     """70 steps of places at different lengths, blocks closing on the way."""
     import torch

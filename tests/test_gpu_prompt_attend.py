@@ -66,7 +66,7 @@ def _check(out, o, A, what=""):
 
 
 LENS = [[1], [2], [63], [64], [65], [127, 1, 129], [0, 5, 0, 0, 200, 0], [31, 33, 300], [777],
-        list(range(1, 80))]
+        list(range(1, 80)), [1500]]
 
 
 @pytest.mark.parametrize("lens", LENS, ids=lambda x: "-".join(map(str, x[:6])))
@@ -86,6 +86,23 @@ def test_wide_groups(hq, hkv):
     lens = [3, 150, 17]
     q, k, v, cu = _inputs(lens, hq, hkv, seed=5)
     _check(qv.prompt_attend(q, k, v, cu), *_reference(q, k, v, lens))
+
+
+def test_many_prompts():
+    """Thousands of short prompts, empty ones among them, rows before the first."""
+    import torch
+    import paper_2608_05326_amd as qv
+    lens = np.random.default_rng(0).integers(0, 12, 5000).tolist()
+    q, k, v, cu = _inputs(lens, 2, 1, seed=1, extra=40)
+    out = torch.full_like(q, 7.0)
+    qv.prompt_attend(q, k, v, cu, out)
+    n = sum(lens)
+    _check(out[:n], *_reference(q[:n], k[:n], v[:n], lens))
+    assert bool((out[n:] == 7.0).all())
+    out2 = torch.full_like(q, 7.0)
+    qv.prompt_attend(q, k, v, cu[70:].contiguous(), out2)
+    a = int(cu[70])
+    assert bool((out2[:a] == 7.0).all()) and torch.equal(out2[a:], out[a:])
 
 
 @pytest.mark.parametrize("layout", ["fused", "heads_first"])
