@@ -91,7 +91,9 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   // ---- this workgroup's KV head, prompt and rows, the longest tile of a prompt first
   const int g = (int)(blockIdx.x % a.H_kv) + touch_kernargs<sizeof(PromptArgs)>();
   PackedTile pt;
-  if (!find_tile(a.cu, a.n_seqs, a.total, a.gqa, kRows, blockIdx.x / a.H_kv, &pt)) return;
+  int slot = blockIdx.x / a.H_kv;
+  if (slot >= a.fold && slot < a.fold_end) slot = a.fold + a.fold_end - 1 - slot;
+  if (!find_tile(a.cu, a.n_seqs, a.total, a.gqa, kRows, slot, &pt)) return;
   const int start = pt.start, len = pt.len, tile = pt.n_tiles - 1 - pt.tile;
   const int n_rows = len * a.gqa, row0 = tile * kRows;   // at most 2^30 (checked on the host)
   const int rw = wave % RS, kg = wave / RS, kw = 32 * kg;   // the wave's row set and first key
@@ -392,6 +394,8 @@ int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv) {
   return groups_of(total, n_seqs, gqa, H_kv, 64);
 }
 
+constexpr int kUnits = 256;   // compute units
+
 // Which form: 128 rows and four waves that take all keys, two such workgroups to a compute
 // unit, or 64 rows and eight waves, four to a row set, one to a unit.  The second ends its
 // longest row sooner but pays its start and join for half as many rows.  Estimated from the
@@ -407,10 +411,14 @@ static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
   return eight < four;
 }
 
-hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st) {
+hipError_t launch_prompt_attend(PromptArgs a, hipStream_t st) {
   const int64_t n128 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 128);
   const int64_t n64 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 64);
-  if (eight_waves(a, n128, n64)) k_prompt_attend<2, 4><<<dim3((uint32_t)n64), 512, 0, st>>>(a);
+  const bool eight = eight_waves(a, n128, n64);
+  const int64_t slots = (eight ? n64 : n128) / a.H_kv, first = kUnits / a.H_kv;
+  a.fold = (int)std::min(first, slots);
+  a.fold_end = (int)(eight || slots >= 4 * first ? a.fold : std::min(slots, 2 * first));
+  if (eight) k_prompt_attend<2, 4><<<dim3((uint32_t)n64), 512, 0, st>>>(a);
   else k_prompt_attend<4, 1><<<dim3((uint32_t)n128), 256, 0, st>>>(a);
   return hipGetLastError();
 }

@@ -178,6 +178,7 @@ struct PromptArgs {         // causal attention of packed prompts
   int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;   // row and head strides
   const int32_t* cu;        // [n_seqs + 1] first row of each prompt, then the end of the last
   int32_t n_seqs, total, H_kv, gqa;
+  int32_t fold, fold_end;   // tile numbers [fold, fold_end) are served in reverse
   float scale_log2;
 };
 

@@ -42,7 +42,7 @@ hipError_t launch_score_pow(const ScorePowArgs& a, hipStream_t st);
 hipError_t launch_prefill_scores(const ObsArgs& a, hipStream_t st);
 hipError_t static_obs_scratch(void** ptr, const char** what);
 int64_t prompt_attend_groups(int64_t total, int n_seqs, int gqa, int H_kv);
-hipError_t launch_prompt_attend(const PromptArgs& a, hipStream_t st);
+hipError_t launch_prompt_attend(PromptArgs a, hipStream_t st);
 int64_t block_packed_groups(int64_t total, int n_seqs, int H_kv);
 hipError_t launch_block_store(const BlockArgs& a, const PackedRows& r, hipStream_t st);
 hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream_t st);
