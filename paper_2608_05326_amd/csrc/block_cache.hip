@@ -322,13 +322,14 @@ __device__ __forceinline__ int items_of(int len, int max_context) {
   return n > kSmall ? n + kSegCost : 0;
 }
 
-// inclusive sum over the wave's lanes
-__device__ __forceinline__ int wave_scan(int x, int lane) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(x, d, 64);
-    if (lane >= d) x += o;
-  }
+// inclusive sum over the wave's lanes: within rows of 16, then across them
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // from 1, 2, 4, 8 lanes below
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // last lane of rows 0, 2 to rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // lane 31 to rows 2, 3
   return x;
 }
 
@@ -344,24 +345,18 @@ __device__ __forceinline__ int lane_len(const BlockArgs& a, int s0) {
   return s < a.B ? a.lens[s] : -1;
 }
 
-// Items of all places (of one KV head), at most 2^30 / H_kv (checked on the host), and
-// those of the places before `place`.  len0: lane_len of the first 64 places.
-__device__ __forceinline__ int count_items(const BlockArgs& a, int len0, int place, int* before) {
+// Items of the places past the first 64 (of one KV head), and those of them before `place`.
+__device__ __forceinline__ int items_past_64(const BlockArgs& a, int place, int* before) {
   const int lane = threadIdx.x & 63;
-  int sum = items_of(len0, a.max_context), pre = lane < place ? sum : 0;
+  int sum = 0, pre = 0;
 #pragma unroll 4
   for (int s0 = 64; s0 < a.B; s0 += 64) {
     const int n = items_of(lane_len(a, s0), a.max_context);
     sum += n;
     pre += s0 + lane < place ? n : 0;
   }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    sum += __shfl_xor(sum, d, 64);
-    pre += __shfl_xor(pre, d, 64);
-  }
-  *before = __builtin_amdgcn_readfirstlane(pre);
-  return __builtin_amdgcn_readfirstlane(sum);
+  *before = __builtin_amdgcn_readlane(wave_scan(pre), 63);
+  return __builtin_amdgcn_readlane(wave_scan(sum), 63);
 }
 
 // Items of a part: equal parts but for the last.
@@ -595,9 +590,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
     s_end = s_begin + 1;
   }
   const int len0 = lane_len(a, s_begin + touch_kernargs<sizeof(BlockArgs) + sizeof(BlockStep)>());
+  int incl0 = 0;
   if (!own_pair) {
-    int before;
-    const int total = count_items(a, len0, -1, &before) * a.H_kv;
+    incl0 = wave_scan(items_of(len0, a.max_context) * a.H_kv);
+    int total = __builtin_amdgcn_readlane(incl0, 63), before;   // at most 2^30 (checked on the host)
+    if (a.B > 64) total += items_past_64(a, 0, &before) * a.H_kv;
     const int size = part_items(total);
     if ((int64_t)part * size >= total) return;
     begin = part * size;
@@ -607,7 +604,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
   for (int s0 = s_begin; s0 < s_end && base < end; s0 += 64) {
     const int len = s0 == s_begin ? len0 : lane_len(a, s0);
     const int n = items_of(len, a.max_context) * a.H_kv;
-    const int incl = base + wave_scan(n, lane);
+    const int incl = s0 == s_begin ? incl0 : base + wave_scan(n);
     // places of the round that the workgroup serves
     uint64_t mine = own_pair ? (uint64_t)1 << ((blockIdx.x / a.H_kv) & 63)
                              : __ballot(n > 0 && incl > begin && incl - n < end);
@@ -662,11 +659,18 @@ __global__ __launch_bounds__(kThreads) void k_block_merge(BlockArgs a, BlockStep
     return;
   }
   const int b = (blockIdx.x - n_close) / a.H_q, head = (blockIdx.x - n_close) % a.H_q, g = head / a.gqa;
-  const int per = items_of(a.lens[b], a.max_context);
+  const int per = items_of(a.lens[b + touch_kernargs<sizeof(BlockArgs) + sizeof(BlockStep)>()], a.max_context);
   if (per == 0) return;   // no sequence, or written by the attention pass
-  int before;
-  const int total = count_items(a, lane_len(a, 0), b, &before) * a.H_kv;
-  const int size = part_items(total);
+  const int incl0 = wave_scan(items_of(lane_len(a, 0), a.max_context));
+  int all = __builtin_amdgcn_readlane(incl0, 63), before;
+  if (b < 64) before = __builtin_amdgcn_readlane(incl0, b) - per;
+  if (a.B > 64) {
+    int more;
+    const int past = items_past_64(a, b, &more);
+    if (b >= 64) before = all + more;
+    all += past;
+  }
+  const int total = all * a.H_kv, size = part_items(total);
   const int first = before * a.H_kv + g * per;
   const int p0 = first / size, p1 = (first + per - kSegCost - 1) / size;
   const int pair = b * a.H_kv + g, h = head % a.gqa;
