@@ -114,23 +114,22 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     koff[i] = (uint32_t)r * (uint32_t)(2 * a.k_st) + 16 * ((lane & 15) ^ swz_k(r));
     voff[i] = (uint32_t)r * (uint32_t)(2 * a.v_st) + 16 * ((lane & 15) ^ swz_v(r));
   }
-  auto fetch = [&](int t, const uint16_t* base, int64_t stride, const uint32_t (&off)[kLoads], uint8_t* tile) __attribute__((always_inline)) {
-    if (t >= n_tiles) return;
-    const uint8_t* src = (const uint8_t*)(base + (int64_t)t * kKeys * stride);
-    uint8_t* const dst = tile + fr0 * kRowBytes;
-    const int past = t * kKeys + kKeys - len;   // keys past the prompt repeat its last (they are masked)
-    if (past <= 0) {
+  // Keys past the prompt repeat its last (they are masked): the offsets of the last tile,
+  // which is the last to be loaded.
+  auto clamp = [&](int t, int64_t stride, uint32_t (&off)[kLoads]) __attribute__((always_inline)) {
+    const int past = t * kKeys + kKeys - len;
+    if (past <= 0) return;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) dma16(src + off[i], dst + 4 * i * kRowBytes);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const uint32_t back = max(fr + 4 * i - (kKeys - 1 - past), 0);
-        dma16(src + (off[i] - back * (uint32_t)(2 * stride)), dst + 4 * i * kRowBytes);
-      }
-    }
+    for (int i = 0; i < kLoads; ++i)
+      off[i] -= (uint32_t)max(fr + 4 * i - (kKeys - 1 - past), 0) * (uint32_t)(2 * stride);
   };
-  fetch(0, kp, a.k_st, koff, sk0);
+  auto fetch = [&](int t, const uint16_t* base, int64_t stride, const uint32_t (&off)[kLoads], uint8_t* tile,
+                   int i) __attribute__((always_inline)) {
+    if (t < n_tiles) dma16((const uint8_t*)(base + (int64_t)t * kKeys * stride) + off[i], tile + (fr0 + 4 * i) * kRowBytes);
+  };
+  clamp(0, a.k_st, koff);
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) fetch(0, kp, a.k_st, koff, sk0, i);
 
   // this lane's row (rows past the prompt's last repeat it and are not stored)
   const int row = row0 + rw * 32 + lr;
@@ -171,8 +170,8 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   u32x4 p[2 * KT];
 
   // o += V^T P^T of tile t.  Operands are read ahead of their products: a read takes longer
-  // than the products of one step.
-  auto values = [&](int t, const uint8_t* sv) __attribute__((always_inline)) {
+  // than the products of one step.  `beside` goes with each step's.
+  auto values = [&](int t, const uint8_t* sv, auto beside) __attribute__((always_inline)) {
     u32x4 vv[2][4];
     auto read_v = [&](int ks) {
 #pragma unroll
@@ -188,6 +187,7 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
 #pragma unroll
     for (int ks = 0; ks < 2 * KT; ++ks) {
       if (ks + 1 < 2 * KT) read_v(ks + 1);
+      beside(ks);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[c] = mfma32(vv[ks & 1][c], p[ks], o[c]);
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     }
   };
   // s = K Q^T of tile t
-  auto logits = [&](const uint8_t* sk) __attribute__((always_inline)) {
+  auto logits = [&](const uint8_t* sk, auto beside) __attribute__((always_inline)) {
     u32x4 kk[kAhead][KT];
     auto read_k = [&](int ks) {
 #pragma unroll
@@ -228,6 +228,7 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     for (int ks = 0; ks < kAhead; ++ks) read_k(ks);
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
+      beside(ks);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) s[kt] = mfma32(kk[ks % kAhead][kt], q[ks], s[kt]);
@@ -306,12 +307,45 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   };
   // Tile t: the products of the values of the tile before and of its own keys, then its
   // weights.  Meanwhile the next tile's keys and its own values arrive; the arrays they
-  // fill were last read in the products of the tile before.
+  // fill were last read in the products of the tile before.  Eight loads in a row hold a
+  // wave for 500 to 800 cycles (a unit takes 64 bytes a cycle from all its waves).  Two
+  // workgroups a unit fill that with each other's work; a lone one issues them one at a time
+  // beside its products (one prompt of 2067 tokens and 8 heads 30 -> 28 us, but 8192 with
+  // four waves 193 -> 211).
   auto step = [&](int t, uint8_t* sk, uint8_t* sv_before, uint8_t* sk_next, uint8_t* sv) __attribute__((always_inline)) {
-    fetch(t + 1, kp, a.k_st, koff, sk_next);
-    fetch(t, vp, a.v_st, voff, sv);
-    if (t > 0 && t - 1 < n_mine) values(t - 1, sv_before);
-    if (t < n_mine) logits(sk);
+    if (t + 1 < n_tiles) clamp(t + 1, a.k_st, koff);
+    clamp(t, a.v_st, voff);
+    constexpr bool kSpread = KG > 1;
+    auto next_keys = [&](int ks) __attribute__((always_inline)) {
+      if constexpr (kSpread) {
+#pragma unroll
+        for (int i = ks * kLoads / (2 * KT); i < (ks + 1) * kLoads / (2 * KT); ++i)
+          fetch(t + 1, kp, a.k_st, koff, sk_next, i);
+      }
+    };
+    auto own_values = [&](int ks) __attribute__((always_inline)) {
+      if constexpr (kSpread) {
+        if (ks < kLoads) fetch(t, vp, a.v_st, voff, sv, ks);
+      }
+    };
+    if constexpr (!kSpread) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) fetch(t + 1, kp, a.k_st, koff, sk_next, i);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) fetch(t, vp, a.v_st, voff, sv, i);
+    }
+    if (t > 0 && t - 1 < n_mine) {
+      values(t - 1, sv_before, next_keys);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < 2 * KT; ++ks) next_keys(ks);
+    }
+    if (t < n_mine) {
+      logits(sk, own_values);
+    } else {
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) own_values(ks);
+    }
     // (products first: a wave that waits for them delays its own weights and the barrier;
     // 1.5% at 32K)
     if constexpr (KG == 1) __builtin_amdgcn_s_setprio(0);
@@ -329,8 +363,8 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
     if (t + 1 < n_tiles) step(t + 1, sk1, sv0, sk0, sv1);
   }
   if (n_tiles - 1 < n_mine) {
-    if (n_tiles & 1) values(n_tiles - 1, sv0);
-    else values(n_tiles - 1, sv1);
+    if (n_tiles & 1) values(n_tiles - 1, sv0, [](int) {});
+    else values(n_tiles - 1, sv1, [](int) {});
   }
 
   l = half_sum(l);
