@@ -346,11 +346,7 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks) own_values(ks);
     }
-    // (products first: a wave that waits for them delays its own weights and the barrier;
-    // 1.5% at 32K)
-    if constexpr (KG == 1) __builtin_amdgcn_s_setprio(0);
     if (t < n_mine) weights(t);
-    if constexpr (KG == 1) __builtin_amdgcn_s_setprio(1);
     if (edge(t)) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       clean(t, sv);
