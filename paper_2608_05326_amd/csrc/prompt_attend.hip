@@ -364,60 +364,64 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   }
 
   l = half_sum(l);
-  if constexpr (KG > 1) {
-    // the first wave of a row set takes in the others' maxima, sums and outputs (16 KB a
-    // wave, in the tiles' arrays)
+  // channels 32 c .. + 31 of the row, from the 16 of each lane half
+  auto store = [&](int c, const f32x16& x, float inv) __attribute__((always_inline)) {
+    uint16_t* op = a.out + (start + pos) * a.o_st + head * a.o_sh + 32 * c + 8 * lh;
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {   // channels 8 e .. 8 e + 15: eight to each lane half
+      uint32_t y[2], z[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(
+            pack_bf16(x[4 * e + 2 * j] * inv, x[4 * e + 2 * j + 1] * inv),
+            pack_bf16(x[4 * e + 4 + 2 * j] * inv, x[4 * e + 5 + 2 * j] * inv), false, false);
+        y[j] = sw[0];
+        z[j] = sw[1];
+      }
+      if (row < n_rows) *(u32x4*)(op + 8 * e) = (u32x4){y[0], y[1], z[0], z[1]};
+    }
+  };
+  if constexpr (KG == 1) {
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) store(c, o[c], inv);
+  } else {
+    // the waves of a row set put their maxima, sums and outputs (16 KB a wave) in the
+    // tiles' arrays, and each joins 32 of the channels
+    static_assert(KG == 4, "a wave for each 32 channels");
     __shared__ float2 sml[kWaves][64];
     constexpr int kPer = kKeys * kRowBytes / 16384;   // waves per array
-    static_assert((KG - 1) * RS <= 4 * kPer, "room for the waves' outputs");
+    static_assert(kWaves == 4 * kPer, "room for the waves' outputs");
     auto rows_of = [&](int w) {
-      w -= RS;
       uint8_t* const arr = w / kPer == 0 ? sk0 : w / kPer == 1 ? sv0 : w / kPer == 2 ? sk1 : sv1;
       return (float*)(arr + w % kPer * 16384) + lane;
     };
     __syncthreads();   // the tiles are consumed
-    if (kg) {
-      sml[wave][lane] = make_float2(m, l);
-      float* so = rows_of(wave);
+    sml[wave][lane] = make_float2(m, l);
+    float* mine = rows_of(wave);
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+    for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) so[64 * (16 * c + i)] = o[c][i];
-    }
+      for (int i = 0; i < 16; ++i) mine[64 * (16 * c + i)] = o[c][i];
     __syncthreads();
-    if (kg) return;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-    for (int j = 1; j < KG; ++j) {
-      const float2 ml = sml[wave + j * RS][lane];
-      const float* so = rows_of(wave + j * RS);
-      const float mn = fmaxf(m, ml.x), mu = mn > -INFINITY ? mn : 0.f;
-      const float f0 = __builtin_amdgcn_exp2f(m - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
-      m = mn;
-      l = fmaf(f1, ml.y, f0 * l);
+    for (int j = 0; j < KG; ++j) M = fmaxf(M, sml[rw + j * RS][lane].x);
+    const float mu = M > -INFINITY ? M : 0.f;
+    f32x16 x;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] = fmaf(f1, so[64 * (16 * c + i)], f0 * o[c][i]);
+    for (int j = 0; j < KG; ++j) {
+      const float2 ml = sml[rw + j * RS][lane];
+      const float f = __builtin_amdgcn_exp2f(ml.x - mu);
+      L = fmaf(f, ml.y, L);
+      const float* from = rows_of(rw + j * RS) + 64 * 16 * kg;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = fmaf(f, from[64 * i], x[i]);
     }
+    store(kg, x, 1.f / L);
   }
-
-  const float inv = 1.f / l;
-  uint16_t* op = a.out + (start + pos) * a.o_st + head * a.o_sh;
-#pragma unroll
-  for (int c = 0; c < 4; ++c)
-#pragma unroll
-    for (int e = 0; e < 4; e += 2) {   // channels 32 c + 8 e .. + 15: eight to each lane half
-      uint32_t x[2], y[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const auto sw = __builtin_amdgcn_permlane32_swap(
-            pack_bf16(o[c][4 * e + 2 * j] * inv, o[c][4 * e + 2 * j + 1] * inv),
-            pack_bf16(o[c][4 * e + 4 + 2 * j] * inv, o[c][4 * e + 5 + 2 * j] * inv), false, false);
-        x[j] = sw[0];
-        y[j] = sw[1];
-      }
-      if (row < n_rows) *(u32x4*)(op + 32 * c + 8 * (e + lh)) = (u32x4){x[0], x[1], y[0], y[1]};
-    }
 }
 
 // Workgroups of a launch (an upper bound: every prompt's last tile may be a partial one).
