@@ -12,10 +12,18 @@
 //                 maximum and sum are in-lane but for one exchange of the two lane halves
 //   O^T = V^T P^T (A = channels, B = rows): the same lane owns the row's output channels
 // The keys of the A operand are permuted so that a lane's logits 8 s .. 8 s + 7 of a tile
-// are the eight consecutive keys the second product wants from it (acc_key): P goes from
-// the first product's result to the second's operand without moving between lanes.
+// are the eight consecutive keys the second product wants from it: P goes from the first
+// product's result to the second's operand without moving between lanes.
 // P enters the second product in bf16 (off by at most 2^-8 of itself, the size of the
 // output's own rounding); logits, maximum, sum and output are held in 32 bits.
+//
+// Per 32 rows and 64 keys a wave issues 32 products (1024 cycles), 32 exponentials and
+// about 120 other vector instructions (some 730 cycles) and reads 32 KB of LDS; two waves
+// share a SIMD so that one's products run beside the other's exponentials.  A 32K prompt of
+// 32/8 heads takes 7.7 ms (1145 TFLOP/s, a large bf16 matrix product reaches 1260 on such a
+// card); with all inputs zero the same instructions run at 1430, so at that size the
+// clock under load bounds it: orders of the loads, priorities and a barrier that keeps
+// the two waves half a tile apart moved it by 4% at most.
 #include <algorithm>
 
 #include "qv_device.h"
@@ -438,22 +446,24 @@ constexpr int kUnits = 256;   // compute units
 // unit, or 64 rows and eight waves, four to a row set, one to a unit.  The second ends its
 // longest row sooner but pays its start and join for half as many rows.  Estimated from the
 // prompts' mean length t, a launch takes the larger of its longest workgroup and its sum
-// over the chip, in microseconds (measured on one prompt of 2067 tokens and 8 heads: 46 and
-// 30; 4096: 87 and 64; 8192: 204 and 217; on 1024 tokens of 32/8 heads: 27 and 28; on 32
-// prompts of 100 tokens: 24 and 58).
+// over the chip, in microseconds (measured: one prompt of 8 heads and 2067 tokens 47 and
+// 28, 4096 89 and 60, 8192 192 and 218; 32/8 heads and 512 tokens 17 and 13, 2048 54 and
+// 72; 32 prompts of 100 tokens 23 and 54).
 static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
   const float t = (float)a.total / a.n_seqs;
-  const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.74f + 5.f) / 512);
-  if (n64 >= 4096) return false;
-  const float eight = std::max(t / 128 * 1.35f + 8.f, n64 * (t / 256 * 1.35f + 8.f) / 256);
-  return eight < four;
+  const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.6f + 5.f) / (2 * kUnits));
+  const float eight = std::max(t / 128 * 1.28f + 7.f, n64 * (t / 256 * 1.28f + 7.f) / kUnits);
+  return n64 < 4096 && eight < four;
 }
 
 hipError_t launch_prompt_attend(PromptArgs a, hipStream_t st) {
   const int64_t n128 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 128);
   const int64_t n64 = groups_of(a.total, a.n_seqs, a.gqa, a.H_kv, 64);
   const bool eight = eight_waves(a, n128, n64);
-  const int64_t slots = (eight ? n64 : n128) / a.H_kv, first = kUnits / a.H_kv;
+  // Workgroups are dealt round the units, the longest first.  Where they fill the chip about
+  // once (two to a unit), the second of each unit comes in reverse, the shortest beside the
+  // longest: 8 heads of 8192 tokens 204 -> 194 us, 64/8 heads of 1024 35 -> 33.
+  const int64_t slots = n128 / a.H_kv, first = kUnits / a.H_kv;
   a.fold = (int)std::min(first, slots);
   a.fold_end = (int)(eight || slots >= 4 * first ? a.fold : std::min(slots, 2 * first));
   if (eight) k_prompt_attend<2, 4><<<dim3((uint32_t)n64), 512, 0, st>>>(a);
