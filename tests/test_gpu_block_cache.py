@@ -289,6 +289,17 @@ def test_places_without_room_or_sequence():
     assert bool((out == 7.0).all())
 
 
+def test_fetch_of_places_without_a_sequence():
+    """Lengths below zero hold nothing, whatever rows cu_tokens gives them."""
+    import torch
+    bc, k, v = _make([200, 70, 130], 4, 2, max_context=300, seed=36)
+    bc.lens = torch.tensor([-1, -(1 << 31), 1 << 30], dtype=torch.int32)
+    ko, vo = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
+    bc.fetch(0, ko, vo, _cu([200, 70, 130]))
+    assert bool((ko[:270] == 7.0).all()) and bool((vo[:270] == 7.0).all())
+    assert bool((ko[270:398] != 7.0).any(-1).all())      # a length past max_context counts as max_context
+
+
 @pytest.mark.parametrize("drop", [-1, 1 << 30, -(1 << 31)])
 def test_blocks_without_a_page(drop):
     """Dropped blocks take no part, are not stored and are fetched as zeros."""
