@@ -23,9 +23,10 @@
  *    H_kv and d taken from the configuration: the kernels read and write
  *    whole extents and cannot check a buffer's size (null pointers and
  *    misalignment are rejected on the host).
- *  - Work is enqueued on the HIP stream given to qevict_cache_init and is
- *    asynchronous unless the comment says "synchronous".  Inputs must stay
- *    valid until the stream has passed the call.
+ *  - Work is enqueued on the HIP stream given to qevict_cache_init (the calls
+ *    without a handle, at the end, take a stream) and is asynchronous unless
+ *    the comment says "synchronous".  Inputs must stay valid until the stream
+ *    has passed the call.
  *  - Host-side validation runs before anything is enqueued; on error nothing
  *    is enqueued and the cache is unchanged.  Errors found on the device
  *    (non-finite score, exhausted slot pool) latch an error word that the next
