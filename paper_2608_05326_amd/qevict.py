@@ -495,7 +495,8 @@ def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stre
     elements with the channels contiguous (slices of a fused projection, transposed
     [H, T, d] tensors).  cu_tokens: int32 [n + 1] on the device.  Returns out, bf16
     [T, H_q, d]; rows behind the last prompt are left as they were (undefined in an out
-    that is allocated here).  Runs on `stream`, by default torch's current one."""
+    that is allocated here).  No gradient is recorded.  Runs on `stream`, by default
+    torch's current one."""
     lib = load_library()
     import torch
     index = q.get_device()

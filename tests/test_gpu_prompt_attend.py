@@ -184,6 +184,21 @@ def test_masked_values_that_are_not_finite(at, bad):
     _check(out, want, A, "query")
 
 
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("at", [0, 31, 32, 127, 128, 200, 299])
+def test_masked_values_of_a_lone_prompt(at, bad):
+    """The same where a few long rows are shared by four waves each (one prompt, few heads)."""
+    import paper_2608_05326_amd as qv
+    q, k, v, cu = _inputs([300], 2, 1, seed=15)
+    v[at, 0, 5] = bad
+    _check(qv.prompt_attend(q, k, v, cu), *_reference(q, k, v, [300]))
+    q, k, v, cu = _inputs([300], 2, 1, seed=16)
+    want, A = _reference(q, k, v, [300])
+    k[at, 0, 9] = bad
+    out = qv.prompt_attend(q, k, v, cu)
+    _check(out[:at], want[:at], A[:at], "rows before the key")
+
+
 def test_large_and_shifted_logits():
     """Logits in the hundreds (one key takes a row), rising and falling along the prompt."""
     import torch
