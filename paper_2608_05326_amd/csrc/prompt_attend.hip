@@ -133,7 +133,8 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   };
   auto fetch = [&](int t, const uint16_t* base, int64_t stride, const uint32_t (&off)[kLoads], uint8_t* tile,
                    int i) __attribute__((always_inline)) {
-    if (t < n_tiles) dma16((const uint8_t*)(base + (int64_t)t * kKeys * stride) + off[i], tile + (fr0 + 4 * i) * kRowBytes);
+    if (t < n_tiles)
+      dma16((const uint8_t*)(base + (int64_t)t * kKeys * stride) + off[i], tile + (fr0 + 4 * i) * kRowBytes);
   };
   clamp(0, a.k_st, koff);
 #pragma unroll
@@ -320,7 +321,8 @@ __global__ __launch_bounds__(64 * RS * KG, 2) void k_prompt_attend(PromptArgs a)
   // workgroups a unit fill that with each other's work; a lone one issues them one at a time
   // beside its products (one prompt of 2067 tokens and 8 heads 30 -> 28 us, but 8192 with
   // four waves 193 -> 211).
-  auto step = [&](int t, uint8_t* sk, uint8_t* sv_before, uint8_t* sk_next, uint8_t* sv) __attribute__((always_inline)) {
+  auto step = [&](int t, uint8_t* sk, uint8_t* sv_before, uint8_t* sk_next,
+                  uint8_t* sv) __attribute__((always_inline)) {
     if (t + 1 < n_tiles) clamp(t + 1, a.k_st, koff);
     clamp(t, a.v_st, voff);
     constexpr bool kSpread = KG > 1;
