@@ -7,6 +7,7 @@ creating a cache does, and there is no CPU fallback: a missing library raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import dataclasses
@@ -545,7 +546,14 @@ class BlockCache:
     storing a prompt and advances it after each step (advance()).
 
     Assigning to one of them copies into it.  Steps of one cache share its workspace and open
-    blocks: they run one after the other.  Calls run on torch's current stream unless the cache was given one."""
+    blocks: they run one after the other.
+
+    Calls run on torch's current stream unless the cache was given one.  With one of its own,
+    everything the cache enqueues is on that stream: its state's first contents, store, attend,
+    fetch and advance(); an assigned value is copied there after the current stream's work so
+    far, and the current stream waits for the copy.  The tensors that a call takes have to be
+    ready on that stream, and a program that reads or changes the state tensors in place does
+    so on it, or orders its streams with it."""
 
     def __init__(self, cfg: BlockConfig, device="cuda", stream=None):
         import torch
@@ -571,21 +579,45 @@ class BlockCache:
         need = ctypes.c_size_t()
         _check(self.lib, self.lib.qevict_block_workspace_size(ctypes.byref(self._c), ctypes.byref(need)))
         z = torch.zeros
-        self._state = dict(
-            k_codes=z((L, pages, h, n, d), dtype=torch.int8, device=dev),
-            v_codes=z((L, pages, h, d, n), dtype=torch.int8, device=dev),
-            k_scale=z((L, pages, h), dtype=torch.float32, device=dev),
-            v_scale=z((L, pages, h), dtype=torch.float32, device=dev),
-            k_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
-            v_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
-            table=torch.full((B, cols), -1, dtype=torch.int32, device=dev),
-            lens=torch.full((B,), -1, dtype=torch.int32, device=dev))
-        if not cfg.num_pages:
-            self.table.copy_(torch.arange(pages, dtype=torch.int32).view(B, cols))
-        self.workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        with self._on_stream():   # (its memory is then reused in that stream's order, too)
+            self._state = dict(
+                k_codes=z((L, pages, h, n, d), dtype=torch.int8, device=dev),
+                v_codes=z((L, pages, h, d, n), dtype=torch.int8, device=dev),
+                k_scale=z((L, pages, h), dtype=torch.float32, device=dev),
+                v_scale=z((L, pages, h), dtype=torch.float32, device=dev),
+                k_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
+                v_tail=z((L, B, h, n, d), dtype=torch.bfloat16, device=dev),
+                table=torch.full((B, cols), -1, dtype=torch.int32, device=dev),
+                lens=torch.full((B,), -1, dtype=torch.int32, device=dev))
+            if not cfg.num_pages:
+                self._state["table"].copy_(torch.arange(pages, dtype=torch.int32).view(B, cols))
+            self.workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+        current = self._other_stream()
+        if current is not None:
+            current.wait_stream(stream)
         self._layers = [_BlockLayer(*[
             (t if name in ("table", "lens") else t[i]).data_ptr() for name, t in self._state.items()])
             for i in range(L)]
+
+    def _on_stream(self):
+        """Context of the cache's own tensor work: its stream, where it was given one."""
+        return contextlib.nullcontext() if self.stream is None else self.torch.cuda.stream(self.stream)
+
+    def _other_stream(self):
+        """torch's current stream where that is not the one the cache was given, else None."""
+        if self.stream is None:
+            return None
+        current = self.torch.cuda.current_stream(self.device)
+        return None if current == self.stream else current
+
+    def _assign(self, name, value):
+        current = self._other_stream()
+        if current is not None:
+            self.stream.wait_stream(current)
+        with self._on_stream():
+            self._state[name].copy_(value)
+        if current is not None:
+            current.wait_stream(self.stream)
 
     def _call(self, fn, layer: int, *args):
         if not 0 <= layer < self.cfg.num_layers:
@@ -626,7 +658,8 @@ class BlockCache:
 
     def advance(self):
         """After a step's last layer: lens + 1 where a place holds a sequence that has room."""
-        self.lens += ((self.lens >= 0) & (self.lens < self.cfg.max_context)).to(self.lens.dtype)
+        with self._on_stream():
+            self.lens += ((self.lens >= 0) & (self.lens < self.cfg.max_context)).to(self.lens.dtype)
 
 
 def _state_tensor(name):
@@ -635,7 +668,7 @@ def _state_tensor(name):
 
     def put(self, value):   # assignment writes into the tensor the kernels read
         if value is not self._state[name]:
-            self._state[name].copy_(value)
+            self._assign(name, value)
     return property(get, put)
 
 

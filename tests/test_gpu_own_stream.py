@@ -1,0 +1,64 @@
+"""The handle-free calls on a stream of their own that still has work before it, while torch's
+current stream is idle: results equal those of one stream, bit for bit."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+def _rnd(seed, *shape):
+    import torch
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed)).bfloat16().cuda()
+
+
+def _backlog(stream):
+    """Some 40 ms of matrix products on the stream."""
+    import torch
+    with torch.cuda.stream(stream):
+        a = torch.full((4096, 4096), 2.0 ** -12, device="cuda")
+        b = torch.empty_like(a)
+        for _ in range(30):
+            torch.mm(a, a, out=b)
+
+
+@pytest.mark.parametrize("num_pages", [0, 60])
+def test_steps_of_a_cache_with_its_own_stream(num_pages):
+    """Stored prompts, assigned lengths and pages, and 70 steps across block ends, enqueued
+    without a host synchronization behind a backlog."""
+    import torch
+    import paper_2608_05326_amd as qv
+    lens, steps, hq, hkv = [60, 0, 127, -1, 500], 70, 8, 2
+    pos = [max(t, 0) for t in lens]
+    k, v = _rnd(1, sum(pos), hkv, D), _rnd(2, sum(pos), hkv, D)
+    q, kn, vn = (_rnd(3 + i, steps, 5, h, D) for i, h in enumerate((hq, hkv, hkv)))
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(pos)]), dtype=torch.int32).cuda()
+    table = torch.arange(50, dtype=torch.int32).flip(0).view(5, 10).cuda()
+    held = torch.tensor(lens, dtype=torch.int32).cuda()
+
+    def drive(stream):
+        out = torch.full((steps, 5, hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        if stream is not None:
+            _backlog(stream)
+        c = qv.BlockCache(qv.BlockConfig(5, hq, hkv, 640, num_pages=num_pages), stream=stream)
+        if num_pages:
+            c.table = table
+        c.store(0, k, v, cu)
+        mine = held.clone()
+        c.lens = mine
+        mine.fill_(-1)            # the cache has its own copy
+        if stream is not None:
+            _backlog(stream)      # the steps are pending while advance() is called
+        for t in range(steps):
+            c.attend(0, q[t], kn[t], vn[t], out[t])
+            c.advance()
+        torch.cuda.synchronize()
+        return c, out
+
+    a, want = drive(None)
+    assert a.lens.tolist() == [t + steps if t >= 0 else t for t in lens]
+    b, got = drive(torch.cuda.Stream())
+    assert torch.equal(a.lens, b.lens) and torch.equal(want, got)
+    for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail"):
+        assert torch.equal(getattr(a, n), getattr(b, n)), n
