@@ -497,7 +497,9 @@ def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stre
     [H, T, d] tensors).  cu_tokens: int32 [n + 1] on the device.  Returns out, bf16
     [T, H_q, d]; rows behind the last prompt are left as they were (undefined in an out
     that is allocated here).  No gradient is recorded.  Runs on `stream`, by default
-    torch's current one."""
+    torch's current one, as a torch operation under torch.cuda.stream(stream) does: what it
+    takes has to be ready there and stay allocated until it is done, and an out that is
+    allocated here belongs to that stream."""
     lib = load_library()
     import torch
     index = q.get_device()
@@ -507,7 +509,9 @@ def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stre
     hkv = k.shape[1]
     vp, v_st, v_sh = _rows(v, torch, index, "v", hkv, T, d)
     if out is None:
-        out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=q.device)
+        # from the pool of the stream that writes it: elsewhere pending work may still use it
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=q.device)
     op, o_st, o_sh = _rows(out, torch, index, "out", hq, T, d)
     n = cu_tokens.numel() - 1
     cu = _int32(cu_tokens, torch, index, "cu_tokens", n + 1)

@@ -62,3 +62,26 @@ def test_steps_of_a_cache_with_its_own_stream(num_pages):
     assert torch.equal(a.lens, b.lens) and torch.equal(want, got)
     for n in ("k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail"):
         assert torch.equal(getattr(a, n), getattr(b, n)), n
+
+
+def test_prompt_result_allocated_for_a_stream():
+    """Results allocated by the call, behind a backlog, while the current stream keeps using
+    and dropping tensors of the same size."""
+    import torch
+    import paper_2608_05326_amd as qv
+    q, k, v = _rnd(11, 700, 8, D), _rnd(12, 700, 2, D), _rnd(13, 700, 2, D)
+    cu = torch.tensor([0, 300, 700], dtype=torch.int32).cuda()
+    want = qv.prompt_attend(q, k, v, cu)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    _backlog(st)
+    got = []
+    for _ in range(8):
+        x = torch.full_like(q, 3.0)
+        x.mul_(2.0)
+        del x
+        got.append(qv.prompt_attend(q, k, v, cu, stream=st))
+        qv.prompt_attend(q, k, v, cu, stream=st)     # dropped while pending
+        torch.full_like(q, 5.0)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for x in got)
