@@ -473,9 +473,16 @@ def _int32(t, torch, index, name, n):
     return t.data_ptr()
 
 
+def _check_stream(stream, index):
+    """A kernel on another device's stream would run there, on addresses of this one."""
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"the stream belongs to device {stream.device}, the tensors to cuda:{index}")
+
+
 def _launch(lib, torch, index, stream, fn, *args):
     """A handle-free call with the device of its tensors current (kernels run on the
     current device), on `stream` or torch's current one there."""
+    _check_stream(stream, index)
     before = torch.cuda.current_device()
     if before != index:
         torch.cuda.set_device(index)
@@ -573,6 +580,7 @@ class BlockCache:
             raise ValueError("batch, max_context, num_layers and num_kv_heads must be positive")
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
+        _check_stream(stream, dev.index)
         self.device = dev
         self.stream = stream
         L, B, h, d, n = cfg.num_layers, cfg.batch, cfg.num_kv_heads, cfg.head_dim, BLOCK_TOKENS
