@@ -30,6 +30,7 @@ FLAG_ROUTING_QUEUE_WAIT, FLAG_ROUTING_DEVICE_WAIT = 0x8, 0x10
 KERNEL_ATTEND, KERNEL_MERGE, KERNEL_RETIER, KERNEL_MIGRATE = range(4)
 SCORE_CUMULATIVE, SCORE_DECAY, SCORE_KEY_NORM, SCORE_PNORM = 0, 1, 2, 3
 BLOCK_TOKENS = 64
+INT32_MAX = 2 ** 31 - 1
 
 # exported symbols declared in include/qevict.h
 SYMBOLS = (
@@ -458,6 +459,8 @@ def _rows(t, torch, index, name, heads=None, tokens=None, dim=None):
         raise ValueError(f"{name} must be [{'T' if tokens is None else tokens}, "
                          f"{'H' if heads is None else heads}, {'d' if dim is None else dim}], "
                          f"got shape {tuple(sh)}")
+    if sh[0] > INT32_MAX or sh[1] > INT32_MAX:   # (rows that repeat one can be as many)
+        raise ValueError(f"{name}: rows and heads must be below 2^31, got shape {tuple(sh)}")
     st = t.stride()
     if st[2] != 1 and sh[2] > 1:
         raise ValueError(f"{name}: the channels of a row must be contiguous")
@@ -470,6 +473,8 @@ def _int32(t, torch, index, name, n):
             not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor of {n} entries on device cuda:{index}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if n > INT32_MAX:
+        raise ValueError(f"{name} must have fewer than 2^31 entries, got {n}")
     return t.data_ptr()
 
 
@@ -578,6 +583,9 @@ class BlockCache:
         if cfg.batch < 1 or cfg.max_context < 1 or cfg.num_layers < 1 or cfg.num_kv_heads < 1 or \
                 cfg.num_pages < 0:
             raise ValueError("batch, max_context, num_layers and num_kv_heads must be positive")
+        if max(cfg.batch, cfg.max_context, cfg.num_pages, cfg.num_q_heads, cfg.num_kv_heads,
+               cfg.head_dim) > INT32_MAX:   # the C ABI's fields, which ctypes would cut to their low bits
+            raise ValueError("sizes must be below 2^31")
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         _check_stream(stream, dev.index)
