@@ -428,7 +428,7 @@ typedef struct {
   int32_t num_q_heads;
   int32_t num_kv_heads;
   int32_t head_dim;          /* 128 */
-  float softmax_scale;       /* 0 selects 1/sqrt(head_dim) */
+  float softmax_scale;       /* 0 selects 1/sqrt(head_dim), else 2^-64 .. 2^64 */
   int64_t q_token_stride, q_head_stride;
   int64_t k_token_stride, k_head_stride;
   int64_t v_token_stride, v_head_stride;
@@ -469,7 +469,7 @@ typedef struct {
   int32_t head_dim;          /* 128                                                         */
   int32_t max_context;       /* largest sequence length                                     */
   int32_t num_pages;
-  float softmax_scale;       /* 0 selects 1/sqrt(head_dim)                                  */
+  float softmax_scale;       /* 0 selects 1/sqrt(head_dim), else 2^-64 .. 2^64              */
 } qevict_block_config;
 
 /* Stores packed prompts k, v [total, H_kv, d] bf16: sequence s (its rows by

@@ -1368,7 +1368,9 @@ static qevict_status check_heads(int32_t abi, int32_t hq, int32_t hkv, int32_t d
   if (hq < 1 || hkv < 1) return fail(QEVICT_ERR_INVALID_ARG, "head counts must be positive");
   if (hq % hkv) return fail(QEVICT_ERR_INVALID_ARG, "num_q_heads %% num_kv_heads != 0");
   if (d != kHeadDim) return fail(QEVICT_ERR_UNSUPPORTED, "head_dim must be 128");
-  if (!(scale >= 0.f) || std::isinf(scale)) return fail(QEVICT_ERR_INVALID_ARG, "softmax_scale");
+  // (scale log2 e stays a normal float, and logits of ordinary size are products q k in range)
+  if (scale != 0.f && !(scale >= 0x1p-64f && scale <= 0x1p64f))
+    return fail(QEVICT_ERR_INVALID_ARG, "softmax_scale must be 0 or in 2^-64 .. 2^64");
   return QEVICT_OK;
 }
 
