@@ -489,7 +489,11 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
           qf[i][2 * j] = (_Float16)ldexpf(lo_f32(qw[i][j]), 14 - ex);
           qf[i][2 * j + 1] = (_Float16)ldexpf(hi_f32(qw[i][j]), 14 - ex);
         }
-      const float qs = ldexpf(a.scale_log2, ex - 14);   // log2 units per (q' c s)
+      // log2 units per (q' c s): scale_log2 2^(ex - 14) = qm 2^qe.  For small queries that is
+      // below 2^-126, where it would lose bits, though logits need not be small (large keys):
+      // the power of two is applied last, to qm times a block's scale (2^-100 or more).
+      const float qm = __builtin_amdgcn_frexp_mantf(a.scale_log2);
+      const int qe = __builtin_amdgcn_frexp_expf(a.scale_log2) + ex - 14;
 
       for (int blk0 = i0 + wave;;) {
         while (live) {
@@ -498,7 +502,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
           const int8_t* vc = a.v_codes + entry(j) + r * kBlk + 16 * qd;
 #pragma unroll
           for (int ct = 0; ct < 8; ++ct) vb[ct] = get<PAST>(vc + 16 * ct * kBlk);
-          const float sc = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)) * qs;
+          float sc = ldexpf(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)) * qm, qe);
+          if (sc == INFINITY) sc = __FLT_MAX__;   // (a product of zero is a logit of zero)
           const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
           f32x4 acc[4];
 #pragma unroll
