@@ -16,6 +16,7 @@
 // (a channel's tokens together): each is the order in which the matrix instruction of its
 // product reads it, 16 bytes a lane.
 #include "qv_device.h"
+#include "qv_parts.h"
 
 namespace qv {
 
@@ -266,14 +267,6 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // (67 MB) 22 us, of which 3 go by before the first page is asked for and 5 in the join.
 namespace {
 constexpr float kLazyD = 8.f;
-// Two workgroups fit a compute unit (214 registers; at 168, for three, the loop spills):
-// 480 parts leave room for the pairs' own workgroups of a small batch beside them.  8 KV
-// heads: one sequence of 32K 22.2 us a step with 480 parts, 23.1 with 512, 28 with 768.
-constexpr int kParts = 480;
-// A pair of at most kSmall complete blocks (two rounds of four waves) is one workgroup's,
-// and a segment counts as kSegCost blocks beside its own: without either, a part of many
-// short sequences outlasts the others (32 ragged places, 985 MB: 329 -> 191 us).
-constexpr int kSmall = 8, kSegCost = 4;
 
 __device__ __forceinline__ f32x4 mfma_f16(f16x8 x, f16x8 y, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
@@ -318,17 +311,6 @@ __device__ __forceinline__ void raise(Running& st, float mt) {
   }
 }
 
-// Complete blocks of a place that holds a sequence with room for a token, else -1.
-__device__ __forceinline__ int blocks_of(int len, int max_context) {
-  return len < 0 || len >= max_context ? -1 : len / kBlk;
-}
-// Items of one of its pairs in the parts: the blocks of a pair that is not small, and what
-// the segment costs (items that hold nothing).
-__device__ __forceinline__ int items_of(int len, int max_context) {
-  const int n = blocks_of(len, max_context);
-  return n > kSmall ? n + kSegCost : 0;
-}
-
 // inclusive sum over the wave's lanes: within rows of 16, then across them
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // from 1, 2, 4, 8 lanes below
@@ -365,9 +347,6 @@ __device__ __forceinline__ int items_past_64(const BlockArgs& a, int place, int*
   *before = __builtin_amdgcn_readlane(wave_scan(pre), 63);
   return __builtin_amdgcn_readlane(wave_scan(sum), 63);
 }
-
-// Items of a part: equal parts but for the last.
-__device__ __forceinline__ int part_items(int total) { return (int)(((uint32_t)total + kParts - 1) / kParts); }
 
 constexpr int kTailRow = 2 * kHeadDim;
 constexpr int kJoinRow = kHeadDim + 4;
@@ -596,7 +575,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
   // ---- this workgroup's pair, or its part of the items
   const bool own_pair = (int)blockIdx.x < n_pairs;
   const int part = blockIdx.x - n_pairs;
-  int begin = 0, end = INT32_MAX, s_begin = 0, s_end = a.B;
+  int s_begin = 0, s_end = a.B;
+  Span items = {0, 1};   // of the part (a pair's own workgroup has none: the loop's one round)
   if (own_pair) {
     s_begin = (int)(blockIdx.x / a.H_kv) & ~63;
     s_end = s_begin + 1;
@@ -609,17 +589,16 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
     if (a.B > 64) total += items_past_64(a, 0, &before) * a.H_kv;
     const int size = part_items(total);
     if ((int64_t)part * size >= total) return;
-    begin = part * size;
-    end = min(begin + size, total);
+    items = {part * size, min(part * size + size, total)};
   }
   int base = 0;   // items before the 64 places of this round
-  for (int s0 = s_begin; s0 < s_end && base < end; s0 += 64) {
+  for (int s0 = s_begin; s0 < s_end && base < items.end; s0 += 64) {
     const int len = s0 == s_begin ? len0 : lane_len(a, s0);
     const int n = items_of(len, a.max_context) * a.H_kv;
     const int incl = s0 == s_begin ? incl0 : base + wave_scan(n);
     // places of the round that the workgroup serves
     uint64_t mine = own_pair ? (uint64_t)1 << ((blockIdx.x / a.H_kv) & 63)
-                             : __ballot(n > 0 && incl > begin && incl - n < end);
+                             : __ballot(n > 0 && incl > items.begin && incl - n < items.end);
     base = __builtin_amdgcn_readlane(incl, 63);
     for (; mine; mine &= mine - 1) {
       const int w = __builtin_ctzll(mine), b = s0 + w;
@@ -627,21 +606,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_block_attend(BlockArgs a, Block
       const int n_blk = blocks_of(pos, a.max_context), per = n_blk + kSegCost;
       if (n_blk < 0) return;
       const int first = __builtin_amdgcn_readlane(incl, w) - per * a.H_kv;
-      const int lo = max(begin - first, 0), hi = min(end - first, per * a.H_kv);
       const bool small = n_blk <= kSmall;
-      int g = own_pair ? (int)(blockIdx.x % a.H_kv) : lo / per;
-      const int g_end = own_pair ? g + 1 : (hi + per - 1) / per;
-      for (; g < g_end; ++g) {
-        int i0 = max(lo - g * per, 0), i1 = min(hi - g * per, n_blk);
-        if (own_pair) {
-          i0 = 0;
-          i1 = small ? n_blk : 0;
-        } else if (i0 >= i1) {
-          continue;
+      Span pairs = {(int)(blockIdx.x % a.H_kv), (int)(blockIdx.x % a.H_kv) + 1};
+      if (!own_pair) pairs = pairs_of(items, first, per, a.H_kv);
+      for (int g = pairs.begin; g < pairs.end; ++g) {
+        Span blks = {0, small ? n_blk : 0};
+        if (!own_pair) {
+          blks = blocks_in(items, first, per, g);
+          if (blks.begin >= blks.end) continue;
         }
         // (part and pair grow together: no two segments share a slot)
         const int64_t slot = own_pair ? (int64_t)blockIdx.x : (int64_t)n_pairs + part + b * a.H_kv + g;
-        segment(b, g, i0, i1, own_pair ? pos % kBlk + 1 : 0, own_pair && small, slot);
+        segment(b, g, blks.begin, blks.end, own_pair ? pos % kBlk + 1 : 0, own_pair && small, slot);
       }
     }
   }
@@ -684,11 +660,11 @@ __global__ __launch_bounds__(kThreads) void k_block_merge(BlockArgs a, BlockStep
   }
   const int total = all * a.H_kv, size = part_items(total);
   const int first = before * a.H_kv + g * per;
-  const int p0 = first / size, p1 = (first + per - kSegCost - 1) / size;
+  const Span parts = parts_of(first, per, size);
   const int pair = b * a.H_kv + g, h = head % a.gqa;
   // row 0 is the open block's, the others the parts'
-  const int64_t row0 = (int64_t)pair * a.gqa + h, row1 = ((int64_t)a.B * a.H_kv + p0 + pair - 1) * a.gqa + h;
-  const int n = p1 - p0 + 2, grp = tid >> 5, c = tid & 31;
+  const int64_t row0 = (int64_t)pair * a.gqa + h, row1 = ((int64_t)a.B * a.H_kv + parts.begin + pair - 1) * a.gqa + h;
+  const int n = parts.end - parts.begin + 1, grp = tid >> 5, c = tid & 31;
   float M = -INFINITY, L = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   for (int i0 = grp; i0 < n; i0 += 64) {
