@@ -419,6 +419,10 @@ qevict_status qevict_join_routing(qevict_cache *c);
  * h / (H_q / H_kv).
  *   q [total, H_q, d], k, v [total, H_kv, d] bf16 packed, out like q
  * A value that is not finite reaches the rows that attend to it and no other.
+ * Accuracy: q k^T and all sums are fp32 (they are divided by the sum of the
+ * weights at the end, so 2^8 sum |v| of a prompt has to stay in range), a weight
+ * is rounded to bf16 once and so is the output: with A = sum_j p_j |v_j|,
+ *   |error| <= 2^-8 (A + |out|), and that of the fp32 logits.
  * H_q % H_kv == 0; d == 128; total_tokens * H_q <= 2^30; token strides of k and
  * v below 2^23. */
 typedef struct {
@@ -498,6 +502,9 @@ qevict_status qevict_block_fetch(const qevict_block_config *cfg, const qevict_bl
  * quantizes the block if the token filled it.  lens is read, not advanced: the
  * caller adds 1 to it after the last layer of the step.  A place whose length
  * is negative, or max_context and more, is skipped (its row of out stays).
+ * Accuracy: as qevict_prompt_attend's, but a weight beside a complete block is
+ * rounded to fp16: by 2^-11 of itself, below 2^-14 of the largest by 2^-25 of
+ * the largest.  A head's query keeps entries down to 2^-31 of its largest.
  *   q [B, H_q, d], k_new, v_new [B, H_kv, d] bf16, contiguous, 16-byte aligned
  *   out [B, H_q, d] bf16
  *   workspace  device memory of qevict_block_workspace_size bytes, 256-byte

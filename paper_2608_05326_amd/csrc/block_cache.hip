@@ -256,11 +256,12 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // Row r of key tile tt is token 16 (r / 4) + 4 tt + r % 4 of the block, so that lane group
 // qd holds the logits of tokens 16 qd .. + 15: the 16 codes that one 16-byte load of a
 // value channel gives it.  Codes become fp16 integers (exact): byte + 128 placed below
-// 0x64 is 1152 + c, minus 1152.  A head's query is scaled by a power of two into fp16
-// (exact: bf16 has 8 bits; entries 2^-38 below the head's largest round).  P is rounded to
-// fp16 (2^-11) beside codes and to bf16 beside the open block's values; logits, maximum,
-// sum and output are held in 32 bits, a block's value scale is applied to its products'
-// fp32 sum.
+// 0x64 is 1152 + c, minus 1152.  A head's query is scaled by a power of two into fp16, its
+// largest entry to [2^14, 2^15): exact (bf16 has 8 bits) down to entries 2^-31 of that;
+// smaller ones are off by at most 2^-39 of it.  P is rounded beside codes to fp16: by 2^-11
+// of itself, below 2^-14 of the head's reference by 2^-25 of that; beside the open block's
+// values to bf16 (2^-8 of itself).  The sum takes P unrounded; logits, maximum, sum and
+// output are held in 32 bits, a block's value scale is applied to its products' fp32 sum.
 //
 // Bound by the pages' bytes: eight 8B sequences (401 MB) take 77 us, 32 ragged 70B places
 // (985 MB) 174 us, 5.1 and 5.7 TB/s where a large copy reaches 5.1; one sequence of 32K
@@ -744,10 +745,12 @@ hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace,
   s.part_ml = (float2*)(s.part_o + part_rows(a.B, a.H_kv, a.gqa) * kHeadDim);
   const size_t lds = (size_t)4 * a.gqa * kJoinRow * sizeof(float);
   const dim3 grid(a.B * a.H_kv + kParts);
-  // A layer with more than half the 256 MB Infinity Cache of pages is read past the caches
-  // (its pages would be gone before the next step): eight 8B sequences, 401 MB, 85 -> 78 us,
-  // 32 ragged places, 985 MB, 188 -> 174.  A smaller one may be found there: one 32K
-  // sequence whose 67 MB stay, 22.3 us against 23.9.
+  // Pages are read past the caches where the layer's pool (the host does not know the
+  // lengths) is more than half the 256 MB Infinity Cache: eight 8B sequences, 401 MB, 85 ->
+  // 78 us, 32 ragged places, 985 MB, 188 -> 174.  Below, the two are within 1 us: one 32K
+  // sequence, 67 MB, in turn over 8 layers 24.0 us through the caches and 23.2 past them, the
+  // same layer again and again 21.7 and 21.8; a 2K sequence, 4 MB, over 32 layers 11.2 and
+  // (in a large pool) 12.1.
   const bool past = (int64_t)a.n_pages * a.H_kv * (2 * kCodes) > (128 << 20);
   if (past) k_block_attend<true><<<grid, kThreads, lds, st>>>(a, s);
   else k_block_attend<false><<<grid, kThreads, lds, st>>>(a, s);

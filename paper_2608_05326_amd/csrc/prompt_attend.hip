@@ -15,7 +15,9 @@
 // are the eight consecutive keys the second product wants from it: P goes from the first
 // product's result to the second's operand without moving between lanes.
 // P enters the second product in bf16 (off by at most 2^-8 of itself, the size of the
-// output's own rounding); logits, maximum, sum and output are held in 32 bits.
+// output's own rounding; against 64 bits the output is off by 0.0021 of its norm, 0.0016
+// where only the output is rounded), the sum takes it unrounded; logits, maximum, sum and
+// output are held in 32 bits.
 //
 // Per 32 rows and 64 keys a wave issues 32 products (1024 cycles), 32 exponentials and
 // about 120 other vector instructions (some 730 cycles) and reads 32 KB of LDS; two waves
@@ -450,7 +452,10 @@ constexpr int kUnits = 256;   // compute units
 // prompts' mean length t, a launch takes the larger of its longest workgroup and its sum
 // over the chip, in microseconds (measured: one prompt of 8 heads and 2067 tokens 47 and
 // 28, 4096 89 and 60, 8192 192 and 218; 32/8 heads and 512 tokens 17 and 13, 2048 54 and
-// 72; 32 prompts of 100 tokens 23 and 54).
+// 72; 32 prompts of 100 tokens 23 and 54).  The host sees the rows and the number of prompts
+// only: one long prompt among short or empty ones, or beside rows outside all prompts, is
+// taken for short ones (2067 tokens, 8 heads, beside 31 empty prompts 45 us instead of 27;
+// 4000 beside fifteen of 16 tokens 82 instead of 56).
 static bool eight_waves(const PromptArgs& a, int64_t n128, int64_t n64) {
   const float t = (float)a.total / a.n_seqs;
   const float four = std::max(t / 64 * 1.3f + 5.f, n128 * (t / 128 * 1.6f + 5.f) / (2 * kUnits));

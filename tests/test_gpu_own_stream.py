@@ -85,3 +85,38 @@ def test_prompt_result_allocated_for_a_stream():
         torch.full_like(q, 5.0)
     torch.cuda.synchronize()
     assert all(torch.equal(x, want) for x in got)
+
+
+def test_steps_captured_on_the_stream_of_the_cache():
+    """A step and its advance captured on the cache's stream, replayed there across a block
+    end with eager steps between, against a cache on one stream."""
+    import torch
+    import paper_2608_05326_amd as qv
+    st = torch.cuda.Stream()
+    lens = torch.tensor([700, 60, -1], dtype=torch.int32).cuda()
+    k, v = _rnd(21, 760, 2, D), _rnd(22, 760, 2, D)
+    cu = torch.tensor([0, 700, 760, 760], dtype=torch.int32).cuda()
+    q, kn, vn = _rnd(23, 3, 8, D), _rnd(24, 3, 2, D), _rnd(25, 3, 2, D)
+    oa, ob = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    a, b = (qv.BlockCache(qv.BlockConfig(3, 8, 2, 800), stream=s) for s in (st, None))
+    for c in (a, b):
+        c.store(0, k, v, cu)
+        c.lens = lens
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        a.attend(0, q, kn, vn, oa)
+        a.advance()
+    for t in range(8):
+        if t % 3 == 2:
+            a.attend(0, q, kn, vn, oa)
+            a.advance()
+        else:
+            with torch.cuda.stream(st):
+                graph.replay()
+        b.attend(0, q, kn, vn, ob)
+        b.advance()
+        torch.cuda.synchronize()
+        assert torch.equal(oa, ob) and torch.equal(a.lens, b.lens), t
+    assert torch.equal(a.k_codes, b.k_codes) and torch.equal(a.v_scale, b.v_scale)
