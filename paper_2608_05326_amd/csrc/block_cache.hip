@@ -263,9 +263,9 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // values to bf16 (2^-8 of itself).  The sum takes P unrounded; logits, maximum, sum and
 // output are held in 32 bits, a block's value scale is applied to its products' fp32 sum.
 //
-// Bound by the pages' bytes: eight 8B sequences (401 MB) take 77 us, 32 ragged 70B places
-// (985 MB) 174 us, 5.1 and 5.7 TB/s where a large copy reaches 5.1; one sequence of 32K
-// (67 MB) 22 us, of which 3 go by before the first page is asked for and 5 in the join.
+// Bound by the pages' bytes: eight 8B sequences (401 MB) take 76 us, 32 ragged 70B places
+// (985 MB) 189 us, 5.3 and 5.2 TB/s where a large copy reaches 5.2; one sequence of 32K
+// (67 MB) 21 us, of which 3 go by before the first page is asked for and 5 in the join.
 namespace {
 constexpr float kLazyD = 8.f;
 
@@ -746,11 +746,11 @@ hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace,
   const size_t lds = (size_t)4 * a.gqa * kJoinRow * sizeof(float);
   const dim3 grid(a.B * a.H_kv + kParts);
   // Pages are read past the caches where the layer's pool (the host does not know the
-  // lengths) is more than half the 256 MB Infinity Cache: eight 8B sequences, 401 MB, 85 ->
-  // 78 us, 32 ragged places, 985 MB, 188 -> 174.  Below, the two are within 1 us: one 32K
-  // sequence, 67 MB, in turn over 8 layers 24.0 us through the caches and 23.2 past them, the
-  // same layer again and again 21.7 and 21.8; a 2K sequence, 4 MB, over 32 layers 11.2 and
-  // (in a large pool) 12.1.
+  // lengths) is more than half the 256 MB Infinity Cache: the same eight 8B sequences, 401 MB,
+  // again and again 85 -> 78 us, 32 ragged places, 985 MB, 188 -> 174.  Below, the two are
+  // within 1 us: one 32K sequence, 67 MB, in turn over 8 layers 24.0 us through the caches and
+  // 23.2 past them, the same layer again and again 21.7 and 21.8; a 2K sequence, 4 MB, in turn
+  // over 32 layers 11.2 and (in a large pool) 12.1.
   const bool past = (int64_t)a.n_pages * a.H_kv * (2 * kCodes) > (128 << 20);
   if (past) k_block_attend<true><<<grid, kThreads, lds, st>>>(a, s);
   else k_block_attend<false><<<grid, kThreads, lds, st>>>(a, s);

@@ -480,14 +480,15 @@ def _int32(t, torch, index, name, n):
 
 def _check_stream(stream, index):
     """A kernel on another device's stream would run there, on addresses of this one."""
-    if stream is not None and stream.device.index != index:
+    if stream.device.index != index:
         raise ValueError(f"the stream belongs to device {stream.device}, the tensors to cuda:{index}")
 
 
 def _launch(lib, torch, index, stream, fn, *args):
     """A handle-free call with the device of its tensors current (kernels run on the
     current device), on `stream` or torch's current one there."""
-    _check_stream(stream, index)
+    if stream is not None:
+        _check_stream(stream, index)
     before = torch.cuda.current_device()
     if before != index:
         torch.cuda.set_device(index)
@@ -588,7 +589,8 @@ class BlockCache:
             raise ValueError("sizes must be below 2^31")
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
-        _check_stream(stream, dev.index)
+        if stream is not None:
+            _check_stream(stream, dev.index)
         self.device = dev
         self.stream = stream
         L, B, h, d, n = cfg.num_layers, cfg.batch, cfg.num_kv_heads, cfg.head_dim, BLOCK_TOKENS
