@@ -569,8 +569,8 @@ class BlockCache:
     everything the cache enqueues is on that stream: its state's first contents, store, attend,
     fetch and advance(); an assigned value is copied there after the current stream's work so
     far, and the current stream waits for the copy.  The tensors that a call takes have to be
-    ready on that stream, and a program that reads or changes the state tensors in place does
-    so on it, or orders its streams with it."""
+    ready on that stream, a program that reads or changes the state tensors in place does so
+    on it, or orders its streams with it, and a graph of the calls is captured on it."""
 
     def __init__(self, cfg: BlockConfig, device="cuda", stream=None):
         import torch
