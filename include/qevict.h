@@ -518,6 +518,95 @@ qevict_status qevict_block_attend(const qevict_block_config *cfg, const qevict_b
                                   uint16_t *out, void *workspace, size_t workspace_bytes,
                                   void *hip_stream);
 
+/* Rotary positions.  Pair i of a head's channels, (i, i + num_pairs) or, interleaved,
+ * (2 i, 2 i + 1), is turned by t = p f_i, p the token's position along the axis axis[i]
+ * (text has one axis; images and video time, height and width):
+ *   x' = x cos t - y sin t,   y' = y cos t + x sin t;
+ * the channels past 2 num_pairs are copied.  turns[i] is f_i / (2 pi) 2^64 as an integer
+ * modulo 2^64, so that angles are exact to 2^-33 turns at every position; cos, sin and the
+ * products are fp32 (about 2^-23 of the pair's length), the results are rounded to bf16. */
+#define QEVICT_MAX_PAIRS 64
+#define QEVICT_MAX_AXES 4
+typedef struct {
+  int32_t abi_version;
+  int32_t num_pairs;         /* 8 .. 64, a multiple of 8                                     */
+  int32_t num_axes;          /* 1 .. 4                                                       */
+  int32_t interleaved;       /* 0 or 1                                                       */
+  uint64_t turns[QEVICT_MAX_PAIRS];
+  uint8_t axis[QEVICT_MAX_PAIRS];   /* below num_axes                                        */
+} qevict_rotary;
+
+/* Rotates packed queries and keys, as attention and the caches take them (what precedes
+ * qevict_prompt_attend, qevict_block_attend_chunk and qevict_block_attend).
+ *   positions  device int32, row r and axis a at r position_token_stride + a
+ *              position_axis_stride (elements, not negative); any value
+ *   q, q_out [total, H_q, d], k, k_out [total, H_k, d] bf16, H_k = 0: no keys (k, k_out are
+ *              not looked at).  q_out may be q, and k_out k, with the same strides; with
+ *              `inverse` the rotation is by -t: it undoes the other, and takes the gradient
+ *              of its outputs to that of its inputs. */
+typedef struct {
+  int32_t abi_version;
+  int32_t total_tokens;
+  int32_t num_q_heads;
+  int32_t num_k_heads;
+  int32_t head_dim;          /* 128 */
+  int32_t inverse;           /* 0 or 1 */
+  int64_t position_token_stride, position_axis_stride;
+  int64_t q_token_stride, q_head_stride;
+  int64_t k_token_stride, k_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride;
+  int64_t k_out_token_stride, k_out_head_stride;
+} qevict_rotate_config;
+qevict_status qevict_rotate(const qevict_rotate_config *cfg, const qevict_rotary *rotary,
+                            const int32_t *positions, const uint16_t *q, const uint16_t *k,
+                            uint16_t *q_out, uint16_t *k_out, void *hip_stream);
+
+/* Appends packed new tokens k, v [total, H_kv, d] bf16: place s's rows (by cu_tokens, B + 1
+ * entries; at most counts[s] of them, where counts [B] is given, and at most what max_context
+ * leaves) become its tokens lens[s], lens[s] + 1, ...: a block that they complete is quantized
+ * into its page, from the open block's rows and the new ones (as qevict_block_store does), the
+ * rows behind it are the open block.  With `rotary` the keys are rotated on the way (rounded
+ * to bf16, as qevict_rotate does; positions [total] as there), else it is NULL and positions
+ * is not looked at.  Places with a negative length keep what they hold.  lens is read, not
+ * advanced.  A page that is written belongs to one place. */
+qevict_status qevict_block_append(const qevict_block_config *cfg, const qevict_block_layer *layer,
+                                  const uint16_t *k, int64_t k_token_stride, int64_t k_head_stride,
+                                  const uint16_t *v, int64_t v_token_stride, int64_t v_head_stride,
+                                  const int32_t *cu_tokens, const int32_t *counts, int32_t total_tokens,
+                                  const qevict_rotary *rotary, const int32_t *positions,
+                                  int64_t position_token_stride, int64_t position_axis_stride,
+                                  void *hip_stream);
+
+/* Attention of a chunk of new tokens of every place over what the place holds and the chunk
+ * itself: a piece of a prompt, drafted tokens, or one token.  Row i of place s (its rows by
+ * cu_tokens, at most what max_context leaves) is its token lens[s] + i and attends to the
+ * tokens held (codes in complete blocks, bf16 in the open one; blocks without a page take no
+ * part) and to the chunk's rows 0 .. i, in bf16 as they are given.  Nothing is stored:
+ * qevict_block_append, after this call, takes the rows that are to be kept.  Rows of a place
+ * with a negative length, or past max_context, are left as they were.
+ *   q, out [total, H_q, d], k, v [total, H_kv, d] bf16 packed
+ *   workspace  device memory of qevict_block_chunk_workspace_size bytes for total_tokens or
+ *              more, 256-byte aligned, overwritten: calls that may overlap need one each
+ * Accuracy as qevict_prompt_attend's (the weights beside codes are rounded to bf16 with
+ * their block's value scale; a weight below 2^-126 of the row's largest may count as zero).  A value that is not finite reaches the rows that attend to it
+ * and no other.  The sums run in an order that depends on the lengths only: a call is bitwise
+ * repeatable.  total_tokens * H_q <= 2^30. */
+typedef struct {
+  int32_t abi_version;
+  int32_t total_tokens;      /* rows of the packed tensors */
+  int64_t q_token_stride, q_head_stride;
+  int64_t k_token_stride, k_head_stride;
+  int64_t v_token_stride, v_head_stride;
+  int64_t out_token_stride, out_head_stride;
+} qevict_chunk_config;
+qevict_status qevict_block_chunk_workspace_size(const qevict_block_config *cfg, int32_t total_tokens,
+                                                size_t *bytes);
+qevict_status qevict_block_attend_chunk(const qevict_block_config *cfg, const qevict_block_layer *layer,
+                                        const qevict_chunk_config *rows, const uint16_t *q,
+                                        const uint16_t *k, const uint16_t *v, const int32_t *cu_tokens,
+                                        uint16_t *out, void *workspace, size_t workspace_bytes,
+                                        void *hip_stream);
+
 const char *qevict_status_string(qevict_status s);
 const char *qevict_last_error(void);
 

@@ -142,18 +142,19 @@ struct ObsArgs {            // initial window scores from the observation querie
 // floor(cu[s] G / rows) + s on, never fewer than its tiles (a difference of floors plus one
 // is at least the ceiling of the difference), so a search over cu finds it, 64 entries a
 // step.  cu is read within [0, total]; false when tile `idx` is nobody's.  The same in
-// every lane.
+// every lane.  With `each` = 2 a sequence has a number more, for tiles that do not begin at
+// its first row (out->tile is then below n_tiles or equal, and the caller decides).
 struct PackedTile {
   int seq, start, len, tile, n_tiles;   // tile: the number inside the sequence, < n_tiles
 };
 __device__ __forceinline__ bool find_tile(const int32_t* cu, int n_seqs, int total, int per, int rows, int idx,
-                                          PackedTile* out) {
+                                          PackedTile* out, int each = 1) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = n_seqs;   // the sequence is one of [lo, lo + n)
   for (;;) {
     const int step = (n + 63) / 64, s = lo + min(lane * step, n - 1);
     const int b = min(max(cu[s], 0), total), e = min(max(cu[s + 1], b), total);
-    const int base = (int)((int64_t)b * per / rows) + s;
+    const int base = (int)((int64_t)b * per / rows) + s * each;
     const uint64_t below = __ballot(base <= idx && lane * step < n);
     if (!below) return false;
     const int w = 63 - __builtin_clzll(below);
@@ -163,12 +164,22 @@ __device__ __forceinline__ bool find_tile(const int32_t* cu, int n_seqs, int tot
       out->len = __builtin_amdgcn_readlane(e, w) - out->start;
       out->tile = idx - __builtin_amdgcn_readlane(base, w);
       out->n_tiles = (int)(((int64_t)out->len * per + rows - 1) / rows);
-      return out->tile < out->n_tiles;
+      return out->tile < out->n_tiles + each - 1;
     }
     lo += w * step;
     n = min(step, n - w * step);
   }
 }
+
+struct RotateArgs {         // rotary positions on packed queries and keys (H_k 0: no keys)
+  const uint16_t* q;
+  const uint16_t* k;
+  uint16_t* q_out;
+  uint16_t* k_out;
+  int64_t q_st, q_sh, k_st, k_sh, qo_st, qo_sh, ko_st, ko_sh;   // row and head strides
+  int32_t total, H_q, H_k;
+  int32_t heads;            // of a workgroup
+};
 
 struct PromptArgs {         // causal attention of packed prompts
   const uint16_t* q;        // rows [total] x heads, strides in elements
@@ -205,6 +216,16 @@ struct PackedRows {         // packed keys and values of a store (in) or a fetch
   int32_t total;
 };
 
+struct AppendRows {         // packed new tokens of a block cache
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t k_st, k_sh, v_st, v_sh;
+  const int32_t* cu;        // [B + 1]
+  const int32_t* counts;    // [B] rows of each place that are taken; null: all
+  int32_t total;
+  int32_t rotate;           // keys are rotated on the way
+};
+
 struct BlockStep {          // a decode step on the block cache
   const uint16_t* q;        // [B][H_q][d]
   const uint16_t* k_new;    // [B][H_kv][d]
@@ -212,6 +233,19 @@ struct BlockStep {          // a decode step on the block cache
   uint16_t* out;            // [B][H_q][d]
   float* part_o;            // [kParts + 2 B H_kv][gqa][d] partial output rows
   float2* part_ml;          // [kParts + 2 B H_kv][gqa] (maximum in log2 units, sum)
+};
+
+struct ChunkStep {          // attention of new tokens over the block cache and themselves
+  const uint16_t* q;        // rows [total] x heads, strides in elements
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* out;
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh;   // row and head strides
+  const int32_t* cu;        // [B + 1] first row of each place, then the end of the last
+  int32_t total;
+  int32_t slot_rows;        // rows of a partial result
+  float* part_o;            // [2 parts][slot_rows][d]
+  float2* part_ml;          // [2 parts][slot_rows] (maximum in log2 units, sum)
 };
 
 struct ScorePowArgs {       // p-norm ranking: prompt scores raised to the power p

@@ -1,0 +1,91 @@
+// Rotary positions: pair i of a head's channels is turned by the angle p f_i, p the token's
+// position along the axis that the pair follows.  Angles are held in turns of 2^-64: with
+// F_i = f_i / 2 pi 2^64 the product p F_i, modulo 2^64, is the angle modulo a turn, for
+// every 32-bit position and with an error of |p| 2^-65 turns (the rounding of F_i): no
+// table, and far positions are as exact as near ones.
+#pragma once
+#include "qv_device.h"
+
+namespace qv {
+
+constexpr int kMaxPairs = kHeadDim / 2, kMaxAxes = 4;
+
+struct RotaryArgs {
+  uint64_t turns[kMaxPairs];   // F_i (the inverse rotation: -F_i)
+  uint8_t axis[kMaxPairs];
+  int32_t n_pairs;             // a multiple of 8; channels past 2 n_pairs are left as they are
+  int32_t n_axes;
+  int32_t interleaved;         // pairs (2 i, 2 i + 1), else (i, i + n_pairs)
+  const int32_t* pos;          // position of row r along axis a: pos[r p_st + a p_sa]
+  int64_t p_st, p_sa;
+};
+
+// cos and sin of u 2^-32 turns, to about 2^-24.  The nearest quarter turn is taken off, the
+// rest (at most pi / 4) goes into the Taylor series, whose first terms left out are
+// x^11 / 11! < 2^-29 and x^10 / 10! < 2^-25.
+__device__ __forceinline__ float2 cos_sin(uint32_t u) {
+  const uint32_t quarter = (u + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(u - (quarter << 30)) * 0x1.921fb6p-30f;   // 2 pi 2^-32
+  const float z = x * x;
+  float s = fmaf(z, 1.f / 362880.f, -1.f / 5040.f);
+  s = fmaf(z, s, 1.f / 120.f);
+  s = fmaf(z, s, -1.f / 6.f);
+  s = fmaf(z * x, s, x);
+  float c = fmaf(z, 1.f / 40320.f, -1.f / 720.f);
+  c = fmaf(z, c, 1.f / 24.f);
+  c = fmaf(z, c, -0.5f);
+  c = fmaf(z, c, 1.f);
+  const bool swap = quarter & 1;
+  const float a = swap ? s : c, b = swap ? c : s;
+  // quarter 1: (-s, c), 2: (-c, -s), 3: (s, -c)
+  return make_float2(__uint_as_float(__float_as_uint(a) ^ ((quarter + 1) << 30 & 0x80000000u)),
+                     __uint_as_float(__float_as_uint(b) ^ (quarter << 30 & 0x80000000u)));
+}
+
+// cos and sin of pair i for a token with the positions p[axis]
+__device__ __forceinline__ float2 pair_cos_sin(const RotaryArgs& r, int i, const int32_t (&p)[kMaxAxes]) {
+  const int a = r.axis[i];
+  const int32_t at = a < 2 ? (a ? p[1] : p[0]) : (a == 2 ? p[2] : p[3]);
+  const uint64_t t = (uint64_t)(int64_t)at * r.turns[i] + 0x80000000u;
+  return cos_sin((uint32_t)(t >> 32));
+}
+
+__device__ __forceinline__ void row_positions(const RotaryArgs& r, int64_t row, int32_t (&p)[kMaxAxes]) {
+#pragma unroll
+  for (int a = 0; a < kMaxAxes; ++a) p[a] = a < r.n_axes ? r.pos[row * r.p_st + a * r.p_sa] : 0;
+}
+
+__device__ __forceinline__ uint32_t pack_rne(float lo, float hi) {
+  const bf16x2 p = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, p);
+}
+// (x, y) turned by the angle of cs
+__device__ __forceinline__ float turn_x(float x, float y, float2 cs) { return fmaf(x, cs.x, -(y * cs.y)); }
+__device__ __forceinline__ float turn_y(float x, float y, float2 cs) { return fmaf(y, cs.x, x * cs.y); }
+
+// Eight pairs: x, y are their channels in bf16, eight and eight (apart) or in turn
+// (interleaved: x the first four pairs, y the others).
+__device__ __forceinline__ void rotate_pairs(u32x4& x, u32x4& y, const float2 (&cs)[8], bool interleaved) {
+  auto lo = [](uint32_t w) { return __uint_as_float(w << 16); };
+  auto hi = [](uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); };
+  u32x4 u, v;
+  if (interleaved) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = x[j], b = y[j];
+      u[j] = pack_rne(turn_x(lo(a), hi(a), cs[j]), turn_y(lo(a), hi(a), cs[j]));
+      v[j] = pack_rne(turn_x(lo(b), hi(b), cs[j + 4]), turn_y(lo(b), hi(b), cs[j + 4]));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t a = x[j], b = y[j];
+      u[j] = pack_rne(turn_x(lo(a), lo(b), cs[2 * j]), turn_x(hi(a), hi(b), cs[2 * j + 1]));
+      v[j] = pack_rne(turn_y(lo(a), lo(b), cs[2 * j]), turn_y(hi(a), hi(b), cs[2 * j + 1]));
+    }
+  }
+  x = u;
+  y = v;
+}
+
+}  // namespace qv

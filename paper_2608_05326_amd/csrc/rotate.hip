@@ -1,0 +1,47 @@
+// Rotary positions on packed queries and keys (Sec. 4.3, the rotation that attention's keys
+// and queries carry), with one to four axes: text, or time, height and width of images and
+// video.
+#include <algorithm>
+
+#include "qv_rotary.h"
+
+namespace qv {
+
+// A thread takes eight pairs of one token (two loads of 16 bytes a head) through kHeads
+// heads; eight threads a token.
+namespace {
+constexpr int kRotThreads = 256, kTokens = kRotThreads / 8;
+}
+
+__global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a, RotaryArgs r) {
+  const int j = threadIdx.x & 7;
+  const int64_t row = (int64_t)blockIdx.x * kTokens + (threadIdx.x >> 3);
+  if (row >= a.total) return;
+  int32_t p[kMaxAxes];
+  row_positions(r, row, p);
+  const bool turned = 8 * j < r.n_pairs;
+  float2 cs[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = turned ? pair_cos_sin(r, 8 * j + i, p) : make_float2(1.f, 0.f);
+  const bool apart = turned && !r.interleaved;
+  const int cx = apart ? 8 * j : 16 * j, cy = apart ? 8 * j + r.n_pairs : 16 * j + 8;
+  const int h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.H_q + a.H_k);
+  for (int h = h0; h < h1; ++h) {
+    const bool q = h < a.H_q;
+    const uint16_t* x = q ? a.q + row * a.q_st + h * a.q_sh : a.k + row * a.k_st + (h - a.H_q) * a.k_sh;
+    uint16_t* y = q ? a.q_out + row * a.qo_st + h * a.qo_sh : a.k_out + row * a.ko_st + (h - a.H_q) * a.ko_sh;
+    u32x4 u = *(const u32x4*)(x + cx), v = *(const u32x4*)(x + cy);
+    if (turned) rotate_pairs(u, v, cs, r.interleaved);
+    *(u32x4*)(y + cx) = u;
+    *(u32x4*)(y + cy) = v;
+  }
+}
+
+hipError_t launch_rotate(RotateArgs a, const RotaryArgs& r, hipStream_t st) {
+  a.heads = 8;
+  const dim3 grid((uint32_t)((a.total + kTokens - 1) / kTokens), (uint32_t)((a.H_q + a.H_k + a.heads - 1) / a.heads));
+  k_rotate<<<grid, kRotThreads, 0, st>>>(a, r);
+  return hipGetLastError();
+}
+
+}  // namespace qv

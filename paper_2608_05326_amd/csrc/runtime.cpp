@@ -22,6 +22,7 @@ struct MigrateArgs;
 struct PackArgs;
 }  // namespace qv
 #include "qv_device.h"
+#include "qv_rotary.h"
 
 namespace qv {
 hipError_t launch_attend(const AttnArgs& a, hipStream_t st);
@@ -48,11 +49,17 @@ hipError_t launch_block_store(const BlockArgs& a, const PackedRows& r, hipStream
 hipError_t launch_block_fetch(const BlockArgs& a, const PackedRows& r, hipStream_t st);
 int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa);
 hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace, hipStream_t st);
+hipError_t launch_rotate(RotateArgs a, const RotaryArgs& r, hipStream_t st);
+int64_t block_append_groups(int64_t total, int n_seqs, int H_kv);
+hipError_t launch_block_append(const BlockArgs& a, const AppendRows& r, const RotaryArgs& rot, hipStream_t st);
+int64_t block_chunk_workspace_bytes(int64_t total, int gqa);
+hipError_t launch_chunk_attend(const BlockArgs& a, ChunkStep s, void* workspace, hipStream_t st);
 }  // namespace qv
 
 using namespace qv;
 static_assert(kScorePnorm == QEVICT_SCORE_PNORM, "score mode numbering");
 static_assert(kBlockTokens == QEVICT_BLOCK_TOKENS, "block size");
+static_assert(kMaxPairs == QEVICT_MAX_PAIRS && kMaxAxes == QEVICT_MAX_AXES, "rotary sizes");
 static_assert(kStaticObsScratchBytes == QEVICT_STATIC_SCRATCH_BYTES, "fixed scratch size");
 
 namespace {
@@ -1574,6 +1581,174 @@ qevict_status qevict_block_attend(const qevict_block_config* cfg, const qevict_b
   BlockStep step = {q, k_new, v_new, out, nullptr, nullptr};
   hipError_t e = launch_block_attend(a, step, workspace, (hipStream_t)hip_stream);
   return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_attend launch");
+}
+
+static qevict_status rotary_args(const qevict_rotary* rot, const int32_t* positions, int64_t p_st, int64_t p_sa,
+                                 int64_t total, bool inverse, RotaryArgs* r) {
+  if (!rot) return fail(QEVICT_ERR_INVALID_ARG, "rotary is NULL");
+  if (rot->abi_version != QEVICT_ABI_VERSION)
+    return fail(QEVICT_ERR_UNSUPPORTED, "abi_version %d, library implements %d", rot->abi_version, QEVICT_ABI_VERSION);
+  if (rot->num_pairs < 8 || rot->num_pairs > kMaxPairs || rot->num_pairs % 8)
+    return fail(QEVICT_ERR_UNSUPPORTED, "num_pairs must be a multiple of 8 in 8 .. %d", kMaxPairs);
+  if (rot->num_axes < 1 || rot->num_axes > kMaxAxes)
+    return fail(QEVICT_ERR_UNSUPPORTED, "num_axes must be in 1 .. %d", kMaxAxes);
+  if (rot->interleaved != 0 && rot->interleaved != 1) return fail(QEVICT_ERR_INVALID_ARG, "interleaved must be 0 or 1");
+  for (int i = 0; i < rot->num_pairs; ++i)
+    if (rot->axis[i] >= rot->num_axes) return fail(QEVICT_ERR_INVALID_ARG, "axis of pair %d is out of range", i);
+  if (!positions || ((uintptr_t)positions & 3)) return fail(QEVICT_ERR_INVALID_ARG, "positions");
+  const int64_t limit = (int64_t)1 << 58;
+  if (p_st < 0 || p_sa < 0 || (total > 1 && p_st > limit / total) || p_sa > limit)
+    return fail(QEVICT_ERR_INVALID_ARG, "strides of positions");
+  for (int i = 0; i < kMaxPairs; ++i) {
+    const bool used = i < rot->num_pairs;
+    r->turns[i] = !used ? 0 : inverse ? 0 - rot->turns[i] : rot->turns[i];
+    r->axis[i] = used ? rot->axis[i] : 0;
+  }
+  r->n_pairs = rot->num_pairs;
+  r->n_axes = rot->num_axes;
+  r->interleaved = rot->interleaved;
+  r->pos = positions;
+  r->p_st = p_st;
+  r->p_sa = p_sa;
+  return QEVICT_OK;
+}
+
+qevict_status qevict_rotate(const qevict_rotate_config* cfg, const qevict_rotary* rotary, const int32_t* positions,
+                            const uint16_t* q, const uint16_t* k, uint16_t* q_out, uint16_t* k_out,
+                            void* hip_stream) {
+  if (!cfg) return fail(QEVICT_ERR_INVALID_ARG, "config is NULL");
+  if (cfg->abi_version != QEVICT_ABI_VERSION)
+    return fail(QEVICT_ERR_UNSUPPORTED, "abi_version %d, library implements %d", cfg->abi_version, QEVICT_ABI_VERSION);
+  if (cfg->num_q_heads < 1 || cfg->num_k_heads < 0) return fail(QEVICT_ERR_INVALID_ARG, "head counts");
+  if (cfg->head_dim != kHeadDim) return fail(QEVICT_ERR_UNSUPPORTED, "head_dim must be 128");
+  if (cfg->inverse != 0 && cfg->inverse != 1) return fail(QEVICT_ERR_INVALID_ARG, "inverse must be 0 or 1");
+  if (cfg->total_tokens < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (cfg->total_tokens == 0) return QEVICT_OK;
+  const int64_t n = cfg->total_tokens;
+  const int hq = cfg->num_q_heads, hk = cfg->num_k_heads;
+  RotaryArgs r;
+  qevict_status s = rotary_args(rotary, positions, cfg->position_token_stride, cfg->position_axis_stride, n,
+                                cfg->inverse, &r);
+  if (s) return s;
+  if ((s = check_rows("q", q, n, hq, cfg->q_token_stride, cfg->q_head_stride, false)) ||
+      (s = check_rows("q_out", q_out, n, hq, cfg->q_out_token_stride, cfg->q_out_head_stride, true)))
+    return s;
+  if (hk && ((s = check_rows("k", k, n, hk, cfg->k_token_stride, cfg->k_head_stride, false)) ||
+             (s = check_rows("k_out", k_out, n, hk, cfg->k_out_token_stride, cfg->k_out_head_stride, true))))
+    return s;
+  auto moved = [&](const uint16_t* x, const uint16_t* y, int heads, int64_t st, int64_t sh, int64_t ot, int64_t oh) {
+    return x == y && ((n > 1 && st != ot) || (heads > 1 && sh != oh));
+  };
+  if (moved(q, q_out, hq, cfg->q_token_stride, cfg->q_head_stride, cfg->q_out_token_stride, cfg->q_out_head_stride) ||
+      (hk && moved(k, k_out, hk, cfg->k_token_stride, cfg->k_head_stride, cfg->k_out_token_stride,
+                   cfg->k_out_head_stride)))
+    return fail(QEVICT_ERR_INVALID_ARG, "in place, an output has its input's strides");
+  if (n * ((int64_t)hq + hk) > ((int64_t)1 << 30) || hq + (int64_t)hk > 65535)
+    return fail(QEVICT_ERR_UNSUPPORTED, "too many rows for one call");
+  RotateArgs a;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_st = cfg->q_token_stride;
+  a.q_sh = cfg->q_head_stride;
+  a.k_st = cfg->k_token_stride;
+  a.k_sh = cfg->k_head_stride;
+  a.qo_st = cfg->q_out_token_stride;
+  a.qo_sh = cfg->q_out_head_stride;
+  a.ko_st = cfg->k_out_token_stride;
+  a.ko_sh = cfg->k_out_head_stride;
+  a.total = cfg->total_tokens;
+  a.H_q = hq;
+  a.H_k = hk;
+  hipError_t e = launch_rotate(a, r, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "rotate launch");
+}
+
+qevict_status qevict_block_append(const qevict_block_config* cfg, const qevict_block_layer* layer, const uint16_t* k,
+                                  int64_t k_token_stride, int64_t k_head_stride, const uint16_t* v,
+                                  int64_t v_token_stride, int64_t v_head_stride, const int32_t* cu_tokens,
+                                  const int32_t* counts, int32_t total_tokens, const qevict_rotary* rotary,
+                                  const int32_t* positions, int64_t position_token_stride,
+                                  int64_t position_axis_stride, void* hip_stream) {
+  BlockArgs a;
+  PackedRows r;
+  RotaryArgs rot = {};
+  qevict_status s = block_args(cfg, layer, &a);
+  if (s) return s;
+  if (total_tokens < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (total_tokens == 0) return QEVICT_OK;
+  if ((s = packed_rows(a, k, k_token_stride, k_head_stride, v, v_token_stride, v_head_stride, cu_tokens,
+                       total_tokens, false, &r)))
+    return s;
+  if ((uintptr_t)counts & 3) return fail(QEVICT_ERR_INVALID_ARG, "counts must be 4-byte aligned");
+  if (rotary && (s = rotary_args(rotary, positions, position_token_stride, position_axis_stride, total_tokens, false,
+                                 &rot)))
+    return s;
+  if (block_append_groups(total_tokens, a.B, a.H_kv) > kMaxGroups)
+    return fail(QEVICT_ERR_UNSUPPORTED, "sequences too large for one call");
+  const AppendRows rows = {r.k, r.v, r.k_st, r.k_sh, r.v_st, r.v_sh, r.cu, counts, total_tokens, rotary != nullptr};
+  hipError_t e = launch_block_append(a, rows, rot, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_append launch");
+}
+
+static qevict_status check_chunk_tokens(const qevict_block_config* cfg, int64_t total) {
+  if (total < 0) return fail(QEVICT_ERR_INVALID_ARG, "total_tokens is negative");
+  if (total * cfg->num_q_heads > ((int64_t)1 << 30))
+    return fail(QEVICT_ERR_UNSUPPORTED, "chunks too large for one call");
+  return QEVICT_OK;
+}
+
+qevict_status qevict_block_chunk_workspace_size(const qevict_block_config* cfg, int32_t total_tokens, size_t* bytes) {
+  qevict_status s = check_block_config(cfg);
+  if (s || (s = check_chunk_tokens(cfg, total_tokens))) return s;
+  if (!bytes) return fail(QEVICT_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = total_tokens ? (size_t)block_chunk_workspace_bytes(total_tokens, cfg->num_q_heads / cfg->num_kv_heads) : 0;
+  return QEVICT_OK;
+}
+
+qevict_status qevict_block_attend_chunk(const qevict_block_config* cfg, const qevict_block_layer* layer,
+                                        const qevict_chunk_config* rows, const uint16_t* q, const uint16_t* k,
+                                        const uint16_t* v, const int32_t* cu_tokens, uint16_t* out, void* workspace,
+                                        size_t workspace_bytes, void* hip_stream) {
+  BlockArgs a;
+  qevict_status s = block_args(cfg, layer, &a);
+  if (s) return s;
+  if (!rows) return fail(QEVICT_ERR_INVALID_ARG, "rows is NULL");
+  if (rows->abi_version != QEVICT_ABI_VERSION)
+    return fail(QEVICT_ERR_UNSUPPORTED, "abi_version %d, library implements %d", rows->abi_version,
+                QEVICT_ABI_VERSION);
+  const int64_t n = rows->total_tokens;
+  if ((s = check_chunk_tokens(cfg, n))) return s;
+  if (n == 0) return QEVICT_OK;
+  if (!cu_tokens || ((uintptr_t)cu_tokens & 3)) return fail(QEVICT_ERR_INVALID_ARG, "cu_tokens");
+  if ((s = check_rows("q", q, n, a.H_q, rows->q_token_stride, rows->q_head_stride, false)) ||
+      (s = check_rows("k", k, n, a.H_kv, rows->k_token_stride, rows->k_head_stride, false)) ||
+      (s = check_rows("v", v, n, a.H_kv, rows->v_token_stride, rows->v_head_stride, false)) ||
+      (s = check_rows("out", out, n, a.H_q, rows->out_token_stride, rows->out_head_stride, true)))
+    return s;
+  if (!workspace || ((uintptr_t)workspace & 255))
+    return fail(QEVICT_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
+  const int64_t need = block_chunk_workspace_bytes(n, a.gqa);
+  if (workspace_bytes < (size_t)need)
+    return fail(QEVICT_ERR_WORKSPACE, "workspace has %zu bytes, needs %lld", workspace_bytes, (long long)need);
+  ChunkStep c = {};
+  c.q = q;
+  c.k = k;
+  c.v = v;
+  c.out = out;
+  c.q_st = rows->q_token_stride;
+  c.q_sh = rows->q_head_stride;
+  c.k_st = rows->k_token_stride;
+  c.k_sh = rows->k_head_stride;
+  c.v_st = rows->v_token_stride;
+  c.v_sh = rows->v_head_stride;
+  c.o_st = rows->out_token_stride;
+  c.o_sh = rows->out_head_stride;
+  c.cu = cu_tokens;
+  c.total = rows->total_tokens;
+  hipError_t e = launch_chunk_attend(a, c, workspace, (hipStream_t)hip_stream);
+  return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_attend_chunk launch");
 }
 
 }  // extern "C"

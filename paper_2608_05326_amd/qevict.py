@@ -11,6 +11,7 @@ import contextlib
 import ctypes
 import math
 import dataclasses
+import fractions
 import os
 
 import numpy as np
@@ -30,6 +31,7 @@ FLAG_ROUTING_QUEUE_WAIT, FLAG_ROUTING_DEVICE_WAIT = 0x8, 0x10
 KERNEL_ATTEND, KERNEL_MERGE, KERNEL_RETIER, KERNEL_MIGRATE = range(4)
 SCORE_CUMULATIVE, SCORE_DECAY, SCORE_KEY_NORM, SCORE_PNORM = 0, 1, 2, 3
 BLOCK_TOKENS = 64
+MAX_PAIRS, MAX_AXES = 64, 4
 INT32_MAX = 2 ** 31 - 1
 
 # exported symbols declared in include/qevict.h
@@ -42,7 +44,8 @@ SYMBOLS = (
     "qevict_status_string", "qevict_last_error", "qevict_prefill_scores_scratch_size",
     "qevict_prefill_scores", "qevict_capacities_for_budget", "qevict_memory_report",
     "qevict_prefill_scores_noalloc", "qevict_prompt_attend", "qevict_block_store", "qevict_block_fetch",
-    "qevict_block_workspace_size", "qevict_block_attend",
+    "qevict_block_workspace_size", "qevict_block_attend", "qevict_rotate", "qevict_block_append",
+    "qevict_block_chunk_workspace_size", "qevict_block_attend_chunk",
 )
 
 
@@ -79,6 +82,25 @@ class _BlockConfig(ctypes.Structure):
 class _BlockLayer(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in (
         "k_codes", "v_codes", "k_scale", "v_scale", "k_tail", "v_tail", "table", "lens")]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("abi_version", "num_pairs", "num_axes", "interleaved")] + [
+        ("turns", ctypes.c_uint64 * MAX_PAIRS), ("axis", ctypes.c_uint8 * MAX_PAIRS)]
+
+
+class _RotateConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "abi_version", "total_tokens", "num_q_heads", "num_k_heads", "head_dim", "inverse")] + [
+        (n, ctypes.c_int64) for n in (
+            "position_token_stride", "position_axis_stride", "q_token_stride", "q_head_stride", "k_token_stride",
+            "k_head_stride", "q_out_token_stride", "q_out_head_stride", "k_out_token_stride", "k_out_head_stride")]
+
+
+class _ChunkConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("abi_version", "total_tokens")] + [(n, ctypes.c_int64) for n in (
+        "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride",
+        "out_token_stride", "out_head_stride")]
 
 
 class MemoryReport(ctypes.Structure):
@@ -181,6 +203,12 @@ def load_library(path: str | None = None):
         "qevict_block_fetch": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, i32, vp],
         "qevict_block_workspace_size": [P(_BlockConfig), P(ctypes.c_size_t)],
         "qevict_block_attend": [P(_BlockConfig), P(_BlockLayer), vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+        "qevict_rotate": [P(_RotateConfig), P(_Rotary), vp, vp, vp, vp, vp, vp],
+        "qevict_block_append": [P(_BlockConfig), P(_BlockLayer), vp, i64, i64, vp, i64, i64, vp, vp, i32,
+                                P(_Rotary), vp, i64, i64, vp],
+        "qevict_block_chunk_workspace_size": [P(_BlockConfig), i32, P(ctypes.c_size_t)],
+        "qevict_block_attend_chunk": [P(_BlockConfig), P(_BlockLayer), P(_ChunkConfig), vp, vp, vp, vp, vp, vp,
+                                      ctypes.c_size_t, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -534,6 +562,107 @@ def prompt_attend(q, k, v, cu_tokens, out=None, softmax_scale: float = 0.0, stre
     return out
 
 
+_PI = fractions.Fraction("3.14159265358979323846264338327950288419716939937510582097494")
+
+
+class Rotary:
+    """A rotation by positions: which pairs of a head's channels turn, how fast, and along
+    which axis of the positions.
+
+      base         pair i of n turns by p base^(-i / n) radians at position p
+      dim          the first `dim` channels of a head turn (a multiple of 16, at most 128),
+                   n = dim / 2 pairs; the others are left as they are
+      sections     pairs that follow each axis, one run behind the other, together n:
+                   (n,) for text, three for time, height and width; up to four axes
+      axes         or the axis of every pair, in any order
+      inv_freq     or the radians a position of every pair (scaled or per-axis frequencies)
+      interleaved  pairs (2 i, 2 i + 1) instead of (i, i + n)
+
+    A plain object on the host: it may be shared between devices, streams and graphs."""
+
+    def __init__(self, base: float = 10000.0, dim: int = 128, sections=None, axes=None, inv_freq=None,
+                 interleaved: bool = False):
+        if dim % 16 or not 16 <= dim <= 2 * MAX_PAIRS:
+            raise ValueError(f"dim must be a multiple of 16 in 16 .. {2 * MAX_PAIRS}, got {dim}")
+        n = dim // 2
+        if sections is not None and axes is not None:
+            raise ValueError("give sections or axes, not both")
+        if axes is None:
+            sections = (n,) if sections is None else tuple(int(x) for x in sections)
+            if sum(sections) != n or min(sections) < 0:
+                raise ValueError(f"sections must sum to the {n} pairs, got {sections}")
+            axes = [a for a, m in enumerate(sections) for _ in range(m)]
+            self.num_axes = len(sections)
+        else:
+            axes = [int(a) for a in axes]
+            self.num_axes = max(axes, default=-1) + 1
+        if not 1 <= self.num_axes <= MAX_AXES:
+            raise ValueError(f"1 to {MAX_AXES} axes, got {self.num_axes}")
+        if len(axes) != n or min(axes) < 0:
+            raise ValueError(f"axes must name an axis for each of the {n} pairs, got {axes}")
+        if inv_freq is None:
+            if not (math.isfinite(base) and base > 0):
+                raise ValueError(f"base must be positive, got {base}")
+            inv_freq = [base ** (-i / n) for i in range(n)]
+        inv_freq = [float(f) for f in inv_freq]
+        if len(inv_freq) != n or not all(math.isfinite(f) and abs(f) < 2.0 ** 32 for f in inv_freq):
+            raise ValueError(f"inv_freq must be {n} numbers below 2^32")
+        self.dim, self.interleaved, self.axes, self.inv_freq = dim, bool(interleaved), axes, inv_freq
+        self._c = _Rotary(ABI_VERSION, n, self.num_axes, int(self.interleaved))
+        for i, (a, f) in enumerate(zip(axes, inv_freq)):
+            self._c.axis[i] = a
+            # (a float64 quotient would be off by 2^-53 of itself: by more at far positions)
+            self._c.turns[i] = round(fractions.Fraction(f) / (2 * _PI) * 2 ** 64) % 2 ** 64
+
+    def _positions(self, positions, torch, index, tokens):
+        """Address and (token, axis) strides of positions, int32 [T] (one axis) or [T, axes]."""
+        if positions.get_device() != index or positions.dtype is not torch.int32:
+            raise ValueError(f"positions must be int32 on device cuda:{index}, got {positions.dtype} on "
+                             f"{positions.device}")
+        sh, st = positions.shape, positions.stride()
+        if sh != (tokens, self.num_axes) and not (self.num_axes == 1 and sh == (tokens,)):
+            raise ValueError(f"positions must be [{tokens}, {self.num_axes}], got shape {tuple(sh)}")
+        return (positions.data_ptr(), st[0] if tokens > 1 else 0,
+                st[1] if self.num_axes > 1 else 0)
+
+
+def rotate(q, k, positions, rotary: Rotary, q_out=None, k_out=None, inverse: bool = False, stream=None):
+    """Rotary positions on packed queries and keys, what precedes prompt_attend,
+    BlockCache.attend_chunk and attend.  q: bf16 [T, H_q, 128], k: bf16 [T, H_kv, 128] or None;
+    strides as in prompt_attend.  positions: int32 [T], or [T, axes] for a rotary with several
+    axes; any strides, any values.  Returns (q_out, k_out), allocated here unless given; q_out
+    may be q and k_out k.  inverse: by the opposite angles, which undoes a rotation and takes
+    the gradient of its outputs to the gradient of its inputs (none is recorded).  Streams as in
+    prompt_attend."""
+    lib = load_library()
+    import torch
+    index = q.get_device()
+    qp, q_st, q_sh = _rows(q, torch, index, "q")
+    T, hq, d = q.shape
+    hk, kp, k_st, k_sh, kop, ko_st, ko_sh = 0, None, 0, 0, None, 0, 0
+    if k is not None:
+        kp, k_st, k_sh = _rows(k, torch, index, "k", None, T, d)
+        hk = k.shape[1]
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    if q_out is None or (k is not None and k_out is None):
+        # from the pool of the stream that writes them: elsewhere pending work may still use them
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            if q_out is None:
+                q_out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=q.device)
+            if k is not None and k_out is None:
+                k_out = torch.empty((T, hk, d), dtype=torch.bfloat16, device=q.device)
+    qop, qo_st, qo_sh = _rows(q_out, torch, index, "q_out", hq, T, d)
+    if k is not None:
+        kop, ko_st, ko_sh = _rows(k_out, torch, index, "k_out", hk, T, d)
+    pos, p_st, p_sa = rotary._positions(positions, torch, index, T)
+    c = _RotateConfig(ABI_VERSION, T, hq, hk, d, int(bool(inverse)), p_st, p_sa, q_st, q_sh, k_st, k_sh,
+                      qo_st, qo_sh, ko_st, ko_sh)
+    _launch(lib, torch, index, stream, lib.qevict_rotate, ctypes.byref(c), ctypes.byref(rotary._c), pos, qp, kp,
+            qop, kop)
+    return q_out, k_out
+
+
 @dataclasses.dataclass
 class BlockConfig:
     batch: int
@@ -544,6 +673,7 @@ class BlockConfig:
     num_layers: int = 1
     head_dim: int = 128
     softmax_scale: float = 0.0
+    chunk_tokens: int = 0        # most rows of an attend_chunk call (0: none is made)
 
 
 class BlockCache:
@@ -561,6 +691,10 @@ class BlockCache:
     columns of the table; otherwise the table starts at -1 and the program assigns pages
     (before the block they are for is complete).  lens starts at -1: the program sets it after
     storing a prompt and advances it after each step (advance()).
+
+    A step of several new tokens (pieces of prompts, drafted tokens) is, for every layer,
+    attend_chunk() over what is held and the chunk itself, then append() of the tokens that
+    are kept; then advance(cu_tokens), once.
 
     Assigning to one of them copies into it.  Steps of one cache share its workspace and open
     blocks: they run one after the other.
@@ -582,10 +716,10 @@ class BlockCache:
         if dev.type != "cuda":
             raise ValueError(f"a block cache needs a GPU, got device {dev}")
         if cfg.batch < 1 or cfg.max_context < 1 or cfg.num_layers < 1 or cfg.num_kv_heads < 1 or \
-                cfg.num_pages < 0:
+                cfg.num_pages < 0 or cfg.chunk_tokens < 0:
             raise ValueError("batch, max_context, num_layers and num_kv_heads must be positive")
         if max(cfg.batch, cfg.max_context, cfg.num_pages, cfg.num_q_heads, cfg.num_kv_heads,
-               cfg.head_dim) > INT32_MAX:   # the C ABI's fields, which ctypes would cut to their low bits
+               cfg.head_dim, cfg.chunk_tokens) > INT32_MAX:   # the C ABI's fields, which ctypes would cut to their low bits
             raise ValueError("sizes must be below 2^31")
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
@@ -600,6 +734,9 @@ class BlockCache:
         self._c = _BlockConfig(ABI_VERSION, B, cfg.num_q_heads, h, d, cfg.max_context, pages, cfg.softmax_scale)
         need = ctypes.c_size_t()
         _check(self.lib, self.lib.qevict_block_workspace_size(ctypes.byref(self._c), ctypes.byref(need)))
+        chunk = ctypes.c_size_t()
+        _check(self.lib, self.lib.qevict_block_chunk_workspace_size(ctypes.byref(self._c), cfg.chunk_tokens,
+                                                                    ctypes.byref(chunk)))
         z = torch.zeros
         with self._on_stream():   # (its memory is then reused in that stream's order, too)
             self._state = dict(
@@ -614,6 +751,7 @@ class BlockCache:
             if not cfg.num_pages:
                 self._state["table"].copy_(torch.arange(pages, dtype=torch.int32).view(B, cols))
             self.workspace = torch.empty(need.value, dtype=torch.uint8, device=dev)
+            self.chunk_workspace = torch.empty(chunk.value, dtype=torch.uint8, device=dev) if chunk.value else None
         current = self._other_stream()
         if current is not None:
             current.wait_stream(stream)
@@ -678,10 +816,61 @@ class BlockCache:
             p.append(x.data_ptr())
         self._call(self.lib.qevict_block_attend, layer, *p, self.workspace.data_ptr(), self.workspace.numel())
 
-    def advance(self):
-        """After a step's last layer: lens + 1 where a place holds a sequence that has room."""
+    def attend_chunk(self, layer: int, q, k, v, cu_tokens, out):
+        """Attention of new tokens over what the places hold and themselves: row i of place s
+        (rows cu_tokens[s] .. cu_tokens[s + 1] - 1) is its token lens[s] + i and attends to the
+        tokens held and to its chunk's rows up to itself.  q, out: bf16 [T, H_q, d]; k, v: bf16
+        [T, H_kv, d]; strides as in prompt_attend; T at most the config's chunk_tokens.  Nothing
+        is stored: append() does, afterwards.  Rows of places that hold no sequence (a negative
+        length), and those past max_context, are left as they were."""
+        t, c, i = self.torch, self.cfg, self.device.index
+        T = q.shape[0]
+        if T > c.chunk_tokens:
+            raise ValueError(f"{T} rows, the cache was made for chunk_tokens={c.chunk_tokens}")
+        qp, q_st, q_sh = _rows(q, t, i, "q", c.num_q_heads, None, c.head_dim)
+        kp, k_st, k_sh = _rows(k, t, i, "k", c.num_kv_heads, T, c.head_dim)
+        vp, v_st, v_sh = _rows(v, t, i, "v", c.num_kv_heads, T, c.head_dim)
+        op, o_st, o_sh = _rows(out, t, i, "out", c.num_q_heads, T, c.head_dim)
+        cu = _int32(cu_tokens, t, i, "cu_tokens", c.batch + 1)
+        if T == 0:
+            return
+        rows = _ChunkConfig(ABI_VERSION, T, q_st, q_sh, k_st, k_sh, v_st, v_sh, o_st, o_sh)
+        self._call(self.lib.qevict_block_attend_chunk, layer, ctypes.byref(rows), qp, kp, vp, cu, op,
+                   self.chunk_workspace.data_ptr(), self.chunk_workspace.numel())
+
+    def append(self, layer: int, k, v, cu_tokens, rotary: Rotary | None = None, positions=None, counts=None):
+        """Puts new tokens behind the places': rows cu_tokens[s] .. of k, v (bf16 [T, H_kv, d],
+        strides as in prompt_attend) become tokens lens[s], lens[s] + 1, ... of place s, the
+        first counts[s] of them (int32 [batch]) where counts is given.  Blocks that they complete
+        are quantized.  With a rotary, k holds keys before their rotation, and positions their
+        positions as in rotate(): they are rotated on the way.  After attend_chunk(), if that
+        is called; places with a negative length keep what they hold."""
+        t, i = self.torch, self.device.index
+        pos = (None, 0, 0)
+        if rotary is not None:
+            if positions is None:
+                raise ValueError("a rotary needs positions")
+            pos = rotary._positions(positions, t, i, k.shape[0])
+        elif positions is not None:
+            raise ValueError("positions without a rotary")
+        *rows, cu, T = self._packed(k, v, cu_tokens)
+        n = None if counts is None else _int32(counts, t, i, "counts", self.cfg.batch)
+        self._call(self.lib.qevict_block_append, layer, *rows, cu, n, T,
+                   None if rotary is None else ctypes.byref(rotary._c), *pos)
+
+    def advance(self, cu_tokens=None, counts=None):
+        """After a step's last layer: lens + 1 where a place holds a sequence that has room;
+        with cu_tokens (and counts) lens + the tokens that append() took."""
+        t = self.torch
         with self._on_stream():
-            self.lens += ((self.lens >= 0) & (self.lens < self.cfg.max_context)).to(self.lens.dtype)
+            live = (self.lens >= 0) & (self.lens < self.cfg.max_context)
+            if cu_tokens is None:
+                self.lens += live.to(self.lens.dtype)
+                return
+            n = (cu_tokens[1:] - cu_tokens[:-1]).clamp_(min=0)
+            if counts is not None:
+                n = t.minimum(n, counts.clamp(min=0))
+            self.lens += t.where(live, t.minimum(n, self.cfg.max_context - self.lens), 0).to(self.lens.dtype)
 
 
 def _state_tensor(name):
