@@ -157,253 +157,582 @@ __device__ __forceinline__ int64_t line_total(const BlockArgs& a, const ChunkSte
   return total;
 }
 
-// Bytes between the rows of a wave's staged values, and of joined outputs (floats).
-constexpr int kJoin = kHeadDim + 4;
-constexpr int kLds = std::max(kWaves * kBlk * kRowBytes, kWaves * 32 * kJoin * (int)sizeof(float));
-}  // namespace
+// threadIdx.x, not to be seen through: what is derived from it is computed where it is used
+// (hoisted out of the walk over segments, it would fill the registers that the products need).
+__device__ __forceinline__ int thread_here() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
 
-__global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, ChunkStep s) {
-  // 64 value rows of each wave; later the waves' outputs
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
-  __shared__ float2 sml[kWaves][32];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, lh = lane >> 5;
-  // parts of one KV head on one XCD (workgroup i runs on XCD i % 8)
-  const int part = (blockIdx.x & 7) * (kChunkParts / 8) + (blockIdx.x >> 3);
+// What a row tile's workgroup needs of a segment, beside the segment.
+struct RowTile {
+  int lo, hi;                // its tiles of 64 keys
+  int pos0, n_rows;          // first new token, (position, head) rows
+  bool whole;                // all of the row tile's keys
+};
 
-  __shared__ LinePlaces lp;
-  const int64_t total = line_total(a, s, lp), size = lane_of(chunk_part(total), 0);
-  const int64_t begin = part * size, end = min(begin + size, total);
-
-  const float qm = __builtin_amdgcn_frexp_mantf(a.scale_log2);
-  const int qe0 = __builtin_amdgcn_frexp_expf(a.scale_log2);
-
-  auto segment = [&](const Segment& sg) {
-    const ChunkPlace& p = sg.p;
-    const int v_all = chunk_key_tiles(p, sg.tile);
-    const int lo = chunk_key_tile(sg.from), hi = chunk_key_tile(sg.to);
-    if (lo >= hi) return;
-    const int pos0 = sg.tile * p.per, n_rows = (chunk_end(p, sg.tile) - pos0) * a.gqa;
-    const int row = min(lr, n_rows - 1), i_row = pos0 + row / a.gqa, head = sg.g * a.gqa + row % a.gqa;
-    const int pos = p.held + i_row;                  // this lane's position
-    const int last = p.held + p.n - 1;               // the place's last position
-    // query: k-step 2 j + e covers channels 32 j + 16 lh + 8 e + 0 .. 7
-    u32x4 q[8];
-    const uint16_t* qp = s.q + (sg.start + i_row) * s.q_st + head * s.q_sh + 16 * lh;
+// The query of one row as the B operand of eight k-steps, scaled (a power of two) into
+// bf16's range; returns the power of two that takes the products back.  WIDE: k-step ks
+// covers channels 16 ks + 8 lh + 0 .. 7, else 32 (ks / 2) + 16 lh + 8 (ks % 2) + 0 .. 7.
+template <bool WIDE>
+__device__ __forceinline__ int load_query(const uint16_t* p, int lh, u32x4 (&q)[8]) {
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[ks] = *(const u32x4*)(qp + 32 * (ks >> 1) + 8 * (ks & 1));
-    uint32_t am = 0;
+  for (int ks = 0; ks < 8; ++ks)
+    q[ks] = *(const u32x4*)(p + (WIDE ? 16 * ks + 8 * lh : 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1)));
+  uint32_t am = 0;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) am = amax_pair(q[ks], am);
-    am = amax_bits(am);
-    am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
-    const int ex = max((int)(am >> 23), 1) - 127;    // (a row of subnormals keeps its scale)
+  for (int ks = 0; ks < 8; ++ks) am = amax_pair(q[ks], am);
+  am = amax_bits(am);
+  am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+  const int ex = max((int)(am >> 23), 1) - 127;    // (a row of subnormals keeps its scale)
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
+  for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w = q[ks][j];
-        q[ks][j] = pack_bf16(ldexpf(lo_f32(w), kQueryExp - ex), ldexpf(hi_f32(w), kQueryExp - ex));
-      }
-    const int qe = qe0 + ex - kQueryExp;
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = q[ks][j];
+      q[ks][j] = pack_bf16(ldexpf(lo_f32(w), kQueryExp - ex), ldexpf(hi_f32(w), kQueryExp - ex));
+    }
+  return ex - kQueryExp;
+}
+// Log2 units per raw logit of keys with the scale ks: scale_log2 2^ex ks.  The power of two
+// comes last: products of small queries and large keys are logits of ordinary size.
+__device__ __forceinline__ float logit_scale(const BlockArgs& a, int ex, float ks) {
+  const float x = ldexpf(__builtin_amdgcn_frexp_mantf(a.scale_log2) * ks,
+                         __builtin_amdgcn_frexp_expf(a.scale_log2) + ex);
+  return x == INFINITY ? __FLT_MAX__ : x;   // (a product of zero is a logit of zero)
+}
 
-    f32x16 o[4];
+// Running maximum (log2 units), sum and output of one row: o[c][i] is channel
+// 32 c + 8 (i / 4) + 4 lh + i % 4.
+struct Running {
+  float m, l;
+  f32x16 o[4];
+};
+__device__ __forceinline__ void clear(Running& r) {
+  r.m = -INFINITY;
+  r.l = 0.f;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r.o[c][i] = 0.f;
+}
+// Weights exp2(st sc - m), in bf16 with the values' scale vs; m, l and o are kept.
+template <int KT>
+__device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float sc, float vs, u32x4 (&pw)[2 * KT]) {
+  float mt = -INFINITY;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mt = fmaxf(mt, st[kt][i]);
+  mt = half_max(mt) * sc;
+  if (__any(mt > r.m + kLazy)) {
+    const float mn = fmaxf(r.m, mt);
+    const float al = r.m == mn ? 1.f : __builtin_amdgcn_exp2f(r.m - mn);
+    r.m = mn;
+    r.l *= al;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[c][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+      for (int i = 0; i < 16; ++i) r.o[c][i] *= al;
+  }
+  const float mu = r.m > -INFINITY ? r.m : 0.f;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float e0 = __builtin_amdgcn_exp2f(fmaf(st[kt][i], sc, -mu));
+      const float e1 = __builtin_amdgcn_exp2f(fmaf(st[kt][i + 1], sc, -mu));
+      r.l += e0 + e1;
+      pw[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(e0 * vs, e1 * vs);
+    }
+}
+
+// A value that is not finite must not reach a row that its key is masked for, through
+// 0 * infinity: such values of rows in bf16 are left out of the products, and added to the
+// rows that see them afterwards.
+__device__ __forceinline__ bool take_out(u32x4& x) {
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (nonfinite(x[j])) {
+      odd = true;
+      if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
+      if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
+    }
+  return odd;
+}
+template <class Row>
+__device__ __forceinline__ void add_odd(Running& r, Row row, int n, int lh) {   // rows 0 .. n - 1 are seen
+  for (int key = 0; key < n; ++key) {
+    const uint16_t* vr = row(key) + 4 * lh;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint16_t x = vr[32 * c + 8 * (i >> 2) + (i & 3)];
+        if ((x & 0x7F80u) == 0x7F80u) r.o[c][i] += bf16_to_f32(x);
+      }
+  }
+}
+
+// Keys (values) of position p of a place, a row in bf16: of the open block or of the chunk.
+__device__ __forceinline__ const uint16_t* fresh_row(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
+                                                     bool values, int p) {
+  if (p < sg.p.held)
+    return (values ? a.v_tail : a.k_tail) + ((int64_t)sg.seq * a.H_kv + sg.g) * kCodes + (p % kBlk) * kHeadDim;
+  const int64_t row = sg.start + (p - sg.p.held);
+  return values ? s.v + row * s.v_st + sg.g * s.v_sh : s.k + row * s.k_st + sg.g * s.k_sh;
+}
+
+// Address of a row's output in `out`.
+__device__ __forceinline__ uint16_t* out_row(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
+                                             const RowTile& rt, int row) {
+  return s.out + (sg.start + rt.pos0 + row / a.gqa) * s.o_st + (sg.g * a.gqa + row % a.gqa) * s.o_sh;
+}
+
+// Bytes between the rows of a wave's staged values, and of joined outputs (floats).
+constexpr int kJoin = kHeadDim + 4;
+constexpr int kLds = std::max(kWaves * kBlk * kRowBytes, kWaves * 32 * kJoin * (int)sizeof(float));
+
+// ---- few rows: RS sets of 32 rows, the other waves of a set take the key tiles in turn,
+// pages straight into registers
+__device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
+                                           const RowTile& rt, int part, uint8_t* lds, float2 (*sml)[32]) {
+  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int rs = sg.p.rows >> 5;                      // 1, 2 or 4
+  const int rw = wave & (rs - 1), kg = wave / rs, n_kg = kWaves / rs;
+  const int row = min(rw * 32 + lr, rt.n_rows - 1), i_row = rt.pos0 + row / a.gqa;
+  const int pos = sg.p.held + i_row;                  // this lane's position
+  const int last = sg.p.held + sg.p.n - 1;            // the place's last position
+  u32x4 q[8];
+  const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + row % a.gqa) * s.q_sh, lh, q);
+  Running r;
+  clear(r);
+  f32x16 st[2];
+  u32x4 pw[4];
+  // row lr of an A operand is this key of 32; a lane's logits st[kt][i] are those of keys
+  // 32 kt + 16 lh + i
+  const int krow = 16 * ((lr >> 2) & 1) + 4 * (lr >> 3) + (lr & 3);
+  const int n_blk = sg.p.held / kBlk;
+
+  for (int t = rw * 32 < rt.n_rows ? rt.lo + kg : rt.hi; t < rt.hi; t += n_kg) {
+    if (t < n_blk) {
+      const int page = page_of(a, sg.seq, t);
+      if (page < 0) continue;
+      const int64_t e = (int64_t)page * a.H_kv + sg.g;
+      const int8_t* kc = a.k_codes + e * kCodes + krow * kHeadDim + 16 * lh;
+      const int8_t* vc = a.v_codes + e * kCodes + lr * kBlk + 16 * lh;
+      u32x4 kb[8], vb[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 32 * (i >> 2) * kHeadDim + 32 * (i & 3));
+      const float sc = logit_scale(a, ex, a.k_scale[e]), vs = a.v_scale[e];
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 x = kb[4 * kt + j];
+          st[kt] = mfma32(codes_bf16(x[0], x[1]), q[2 * j], st[kt]);
+          st[kt] = mfma32(codes_bf16(x[2], x[3]), q[2 * j + 1], st[kt]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vb[i] = *(const u32x4*)(vc + 32 * (i >> 1) * kBlk + 32 * (i & 1));
+      weigh<2>(r, st, sc, vs, pw);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const u32x4 x = vb[2 * c + kt];
+          r.o[c] = mfma32(codes_bf16(x[0], x[1]), pw[2 * kt], r.o[c]);
+          r.o[c] = mfma32(codes_bf16(x[2], x[3]), pw[2 * kt + 1], r.o[c]);
+        }
+    } else {
+      // rows in bf16 (past the place's last: that again, masked); the values turn in LDS
+      auto at = [&](bool values, int key) {
+        return fresh_row(a, s, sg, values, min(t * kBlk + key, last));
+      };
+      uint8_t* mine = lds + wave * (kBlk * kRowBytes);
+      bool odd = false;
+#pragma unroll 2
+      for (int i = 0; i < 16; ++i) {
+        const int key = 4 * i + (lane >> 4);
+        u32x4 x = *(const u32x4*)(at(true, key) + 8 * (lane & 15));
+        odd |= take_out(x);
+        *(u32x4*)(mine + key * kRowBytes + 16 * (lane & 15)) = x;
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        const uint16_t* kr = at(false, 32 * kt + krow) + 16 * lh;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks)
+          st[kt] = mfma32(*(const u32x4*)(kr + 32 * (ks >> 1) + 8 * (ks & 1)), q[ks], st[kt]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (t * kBlk + 32 * kt + 16 * lh + i > pos) st[kt][i] = -INFINITY;
+      }
+      weigh<2>(r, st, logit_scale(a, ex, 1.f), 1.f, pw);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's rows are in LDS
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          u32x4 x;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int key = 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1) + 4 * j + ((lane >> 2) & 3);
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                mine + key * kRowBytes + 64 * c + 32 * ((lane >> 4) & 1) + 8 * (lane & 3))));
+            x[2 * j] = y[0];
+            x[2 * j + 1] = y[1];
+          }
+          r.o[c] = mfma32(x, pw[ks], r.o[c]);
+        }
+      if (__any(odd)) add_odd(r, [&](int key) { return at(true, key); }, min(kBlk, pos - t * kBlk + 1), lh);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+  }
+
+  // ---- join the waves of a row set
+  r.l = half_sum(r.l);
+  __syncthreads();
+  float* so = (float*)lds;
+  sml[wave][lr] = make_float2(r.m, r.l);
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *(f32x4*)(so + (wave * 32 + lr) * kJoin + 32 * c + 8 * i + 4 * lh) =
+          (f32x4){r.o[c][4 * i], r.o[c][4 * i + 1], r.o[c][4 * i + 2], r.o[c][4 * i + 3]};
+  __syncthreads();
+  for (int e = tid; e < rt.n_rows * (kHeadDim / 4); e += kChunkThreads) {
+    const int rr = e / (kHeadDim / 4), c = 4 * (e % (kHeadDim / 4)), w0 = rr >> 5, r32 = rr & 31;
+    float M = -INFINITY;
+    for (int w = w0; w < kWaves; w += rs) M = fmaxf(M, sml[w][r32].x);
+    const float mu = M > -INFINITY ? M : 0.f;
+    float L = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int w = w0; w < kWaves; w += rs) {
+      const float f = __builtin_amdgcn_exp2f(sml[w][r32].x - mu);
+      L = fmaf(f, sml[w][r32].y, L);
+      const f32x4 y = *(const f32x4*)(so + (w * 32 + r32) * kJoin + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
+    }
+    if (rt.whole) {
+      *(u32x2*)(out_row(a, s, sg, rt, rr) + c) = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
+    } else {
+      const int64_t slot = (int64_t)chunk_slot(part, rt.lo) * s.slot_rows + rr;
+      *(f32x4*)(s.part_o + slot * kHeadDim + c) = x;
+      if (c == 0) s.part_ml[slot] = make_float2(M, L);
+    }
+  }
+  __syncthreads();
+}
+
+// ---- many rows: eight sets of 32 rows share the key tiles, which are expanded into LDS
+struct PageRef {
+  int page;
+  float ks, vs;
+};
+constexpr int kList = kChunkThreads;   // pages looked up at once
+// two tiles of keys [64][128], then two of values (of a page [128][64], else [64][128]), bf16
+constexpr int kTileBytes = kBlk * kRowBytes;
+static_assert(4 * kTileBytes <= kLds, "");
+// 16-byte chunks of a staged row are stored at chunk ^ swizzle(row), so that the reads of
+// either product meet all banks
+__device__ __forceinline__ int swz_k(int key) { return key & 15; }
+__device__ __forceinline__ int swz_v(int key) { return ((key & 3) << 2) | ((key >> 2) & 3); }
+__device__ __forceinline__ int swz_c(int channel) { return (channel >> 1) & 7; }
+
+// Row lr of the A operand of a 32-key tile is this key of it, so that a lane's logits
+// st[kt][i] are those of keys 32 kt + 16 (i / 8) + 8 lh + i % 8.
+__device__ __forceinline__ int key_of_row(int lr) {
+  return 16 * (lr >> 4) + 8 * ((lr >> 2) & 1) + 4 * ((lr >> 3) & 1) + (lr & 3);
+}
+// st = K Q^T of a staged tile.  Operands are read three steps ahead of their products: a read
+// takes longer than the products of one step.
+__device__ __forceinline__ void wide_logits(const uint8_t* from, int kbase, const u32x4 (&q)[8], f32x16 (&st)[2]) {
+  constexpr int kAhead = 3;
+  u32x4 kk[kAhead][2];
+  auto read = [&](int ks) __attribute__((always_inline)) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+      kk[ks % kAhead][kt] = *(const u32x4*)(from + (kbase ^ (32 * ks)) + 32 * kt * kRowBytes);
+  };
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < kAhead; ++ks) read(ks);
+#pragma unroll
+  for (int ks = 0; ks < 8; ++ks) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) st[kt] = mfma32(kk[ks % kAhead][kt], q[ks], st[kt]);
+    __builtin_amdgcn_sched_barrier(0);
+    if (ks + kAhead < 8) read(ks + kAhead);
+  }
+}
+// o += V^T P^T, read(ks, x): the A operands of k-step ks.
+template <class Read>
+__device__ __forceinline__ void wide_values(Running& r, const u32x4 (&pw)[4], Read read) {
+  u32x4 vv[2][4];
+  read(0, vv[0]);
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    if (ks < 3) read(ks + 1, vv[(ks + 1) & 1]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r.o[c] = mfma32(vv[ks & 1][c], pw[ks], r.o[c]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+// The pages of tiles [lo, hi), all of whose keys every row sees.  Step e of the loop: the
+// products of the values of the tile before and of its own keys, then its weights; before
+// them the next tile's keys and its own values are expanded into the arrays that were last
+// read in the step before, and the loads of those behind them start.  One step more ends with
+// the last tile's values.
+__device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg, int lo, int hi, bool idle, int ex,
+                                           const u32x4 (&q)[8], Running& r, uint8_t* lds, PageRef* list, int* scnt) {
+  uint8_t* const sk = lds;
+  uint8_t* const sv = lds + 2 * kTileBytes;
+  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int krow = key_of_row(lr);
+  const int kbase = krow * kRowBytes + 16 * (lh ^ swz_k(krow));
+  const int vbase = lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr));
+  const int kput = (tid >> 3) * kRowBytes + 16 * ((2 * (tid & 7)) ^ swz_k(tid >> 3));
+  const int vput = (tid >> 2) * (2 * kBlk) + 16 * ((2 * (tid & 3)) ^ swz_c(tid >> 2));
+  auto load = [&](const int8_t* codes, int page) __attribute__((always_inline)) {
+    return *(const u32x4*)(codes + ((int64_t)page * a.H_kv + sg.g) * kCodes + (uint32_t)(16 * tid));
+  };
+  auto put = [&](const u32x4& x, uint8_t* to, int at) __attribute__((always_inline)) {
+    *(u32x4*)(to + at) = codes_bf16(x[0], x[1]);
+    *(u32x4*)(to + (at ^ 16)) = codes_bf16(x[2], x[3]);
+  };
+  for (int t0 = lo; t0 < hi; t0 += kList) {
+    // ---- the next pages (blocks without one are left out)
+    PageRef x = {-1, 0.f, 0.f};
+    if (t0 + tid < hi) x.page = page_of(a, sg.seq, t0 + tid);
+    if (x.page >= 0) {
+      x.ks = a.k_scale[(int64_t)x.page * a.H_kv + sg.g];
+      x.vs = a.v_scale[(int64_t)x.page * a.H_kv + sg.g];
+    }
+    const uint64_t mask = __ballot(x.page >= 0);
+    if (lane == 0) scnt[wave] = __builtin_popcountll(mask);
+    __syncthreads();
+    int at = __builtin_popcountll(mask & (((uint64_t)1 << lane) - 1)), n = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      at += w < wave ? scnt[w] : 0;
+      n += scnt[w];
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    if (x.page >= 0) list[at] = x;
+    __syncthreads();
+    if (n == 0) continue;
+
+    auto page = [&](int e) { return __builtin_amdgcn_readfirstlane(list[min(e, n - 1)].page); };
+    u32x4 kr = load(a.k_codes, page(0)), vr = load(a.v_codes, page(0));
+    put(kr, sk, kput);
+    kr = load(a.k_codes, page(1));
+    int next = page(1);
+    __syncthreads();
     f32x16 st[2];
     u32x4 pw[4];
-    // weights from the raw logits st[kt][i] of keys 32 kt + 16 lh + i: exp2(st sc - m + ve),
-    // with the sum l that leaves the values' scale 2^ve out
-    auto weights = [&](float sc, float vs) __attribute__((always_inline)) {
-      float mt = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, st[kt][i]);
-      mt = half_max(mt) * sc;
-      if (__any(mt > m + kLazy)) {
-        const float mn = fmaxf(m, mt);
-        const float al = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= al;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[c][i] *= al;
+#pragma unroll 1
+    for (int e = 0; e <= n; ++e) {
+      const int b = (e & 1) * kTileBytes, c = b ^ kTileBytes;
+      if (e < n) {   // (past the last page: that again, in arrays that are not read)
+        put(kr, sk + c, kput);
+        put(vr, sv + b, vput);
+        vr = load(a.v_codes, next);
+        next = page(e + 2);
+        kr = load(a.k_codes, next);
       }
-      const float mu = m > -INFINITY ? m : 0.f;
+      if (!idle) {
+        if (e > 0)
+          wide_values(r, pw, [&](int ks, u32x4 (&y)[4]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float e0 = __builtin_amdgcn_exp2f(fmaf(st[kt][i], sc, -mu));
-          const float e1 = __builtin_amdgcn_exp2f(fmaf(st[kt][i + 1], sc, -mu));
-          l += e0 + e1;
-          pw[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(e0 * vs, e1 * vs);
+            for (int i = 0; i < 4; ++i) y[i] = *(const u32x4*)(sv + c + (vbase ^ (32 * ks)) + i * 32 * 2 * kBlk);
+          });
+        if (e < n) {
+          wide_logits(sk + b, kbase, q, st);
+          weigh<2>(r, st, logit_scale(a, ex, list[e].ks), list[e].vs, pw);
         }
-    };
-    // row lr of an A operand is this key of 32
-    const int krow = 16 * ((lr >> 2) & 1) + 4 * (lr >> 3) + (lr & 3);
-    const int n_blk = p.held / kBlk;
+      }
+      __syncthreads();   // (the last one before the list and the arrays are written again)
+    }
+  }
+}
 
-    for (int t = lo + wave; t < hi; t += kWaves) {
-      if (t < n_blk) {
-        const int page = page_of(a, sg.seq, t);
-        if (page < 0) continue;
-        const int64_t e = (int64_t)page * a.H_kv + sg.g;
-        const int8_t* kc = a.k_codes + e * kCodes + krow * kHeadDim + 16 * lh;
-        const int8_t* vc = a.v_codes + e * kCodes + lr * kBlk + 16 * lh;
-        u32x4 kb[8], vb[8];
+// Tiles [lo, hi) of rows in bf16: the open block and the chunk.
+__device__ __forceinline__ void wide_rows(const BlockArgs& a, const ChunkStep& s, const Segment& sg, int lo, int hi,
+                                          int pos, int wpos0, int wpos1, int ex, const u32x4 (&q)[8], Running& r,
+                                          uint8_t* lds, int (*sodd)[kWaves]) {
+  uint8_t* const sk = lds;
+  uint8_t* const sv = lds + 2 * kTileBytes;
+  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int last = sg.p.held + sg.p.n - 1;            // the place's last position
+  const int krow = key_of_row(lr);
+  const int kbase = krow * kRowBytes + 16 * (lh ^ swz_k(krow));
+  int vbase[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 32 * (i >> 2) * kHeadDim + 32 * (i & 3));
-        float sc = ldexpf(a.k_scale[e] * qm, qe);
-        if (sc == INFINITY) sc = __FLT_MAX__;   // (a product of zero is a logit of zero)
-        const float vs = a.v_scale[e];
+  for (int j = 0; j < 2; ++j) {
+    const int key = 8 * lh + 4 * j + ((lane >> 2) & 3);
+    vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
+  }
+  const int fr = tid >> 4;                            // a thread has chunk tid % 16 of rows fr and fr + 32
+  const int kput = fr * kRowBytes + 16 * ((tid & 15) ^ swz_k(fr));
+  const int vput = fr * kRowBytes + 16 * ((tid & 15) ^ swz_v(fr));
+  auto load = [&](bool values, int t, u32x4 (&x)[2]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+    for (int i = 0; i < 2; ++i)
+      x[i] = *(const u32x4*)(fresh_row(a, s, sg, values, min(t * kBlk + fr + 32 * i, last)) + 8 * (tid & 15));
+  };
+  u32x4 kr[2], vr[2];
+  load(false, lo, kr);
+  load(true, lo, vr);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+  for (int i = 0; i < 2; ++i) *(u32x4*)(sk + kput + 32 * i * kRowBytes) = kr[i];
+  load(false, min(lo + 1, hi - 1), kr);
+  __syncthreads();
+  f32x16 st[2];
+  u32x4 pw[4];
+  bool mine = false;             // the wave has rows that see keys of the tile before
+#pragma unroll 1
+  for (int t = lo; t <= hi; ++t) {
+    const int p = (t - lo) & 1, b = p * kTileBytes, c = b ^ kTileBytes;
+    if (t < hi) {
+      bool odd = false;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const u32x4 x = kb[4 * kt + j];
-            st[kt] = mfma32(codes_bf16(x[0], x[1]), q[2 * j], st[kt]);
-            st[kt] = mfma32(codes_bf16(x[2], x[3]), q[2 * j + 1], st[kt]);
-          }
+      for (int i = 0; i < 2; ++i) {
+        *(u32x4*)(sk + c + kput + 32 * i * kRowBytes) = kr[i];
+        odd |= take_out(vr[i]);
+        *(u32x4*)(sv + b + vput + 32 * i * kRowBytes) = vr[i];
+      }
+      const int any = __any(odd);
+      if (lane == 0) sodd[p][wave] = any;
+      load(true, min(t + 1, hi - 1), vr);
+      load(false, min(t + 2, hi - 1), kr);
+    }
+    if (mine) {
+      wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                        sv + c + (vbase[0] ^ (64 * i)) + 16 * ks * kRowBytes)));
+          const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                        sv + c + (vbase[1] ^ (64 * i)) + 16 * ks * kRowBytes)));
+          x[i] = (u32x4){y[0], y[1], z[0], z[1]};
         }
+      });
+      int odd = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) vb[i] = *(const u32x4*)(vc + 32 * (i >> 1) * kBlk + 32 * (i & 1));
-        weights(sc, vs);
+      for (int w = 0; w < kWaves; ++w) odd |= sodd[p ^ 1][w];
+      if (__builtin_amdgcn_readfirstlane(odd))
+        add_odd(r, [&](int key) { return fresh_row(a, s, sg, true, (t - 1) * kBlk + key); },
+                min(kBlk, pos - (t - 1) * kBlk + 1), lh);
+    }
+    mine = t < hi && t * kBlk <= wpos1;
+    if (mine) {
+      wide_logits(sk + b, kbase, q, st);
+      if (t * kBlk + kBlk - 1 > wpos0) {
+        const int rel = pos - t * kBlk - 8 * lh;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int kt = 0; kt < 2; ++kt) {
-            const u32x4 x = vb[2 * c + kt];
-            o[c] = mfma32(codes_bf16(x[0], x[1]), pw[2 * kt], o[c]);
-            o[c] = mfma32(codes_bf16(x[2], x[3]), pw[2 * kt + 1], o[c]);
-          }
-      } else {
-        // rows in bf16: positions of the open block, then of the chunk (past the last: the
-        // last again, masked)
-        const int64_t tail = ((int64_t)sg.seq * a.H_kv + sg.g) * kCodes;
-        auto k_row = [&](int key) -> const uint16_t* {
-          const int pp = min(t * kBlk + key, last);
-          return pp < p.held ? a.k_tail + tail + (pp % kBlk) * kHeadDim
-                             : s.k + (sg.start + (pp - p.held)) * s.k_st + sg.g * s.k_sh;
-        };
-        auto v_row = [&](int key) -> const uint16_t* {
-          const int pp = min(t * kBlk + key, last);
-          return pp < p.held ? a.v_tail + tail + (pp % kBlk) * kHeadDim
-                             : s.v + (sg.start + (pp - p.held)) * s.v_st + sg.g * s.v_sh;
-        };
-        uint8_t* mine = lds + wave * (kBlk * kRowBytes);
-        bool odd = false;
-#pragma unroll 2
-        for (int i = 0; i < 16; ++i) {
-          const int key = 4 * i + (lane >> 4);
-          u32x4 x = *(const u32x4*)(v_row(key) + 8 * (lane & 15));
-          // a masked key's value must not reach a row through 0 * infinity: values that are
-          // not finite are left out here and added below to the rows that see them
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (nonfinite(x[j])) {
-              odd = true;
-              if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
-              if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
-            }
-          }
-          *(u32x4*)(mine + key * kRowBytes + 16 * (lane & 15)) = x;
-        }
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const uint16_t* kr = k_row(32 * kt + krow) + 16 * lh;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
-#pragma unroll
-          for (int ks = 0; ks < 8; ++ks)
-            st[kt] = mfma32(*(const u32x4*)(kr + 32 * (ks >> 1) + 8 * (ks & 1)), q[ks], st[kt]);
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            if (t * kBlk + 32 * kt + 16 * lh + i > pos) st[kt][i] = -INFINITY;
-        }
-        float sc = ldexpf(qm, qe);
-        if (sc == INFINITY) sc = __FLT_MAX__;
-        weights(sc, 1.f);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's rows are in LDS
-#pragma unroll
-        for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            u32x4 x;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int key = 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1) + 4 * j + ((lane >> 2) & 3);
-              const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                  mine + key * kRowBytes + 64 * c + 32 * ((lane >> 4) & 1) + 8 * (lane & 3))));
-              x[2 * j] = y[0];
-              x[2 * j + 1] = y[1];
-            }
-            o[c] = mfma32(x, pw[ks], o[c]);
-          }
-        if (__any(odd)) {
-          for (int key = 0; key < kBlk && t * kBlk + key <= pos; ++key) {
-            const uint16_t* vr = v_row(key) + 4 * lh;
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const uint16_t x = vr[32 * c + 8 * (i >> 2) + (i & 3)];
-                if ((x & 0x7F80u) == 0x7F80u) o[c][i] += bf16_to_f32(x);
-              }
-          }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) st[kt][i] = -INFINITY;
       }
+      weigh<2>(r, st, logit_scale(a, ex, 1.f), 1.f, pw);
     }
-
-    // ---- join the waves; o[c][i]: channel 32 c + 8 (i / 4) + 4 lh + i % 4 of row lr
-    l = half_sum(l);
     __syncthreads();
-    float* so = (float*)lds;
-    sml[wave][lr] = make_float2(m, l);
+  }
+}
+
+__device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
+                                            const RowTile& rt, int part, uint8_t* lds, PageRef* list,
+                                            int (*sodd)[kWaves], int* scnt) {
+  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int row = wave * 32 + lr, rowc = min(row, rt.n_rows - 1), i_row = rt.pos0 + rowc / a.gqa;
+  const bool idle = wave * 32 >= rt.n_rows;
+  u32x4 q[8];
+  const int ex = load_query<true>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + rowc % a.gqa) * s.q_sh, lh, q);
+  Running r;
+  clear(r);
+  const int n_blk = sg.p.held / kBlk;
+  if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, ex, q, r, lds, list, scnt);
+  if (rt.hi > n_blk) {
+    // first and last position of the wave's rows
+    const int wpos0 = sg.p.held + rt.pos0 + wave * 32 / a.gqa;
+    const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + min(wave * 32 + 31, rt.n_rows - 1) / a.gqa;
+    wide_rows(a, s, sg, max(rt.lo, n_blk), rt.hi, sg.p.held + i_row, wpos0, wpos1, ex, q, r, lds, sodd);
+  }
+
+  r.l = half_sum(r.l);
+  if (rt.whole) {
+    const float inv = 1.f / r.l;
+    uint16_t* op = out_row(a, s, sg, rt, rowc) + 8 * lh;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {   // channels 8 e .. 8 e + 15: eight to each lane half
+        uint32_t y[2], z[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const auto sw = __builtin_amdgcn_permlane32_swap(
+              pack_bf16(r.o[c][4 * e + 2 * j] * inv, r.o[c][4 * e + 2 * j + 1] * inv),
+              pack_bf16(r.o[c][4 * e + 4 + 2 * j] * inv, r.o[c][4 * e + 5 + 2 * j] * inv), false, false);
+          y[j] = sw[0];
+          z[j] = sw[1];
+        }
+        if (row < rt.n_rows) *(u32x4*)(op + 32 * c + 8 * e) = (u32x4){y[0], y[1], z[0], z[1]};
+      }
+  } else if (row < rt.n_rows) {
+    const int64_t slot = (int64_t)chunk_slot(part, rt.lo) * s.slot_rows + row;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *(f32x4*)(so + (wave * 32 + lr) * kJoin + 32 * c + 8 * i + 4 * lh) =
-            (f32x4){o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]};
-    __syncthreads();
-    const bool whole = lo == 0 && hi == v_all;
-    for (int e = tid; e < n_rows * (kHeadDim / 4); e += kChunkThreads) {
-      const int r = e / (kHeadDim / 4), c = 4 * (e % (kHeadDim / 4));
-      float M = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) M = fmaxf(M, sml[w][r].x);
-      const float mu = M > -INFINITY ? M : 0.f;
-      float L = 0.f;
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(sml[w][r].x - mu);
-        L = fmaf(f, sml[w][r].y, L);
-        const f32x4 y = *(const f32x4*)(so + (w * 32 + r) * kJoin + c);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
-      }
-      if (whole) {
-        uint16_t* op = s.out + (sg.start + pos0 + r / a.gqa) * s.o_st + (sg.g * a.gqa + r % a.gqa) * s.o_sh + c;
-        *(u32x2*)op = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
-      } else {
-        const int64_t slot = (int64_t)chunk_slot(part, lo) * s.slot_rows + r;
-        *(f32x4*)(s.part_o + slot * kHeadDim + c) = x;
-        if (c == 0) s.part_ml[slot] = make_float2(M, L);
-      }
-    }
-    __syncthreads();
-  };
-  walk(a, begin, end, s, lp, segment);
+        *(f32x4*)(s.part_o + slot * kHeadDim + 32 * c + 8 * i + 4 * lh) =
+            (f32x4){r.o[c][4 * i], r.o[c][4 * i + 1], r.o[c][4 * i + 2], r.o[c][4 * i + 3]};
+    if (lh == 0) s.part_ml[slot] = make_float2(r.m, r.l);
+  }
+}
+}  // namespace
+
+__global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, ChunkStep s) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
+  __shared__ float2 sml[kWaves][32];
+  __shared__ PageRef list[kList];
+  __shared__ int sodd[2][kWaves], scnt[kWaves];
+  __shared__ LinePlaces lp;
+  // parts of one KV head on one XCD (workgroup i runs on XCD i % 8)
+  const int part = (blockIdx.x & 7) * (kChunkParts / 8) + (blockIdx.x >> 3);
+  const int64_t total = line_total(a, s, lp), size = lane_of(chunk_part(total), 0);
+  const int64_t begin = part * size, end = min(begin + size, total);
+  walk(a, begin, end, s, lp, [&](const Segment& sg) {
+    RowTile rt;
+    rt.lo = chunk_key_tile(sg.from);
+    rt.hi = chunk_key_tile(sg.to);
+    if (rt.lo >= rt.hi) return;
+    rt.pos0 = sg.tile * sg.p.per;
+    rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
+    rt.whole = rt.lo == 0 && rt.hi == chunk_key_tiles(sg.p, sg.tile);
+    if (sg.p.rows < 256) attend_few(a, s, sg, rt, part, lds, sml);
+    else attend_many(a, s, sg, rt, part, lds, list, sodd, scnt);
+  });
 }
 
 // Joins the row tiles that more than one part served: workgroup (w, r) takes rows 8 r .. + 7

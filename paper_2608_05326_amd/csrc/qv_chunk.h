@@ -17,7 +17,7 @@ constexpr int kChunkCost = 128;     // keys
 constexpr int kChunkMin = 128;      // the least a part is, in keys
 
 // Rows of a workgroup for a place with this many in all.
-QV_HD int chunk_rows(int64_t rows) { return rows > 0 ? 32 : 32; }
+QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 
 struct ChunkPlace {
   int held, n;        // tokens held, new tokens (0: none)
