@@ -310,93 +310,122 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + row % a.gqa) * s.q_sh, lh, q);
   Running r;
   clear(r);
-  f32x16 st[2];
-  u32x4 pw[4];
-  // row lr of an A operand is this key of 32; a lane's logits st[kt][i] are those of keys
-  // 32 kt + 16 lh + i
+  // row lr of an A operand is this key of 32; a lane's logits st[i] are those of keys 16 lh + i
   const int krow = 16 * ((lr >> 2) & 1) + 4 * (lr >> 3) + (lr & 3);
   const int n_blk = sg.p.held / kBlk;
 
-  for (int t = rw * 32 < rt.n_rows ? rt.lo + kg : rt.hi; t < rt.hi; t += n_kg) {
-    if (t < n_blk) {
-      const int page = page_of(a, sg.seq, t);
-      if (page < 0) continue;
-      const int64_t e = (int64_t)page * a.H_kv + sg.g;
-      const int8_t* kc = a.k_codes + e * kCodes + krow * kHeadDim + 16 * lh;
-      const int8_t* vc = a.v_codes + e * kCodes + lr * kBlk + 16 * lh;
-      u32x4 kb[8], vb[8];
+  const bool idle = rw * 32 >= rt.n_rows;
+  const int page_end = idle ? 0 : min(rt.hi, n_blk);
+  for (int t0 = rt.lo + kg; t0 < page_end; t0 += 64 * n_kg) {
+    // pages and scales of the wave's next 64 blocks, one per lane (dropped blocks are left out)
+    int page = -1;
+    float ks_l = 0.f, vs_l = 0.f;
+    if (t0 + lane * n_kg < page_end) page = page_of(a, sg.seq, t0 + lane * n_kg);
+    uint64_t live = __ballot(page >= 0);
+    if (!live) continue;
+    if (page >= 0) {
+      ks_l = a.k_scale[(int64_t)page * a.H_kv + sg.g];
+      vs_l = a.v_scale[(int64_t)page * a.H_kv + sg.g];
+    }
+    // codes of 32 keys and their values, reloaded as soon as they are used: a page ahead
+    u32x4 kb[2][4], vb[2][4];
+    auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + sg.g) * kCodes; };
+    auto load_k = [&](int64_t e, int kt) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) kb[i] = *(const u32x4*)(kc + 32 * (i >> 2) * kHeadDim + 32 * (i & 3));
-      const float sc = logit_scale(a, ex, a.k_scale[e]), vs = a.v_scale[e];
+      for (int i = 0; i < 4; ++i)
+        kb[kt][i] = *(const u32x4*)(a.k_codes + e + (uint32_t)(krow * kHeadDim + 16 * lh + 32 * kt * kHeadDim + 32 * i));
+    };
+    auto load_v = [&](int64_t e, int kt) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        vb[kt][i] = *(const u32x4*)(a.v_codes + e + (uint32_t)(lr * kBlk + 16 * lh + 32 * i * kBlk + 32 * kt));
+    };
+    int64_t e = entry(__builtin_ctzll(live));
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      load_k(e, kt);
+      load_v(e, kt);
+    }
+    while (live) {
+      const int j = __builtin_ctzll(live);
+      live &= live - 1;
+      const float sc = logit_scale(a, ex, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)));
+      const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
+      e = entry(live ? __builtin_ctzll(live) : j);   // (after the last: that again)
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt) {
+        f32x16 st[1];
+        u32x4 pw[2];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+        for (int i = 0; i < 16; ++i) st[0][i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x4 x = kb[4 * kt + j];
-          st[kt] = mfma32(codes_bf16(x[0], x[1]), q[2 * j], st[kt]);
-          st[kt] = mfma32(codes_bf16(x[2], x[3]), q[2 * j + 1], st[kt]);
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 x = kb[kt][i];
+          st[0] = mfma32(codes_bf16(x[0], x[1]), q[2 * i], st[0]);
+          st[0] = mfma32(codes_bf16(x[2], x[3]), q[2 * i + 1], st[0]);
         }
+        load_k(e, kt);
+        weigh<1>(r, st, sc, vs, pw);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const u32x4 x = vb[kt][c];
+          r.o[c] = mfma32(codes_bf16(x[0], x[1]), pw[0], r.o[c]);
+          r.o[c] = mfma32(codes_bf16(x[2], x[3]), pw[1], r.o[c]);
+        }
+        load_v(e, kt);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) vb[i] = *(const u32x4*)(vc + 32 * (i >> 1) * kBlk + 32 * (i & 1));
-      weigh<2>(r, st, sc, vs, pw);
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          const u32x4 x = vb[2 * c + kt];
-          r.o[c] = mfma32(codes_bf16(x[0], x[1]), pw[2 * kt], r.o[c]);
-          r.o[c] = mfma32(codes_bf16(x[2], x[3]), pw[2 * kt + 1], r.o[c]);
-        }
-    } else {
-      // rows in bf16 (past the place's last: that again, masked); the values turn in LDS
-      auto at = [&](bool values, int key) {
-        return fresh_row(a, s, sg, values, min(t * kBlk + key, last));
-      };
+    }
+  }
+
+  // tiles of rows in bf16, 32 keys at a time (keys past the place's last are that again, and
+  // masked); the values turn in LDS
+  const int first = max(rt.lo, n_blk), skip = (first - rt.lo) % n_kg;
+  for (int t = first + (kg >= skip ? kg - skip : kg - skip + n_kg); !idle && t < rt.hi; t += n_kg)
+#pragma unroll 1
+    for (int k0 = t * kBlk; k0 < t * kBlk + kBlk && k0 <= last; k0 += 32) {
+      auto at = [&](bool values, int key) { return fresh_row(a, s, sg, values, min(k0 + key, last)); };
       uint8_t* mine = lds + wave * (kBlk * kRowBytes);
+      u32x4 vb[8], kb[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vb[i] = *(const u32x4*)(at(true, 4 * i + (lane >> 4)) + 8 * (lane & 15));
+      const uint16_t* kr = at(false, krow) + 16 * lh;
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) kb[ks] = *(const u32x4*)(kr + 32 * (ks >> 1) + 8 * (ks & 1));
       bool odd = false;
-#pragma unroll 2
-      for (int i = 0; i < 16; ++i) {
-        const int key = 4 * i + (lane >> 4);
-        u32x4 x = *(const u32x4*)(at(true, key) + 8 * (lane & 15));
-        odd |= take_out(x);
-        *(u32x4*)(mine + key * kRowBytes + 16 * (lane & 15)) = x;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        odd |= take_out(vb[i]);
+        *(u32x4*)(mine + (4 * i + (lane >> 4)) * kRowBytes + 16 * (lane & 15)) = vb[i];
       }
+      f32x16 sr[1];
+      u32x4 pr[2];
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        const uint16_t* kr = at(false, 32 * kt + krow) + 16 * lh;
+      for (int i = 0; i < 16; ++i) sr[0][i] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+      for (int ks = 0; ks < 8; ++ks) sr[0] = mfma32(kb[ks], q[ks], sr[0]);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks)
-          st[kt] = mfma32(*(const u32x4*)(kr + 32 * (ks >> 1) + 8 * (ks & 1)), q[ks], st[kt]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t * kBlk + 32 * kt + 16 * lh + i > pos) st[kt][i] = -INFINITY;
-      }
-      weigh<2>(r, st, logit_scale(a, ex, 1.f), 1.f, pw);
+      for (int i = 0; i < 16; ++i)
+        if (k0 + 16 * lh + i > pos) sr[0][i] = -INFINITY;
+      weigh<1>(r, sr, logit_scale(a, ex, 1.f), 1.f, pr);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's rows are in LDS
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+      for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           u32x4 x;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const int key = 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1) + 4 * j + ((lane >> 2) & 3);
+            const int key = 16 * lh + 8 * ks + 4 * j + ((lane >> 2) & 3);
             const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
                 mine + key * kRowBytes + 64 * c + 32 * ((lane >> 4) & 1) + 8 * (lane & 3))));
             x[2 * j] = y[0];
             x[2 * j + 1] = y[1];
           }
-          r.o[c] = mfma32(x, pw[ks], r.o[c]);
+          r.o[c] = mfma32(x, pr[ks], r.o[c]);
         }
-      if (__any(odd)) add_odd(r, [&](int key) { return at(true, key); }, min(kBlk, pos - t * kBlk + 1), lh);
+      if (__any(odd)) add_odd(r, [&](int key) { return at(true, key); }, min(32, pos - k0 + 1), lh);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-  }
 
   // ---- join the waves of a row set
   r.l = half_sum(r.l);
