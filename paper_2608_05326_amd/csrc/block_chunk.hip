@@ -577,15 +577,25 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
     __syncthreads();
     f32x16 st[2];
     u32x4 pw[4];
+    // The waves of a SIMD (w and w + 4) are half a step apart: while one has products, the
+    // other has weights and codes.
+    const bool ahead = wave < kWaves / 2;
+    auto weights = [&](int e) __attribute__((always_inline)) {
+      if (!idle) weigh<2>(r, st, logit_scale(a, ex, list[e].ks), list[e].vs, pw);
+    };
+    auto stage = [&](int e, uint8_t* k_to, uint8_t* v_to) __attribute__((always_inline)) {
+      put(kr, k_to, kput);     // (past the last page: that again, in arrays that are not read)
+      put(vr, v_to, vput);
+      vr = load(a.v_codes, next);
+      next = page(e + 2);
+      kr = load(a.k_codes, next);
+    };
 #pragma unroll 1
     for (int e = 0; e <= n; ++e) {
       const int b = (e & 1) * kTileBytes, c = b ^ kTileBytes;
-      if (e < n) {   // (past the last page: that again, in arrays that are not read)
-        put(kr, sk + c, kput);
-        put(vr, sv + b, vput);
-        vr = load(a.v_codes, next);
-        next = page(e + 2);
-        kr = load(a.k_codes, next);
+      if (!ahead) {
+        if (e > 0) weights(e - 1);
+        if (e < n) stage(e, sk + c, sv + b);
       }
       if (!idle) {
         if (e > 0)
@@ -593,10 +603,11 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = *(const u32x4*)(sv + c + (vbase ^ (32 * ks)) + i * 32 * 2 * kBlk);
           });
-        if (e < n) {
-          wide_logits(sk + b, kbase, q, st);
-          weigh<2>(r, st, logit_scale(a, ex, list[e].ks), list[e].vs, pw);
-        }
+        if (e < n) wide_logits(sk + b, kbase, q, st);
+      }
+      if (ahead && e < n) {
+        weights(e);
+        stage(e, sk + c, sv + b);
       }
       __syncthreads();   // (the last one before the list and the arrays are written again)
     }
