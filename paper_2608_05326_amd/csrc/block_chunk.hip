@@ -59,6 +59,14 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w0, uint32_t w1) {
   return (u32x4){a[0], a[1], b[0], b[1]};
 }
 
+// threadIdx.x, not to be seen through: what is derived from it is computed where it is used
+// (hoisted out of the walk over segments, it would fill the registers that the products need).
+__device__ __forceinline__ int thread_here() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 // The place in lane, with its length on the line.
 __device__ __forceinline__ ChunkPlace lane_place(const BlockArgs& a, const ChunkStep& s, int place, int* start) {
   const int i = min(place, a.B - 1);
@@ -67,11 +75,12 @@ __device__ __forceinline__ ChunkPlace lane_place(const BlockArgs& a, const Chunk
   return chunk_place(place < a.B ? a.lens[i] : -1, e - b, a.gqa, a.max_context);
 }
 __device__ __forceinline__ int64_t wave_scan(int64_t x) {   // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
+  const int lane = thread_here() & 63;
+#pragma unroll 1
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
+    const uint32_t lo = __builtin_amdgcn_ds_bpermute(4 * (lane - d), (int)x);
+    const int hi = __builtin_amdgcn_ds_bpermute(4 * (lane - d), (int)(x >> 32));
+    if (lane >= d) x += (int64_t)((uint64_t)lo | (uint64_t)(uint32_t)hi << 32);
   }
   return x;
 }
@@ -95,7 +104,7 @@ struct LinePlaces {
 };
 __device__ __forceinline__ void put_places(const BlockArgs& a, const ChunkStep& s, int s0, int64_t base,
                                            LinePlaces& lp) {
-  const int lane = threadIdx.x & 63;
+  const int lane = thread_here() & 63;
   int start;
   const ChunkPlace p = lane_place(a, s, s0 + lane, &start);
   lp.incl[lane] = base + wave_scan(chunk_pair_cost(p) * a.H_kv);
@@ -106,18 +115,17 @@ __device__ __forceinline__ void put_places(const BlockArgs& a, const ChunkStep& 
 template <class F>
 __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end, const ChunkStep& s, LinePlaces& lp,
                                      F&& f) {
-  const int lane = threadIdx.x & 63;
   int64_t base = 0;
   for (int s0 = 0; x < end; s0 += 64) {
     if (s0) {   // (the first 64 are there)
       if (s0 >= a.B) return;
       __syncthreads();
-      if (threadIdx.x < 64) put_places(a, s, s0, base, lp);
+      if (thread_here() < 64) put_places(a, s, s0, base, lp);
       __syncthreads();
     }
     base = lane_of(lp.incl[63], 0);
     while (x < end && x < base) {
-      const int w = __builtin_ctzll(__ballot(lp.incl[lane] > x));
+      const int w = __builtin_ctzll(__ballot(lp.incl[thread_here() & 63] > x));
       Segment g;
       g.seq = s0 + w;
       g.start = __builtin_amdgcn_readfirstlane(lp.start[w]);
@@ -127,7 +135,7 @@ __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end,
       g.p.tiles = __builtin_amdgcn_readfirstlane(g.p.tiles);
       const int64_t pair = chunk_pair_cost(g.p), last = lane_of(lp.incl[w], 0);
       const int64_t first = last - pair * a.H_kv;
-      for (g.g = __builtin_amdgcn_readfirstlane((int)((x - first) / pair)); g.g < a.H_kv && x < end; ++g.g) {
+      for (g.g = __builtin_amdgcn_readfirstlane(chunk_quotient(x - first, pair)); g.g < a.H_kv && x < end; ++g.g) {
         const int64_t at = first + g.g * pair;
         for (g.tile = __builtin_amdgcn_readfirstlane(chunk_tile_at(g.p, x - at)); g.tile < g.p.tiles && x < end; ++g.tile) {
           g.at = at + chunk_before(g.p, g.tile);
@@ -157,14 +165,6 @@ __device__ __forceinline__ int64_t line_total(const BlockArgs& a, const ChunkSte
   return total;
 }
 
-// threadIdx.x, not to be seen through: what is derived from it is computed where it is used
-// (hoisted out of the walk over segments, it would fill the registers that the products need).
-__device__ __forceinline__ int thread_here() {
-  int t = threadIdx.x;
-  asm volatile("" : "+v"(t));
-  return t;
-}
-
 // What a row tile's workgroup needs of a segment, beside the segment.
 struct RowTile {
   int lo, hi;                // its tiles of 64 keys
@@ -184,7 +184,9 @@ __device__ __forceinline__ int load_query(const uint16_t* p, int lh, u32x4 (&q)[
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) am = amax_pair(q[ks], am);
   am = amax_bits(am);
-  am = max(am, (uint32_t)__shfl_xor((int)am, 32, 64));
+  const auto swapped = __builtin_amdgcn_permlane32_swap(am, am, false, false);
+  const uint32_t am0 = swapped[0], am1 = swapped[1];
+  am = max(am0, am1);
   const int ex = max((int)(am >> 23), 1) - 127;    // (a row of subnormals keeps its scale)
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks)
@@ -291,14 +293,26 @@ __device__ __forceinline__ uint16_t* out_row(const BlockArgs& a, const ChunkStep
   return s.out + (sg.start + rt.pos0 + row / a.gqa) * s.o_st + (sg.g * a.gqa + row % a.gqa) * s.o_sh;
 }
 
-// Bytes between the rows of a wave's staged values, and of joined outputs (floats).
-constexpr int kJoin = kHeadDim + 4;
-constexpr int kLds = std::max(kWaves * kBlk * kRowBytes, kWaves * 32 * kJoin * (int)sizeof(float));
+// LDS of a workgroup, in two arrays: reads of one do not wait for the loads on their way into
+// the other (the compiler tells arrays apart, not parts of one).
+constexpr int kLds = 64 * 1024;
+struct Shared {
+  uint8_t* k;
+  uint8_t* v;
+};
+// A wave's output rows for the join, 16 KB: 16-byte chunk c of row r.
+__device__ __forceinline__ float* join_at(const Shared& sm, int wave, int r, int c) {
+  return (float*)((wave < 4 ? sm.k : sm.v) + (wave & 3) * 16384 + r * 512 + 16 * (c ^ r));
+}
+// 16 bytes a lane from global memory to LDS, in lane order from an address that is uniform
+__device__ __forceinline__ void dma16(const void* g, uint8_t* to) {
+  __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
 
 // ---- few rows: RS sets of 32 rows, the other waves of a set take the key tiles in turn,
 // pages straight into registers
 __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
-                                           const RowTile& rt, int part, uint8_t* lds, float2 (*sml)[32]) {
+                                           const RowTile& rt, int part, const Shared& sm, float2 (*sml)[32]) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int rs = sg.p.rows >> 5;                      // 1, 2 or 4
@@ -306,75 +320,102 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   const int row = min(rw * 32 + lr, rt.n_rows - 1), i_row = rt.pos0 + row / a.gqa;
   const int pos = sg.p.held + i_row;                  // this lane's position
   const int last = sg.p.held + sg.p.n - 1;            // the place's last position
+  const int n_blk = sg.p.held / kBlk, page_end = rw * 32 < rt.n_rows ? min(rt.hi, n_blk) : 0;
+  // page (-1: none) of block t0 + n_kg lane; the first look-up goes before the query's loads
+  auto page_at = [&](int t0) { return t0 + lane * n_kg < page_end ? page_of(a, sg.seq, t0 + lane * n_kg) : -1; };
+  int page = page_at(rt.lo + kg);
   u32x4 q[8];
   const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + row % a.gqa) * s.q_sh, lh, q);
   Running r;
   clear(r);
   // row lr of an A operand is this key of 32; a lane's logits st[i] are those of keys 16 lh + i
   const int krow = 16 * ((lr >> 2) & 1) + 4 * (lr >> 3) + (lr & 3);
-  const int n_blk = sg.p.held / kBlk;
 
   const bool idle = rw * 32 >= rt.n_rows;
-  const int page_end = idle ? 0 : min(rt.hi, n_blk);
+  uint8_t* const sk = sm.k + wave * kCodes;   // a page's keys [64][128] and values [128][64], codes
+  uint8_t* const sv = sm.v + wave * kCodes;
+  // A wave's load of 1 KB fills LDS in lane order.  16-byte chunks of a row are swizzled
+  // through the address that a lane fetches, so that the reads below meet all banks: chunk c
+  // of key t is at c ^ ((t / 2) % 4 + 4 ((t / 16) % 2)), of channel h at c ^ ((h / 4) % 4).
+  const uint32_t k_from = (lane >> 3) * kHeadDim + 16 * ((lane & 7) ^ ((lane >> 4) & 3));
+  const uint32_t v_from = (lane >> 2) * kBlk + 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+  const int k_at = krow * kHeadDim + 16 * (lh ^ (((krow >> 1) & 3) | ((krow >> 4) & 1) << 2));
+  const int v_at = lr * kBlk + 16 * (lh ^ ((lr >> 2) & 3));
   for (int t0 = rt.lo + kg; t0 < page_end; t0 += 64 * n_kg) {
     // pages and scales of the wave's next 64 blocks, one per lane (dropped blocks are left out)
-    int page = -1;
+    if (t0 != rt.lo + kg) page = page_at(t0);
     float ks_l = 0.f, vs_l = 0.f;
-    if (t0 + lane * n_kg < page_end) page = page_of(a, sg.seq, t0 + lane * n_kg);
     uint64_t live = __ballot(page >= 0);
     if (!live) continue;
     if (page >= 0) {
       ks_l = a.k_scale[(int64_t)page * a.H_kv + sg.g];
       vs_l = a.v_scale[(int64_t)page * a.H_kv + sg.g];
     }
-    // codes of 32 keys and their values, reloaded as soon as they are used: a page ahead
-    u32x4 kb[2][4], vb[2][4];
     auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + sg.g) * kCodes; };
-    auto load_k = [&](int64_t e, int kt) __attribute__((always_inline)) {
+    auto load_k = [&](int64_t e) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        kb[kt][i] = *(const u32x4*)(a.k_codes + e + (uint32_t)(krow * kHeadDim + 16 * lh + 32 * kt * kHeadDim + 32 * i));
+      for (int i = 0; i < 8; ++i)
+        dma16(a.k_codes + e + (i & 2 ? k_from ^ 64 : k_from) + 1024 * i, sk + 1024 * i);
     };
-    auto load_v = [&](int64_t e, int kt) __attribute__((always_inline)) {
+    auto load_v = [&](int64_t e) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        vb[kt][i] = *(const u32x4*)(a.v_codes + e + (uint32_t)(lr * kBlk + 16 * lh + 32 * i * kBlk + 32 * kt));
+      for (int i = 0; i < 8; ++i) dma16(a.v_codes + e + v_from + 1024 * i, sv + 1024 * i);
     };
     int64_t e = entry(__builtin_ctzll(live));
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-      load_k(e, kt);
-      load_v(e, kt);
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (the scales: the waits below count the pages' loads)
+    load_k(e);
+    load_v(e);
     while (live) {
       const int j = __builtin_ctzll(live);
       live &= live - 1;
+      e = entry(live ? __builtin_ctzll(live) : j);     // (after the last: that again)
       const float sc = logit_scale(a, ex, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)));
       const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
-      e = entry(live ? __builtin_ctzll(live) : j);   // (after the last: that again)
+      f32x16 st[2];
+      u32x4 pw[4];
+      {
+        u32x4 kb[2][4];
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the keys are there, the values on their way
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-        f32x16 st[1];
-        u32x4 pw[2];
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[0][i] = 0.f;
+          for (int kt = 0; kt < 2; ++kt)
+            kb[kt][i] = *(const u32x4*)(sk + (k_at ^ (32 * i)) + 32 * kt * kHeadDim);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before they are overwritten
+        load_k(e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32x4 x = kb[kt][i];
-          st[0] = mfma32(codes_bf16(x[0], x[1]), q[2 * i], st[0]);
-          st[0] = mfma32(codes_bf16(x[2], x[3]), q[2 * i + 1], st[0]);
-        }
-        load_k(e, kt);
-        weigh<1>(r, st, sc, vs, pw);
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const u32x4 x = vb[kt][c];
-          r.o[c] = mfma32(codes_bf16(x[0], x[1]), pw[0], r.o[c]);
-          r.o[c] = mfma32(codes_bf16(x[2], x[3]), pw[1], r.o[c]);
-        }
-        load_v(e, kt);
+          for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int b = 0; b < 4; b += 2)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+              st[kt] = mfma32(codes_bf16(kb[kt][i][b], kb[kt][i][b + 1]), q[2 * i + b / 2], st[kt]);
+      }
+      weigh<2>(r, st, sc, vs, pw);
+      {
+        u32x4 vb[2][4];
+        asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            vb[kt][c] = *(const u32x4*)(sv + (v_at ^ (32 * kt)) + 32 * c * kBlk);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        load_v(e);
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int b = 0; b < 4; b += 2)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              r.o[c] = mfma32(codes_bf16(vb[kt][c][b], vb[kt][c][b + 1]), pw[2 * kt + b / 2], r.o[c]);
       }
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 
   // tiles of rows in bf16, 32 keys at a time (keys past the place's last are that again, and
@@ -384,7 +425,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
 #pragma unroll 1
     for (int k0 = t * kBlk; k0 < t * kBlk + kBlk && k0 <= last; k0 += 32) {
       auto at = [&](bool values, int key) { return fresh_row(a, s, sg, values, min(k0 + key, last)); };
-      uint8_t* mine = lds + wave * (kBlk * kRowBytes);
+      uint8_t* mine = sv;   // 32 rows of 256 bytes
       u32x4 vb[8], kb[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) vb[i] = *(const u32x4*)(at(true, 4 * i + (lane >> 4)) + 8 * (lane & 15));
@@ -430,13 +471,12 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   // ---- join the waves of a row set
   r.l = half_sum(r.l);
   __syncthreads();
-  float* so = (float*)lds;
   sml[wave][lr] = make_float2(r.m, r.l);
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *(f32x4*)(so + (wave * 32 + lr) * kJoin + 32 * c + 8 * i + 4 * lh) =
+      *(f32x4*)join_at(sm, wave, lr, 8 * c + 2 * i + lh) =
           (f32x4){r.o[c][4 * i], r.o[c][4 * i + 1], r.o[c][4 * i + 2], r.o[c][4 * i + 3]};
   __syncthreads();
   for (int e = tid; e < rt.n_rows * (kHeadDim / 4); e += kChunkThreads) {
@@ -449,7 +489,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
     for (int w = w0; w < kWaves; w += rs) {
       const float f = __builtin_amdgcn_exp2f(sml[w][r32].x - mu);
       L = fmaf(f, sml[w][r32].y, L);
-      const f32x4 y = *(const f32x4*)(so + (w * 32 + r32) * kJoin + c);
+      const f32x4 y = *(const f32x4*)join_at(sm, w, r32, c / 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
     }
@@ -470,9 +510,9 @@ struct PageRef {
   float ks, vs;
 };
 constexpr int kList = kChunkThreads;   // pages looked up at once
-// two tiles of keys [64][128], then two of values (of a page [128][64], else [64][128]), bf16
+// bytes of a tile's keys [64][128] or values (of a page [128][64], else [64][128]), bf16
 constexpr int kTileBytes = kBlk * kRowBytes;
-static_assert(4 * kTileBytes <= kLds, "");
+static_assert(2 * kTileBytes <= kLds && kWaves * kCodes <= kLds && 4 * 16384 <= kLds, "LDS");
 // 16-byte chunks of a staged row are stored at chunk ^ swizzle(row), so that the reads of
 // either product meet all banks
 __device__ __forceinline__ int swz_k(int key) { return key & 15; }
@@ -524,29 +564,97 @@ __device__ __forceinline__ void wide_values(Running& r, const u32x4 (&pw)[4], Re
   }
 }
 
-// The pages of tiles [lo, hi), all of whose keys every row sees.  Step e of the loop: the
-// products of the values of the tile before and of its own keys, then its weights; before
-// them the next tile's keys and its own values are expanded into the arrays that were last
-// read in the step before, and the loads of those behind them start.  One step more ends with
-// the last tile's values.
-__device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg, int lo, int hi, bool idle, int ex,
-                                           const u32x4 (&q)[8], Running& r, uint8_t* lds, PageRef* list, int* scnt) {
-  uint8_t* const sk = lds;
-  uint8_t* const sv = lds + 2 * kTileBytes;
-  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, lh = lane >> 5;
-  const int krow = key_of_row(lr);
-  const int kbase = krow * kRowBytes + 16 * (lh ^ swz_k(krow));
-  const int vbase = lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr));
-  const int kput = (tid >> 3) * kRowBytes + 16 * ((2 * (tid & 7)) ^ swz_k(tid >> 3));
-  const int vput = (tid >> 2) * (2 * kBlk) + 16 * ((2 * (tid & 3)) ^ swz_c(tid >> 2));
-  auto load = [&](const int8_t* codes, int page) __attribute__((always_inline)) {
-    return *(const u32x4*)(codes + ((int64_t)page * a.H_kv + sg.g) * kCodes + (uint32_t)(16 * tid));
+// Key tiles 0 .. n - 1 of a source (pages or rows in bf16).  Step e of the loop: the products
+// of the values of the tile before and of its own keys, then its weights; meanwhile the next
+// tile's keys and its own values are put into the arrays that were last read in the step
+// before, and the loads of those behind them start.  One step more ends with the last tile's
+// values.  The waves of a SIMD (w and w + 4) are half a step apart: while one has products,
+// the other has weights and stages.
+//   src.load_k(e), src.load_v(e)     into registers
+//   src.put_k(to), src.put_v(e, to)  from there into LDS
+//   src.sees(e)                      the wave has rows that see keys of tile e
+//   src.logits(e, st)                what is left to do with raw logits, returns their scale
+//   src.values(e, ...)               the operands of the second product
+template <class Source>
+__device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ahead, const u32x4 (&q)[8], Running& r,
+                                          const Shared& sm) {
+  src.load_k(0);
+  src.load_v(0);
+  src.put_k(sm.k);
+  src.load_k(min(1, n - 1));
+  __syncthreads();
+  f32x16 st[2];
+  u32x4 pw[4];
+  auto weights = [&](int e) __attribute__((always_inline)) {
+    if (!src.sees(e)) return;
+    float vs;
+    const float sc = src.logits(e, st, vs);
+    weigh<2>(r, st, sc, vs, pw);
   };
-  auto put = [&](const u32x4& x, uint8_t* to, int at) __attribute__((always_inline)) {
+  auto stage = [&](int e, int b, int c) __attribute__((always_inline)) {
+    src.put_k(sm.k + c);           // (past the last tile: that again, in an array that is not read)
+    src.put_v(e, sm.v + b);
+    src.load_v(min(e + 1, n - 1));
+    src.load_k(min(e + 2, n - 1));
+  };
+#pragma unroll 1
+  for (int e = 0; e <= n; ++e) {
+    const int b = (e & 1) * kTileBytes, c = b ^ kTileBytes;
+    if (!ahead) {
+      if (e > 0) weights(e - 1);
+      if (e < n) stage(e, b, c);
+    }
+    if (e > 0 && src.sees(e - 1)) src.values(e - 1, sm.v + c, r, pw);
+    if (e < n && src.sees(e)) wide_logits(sm.k + b, kbase, q, st);
+    if (ahead && e < n) {
+      weights(e);
+      stage(e, b, c);
+    }
+    __syncthreads();   // (the last one before the arrays are written again)
+  }
+}
+
+struct PageSource {
+  const BlockArgs& a;
+  const PageRef* list;
+  int g, ex, tid, kput, vput, vbase;
+  bool idle;
+  u32x4 kr, vr;
+  __device__ __forceinline__ u32x4 load(const int8_t* codes, int e) const {
+    const int page = __builtin_amdgcn_readfirstlane(list[e].page);
+    return *(const u32x4*)(codes + ((int64_t)page * a.H_kv + g) * kCodes + (uint32_t)(16 * tid));
+  }
+  __device__ __forceinline__ void put(const u32x4& x, uint8_t* to, int at) const {
     *(u32x4*)(to + at) = codes_bf16(x[0], x[1]);
     *(u32x4*)(to + (at ^ 16)) = codes_bf16(x[2], x[3]);
-  };
+  }
+  __device__ __forceinline__ void load_k(int e) { kr = load(a.k_codes, e); }
+  __device__ __forceinline__ void load_v(int e) { vr = load(a.v_codes, e); }
+  __device__ __forceinline__ void put_k(uint8_t* to) const { put(kr, to, kput); }
+  __device__ __forceinline__ void put_v(int, uint8_t* to) const { put(vr, to, vput); }
+  __device__ __forceinline__ bool sees(int) const { return !idle; }
+  __device__ __forceinline__ float logits(int e, f32x16 (&)[2], float& vs) const {
+    vs = list[e].vs;
+    return logit_scale(a, ex, list[e].ks);
+  }
+  __device__ __forceinline__ void values(int, const uint8_t* from, Running& r, const u32x4 (&pw)[4]) const {
+    wide_values(r, pw, [&](int ks, u32x4 (&y)[4]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = *(const u32x4*)(from + (vbase ^ (32 * ks)) + i * 32 * 2 * kBlk);
+    });
+  }
+};
+
+// The pages of tiles [lo, hi), all of whose keys every row sees.
+__device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg, int lo, int hi, bool idle, int ex,
+                                           const u32x4 (&q)[8], Running& r, const Shared& sm, PageRef* list,
+                                           int* scnt) {
+  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 31, lh = lane >> 5, krow = key_of_row(lr);
+  PageSource src = {a, list, sg.g, ex, tid,
+                    (tid >> 3) * kRowBytes + 16 * ((2 * (tid & 7)) ^ swz_k(tid >> 3)),
+                    (tid >> 2) * (2 * kBlk) + 16 * ((2 * (tid & 3)) ^ swz_c(tid >> 2)),
+                    lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr)), idle};
   for (int t0 = lo; t0 < hi; t0 += kList) {
     // ---- the next pages (blocks without one are left out)
     PageRef x = {-1, 0.f, 0.f};
@@ -567,141 +675,92 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
     n = __builtin_amdgcn_readfirstlane(n);
     if (x.page >= 0) list[at] = x;
     __syncthreads();
-    if (n == 0) continue;
-
-    auto page = [&](int e) { return __builtin_amdgcn_readfirstlane(list[min(e, n - 1)].page); };
-    u32x4 kr = load(a.k_codes, page(0)), vr = load(a.v_codes, page(0));
-    put(kr, sk, kput);
-    kr = load(a.k_codes, page(1));
-    int next = page(1);
-    __syncthreads();
-    f32x16 st[2];
-    u32x4 pw[4];
-    // The waves of a SIMD (w and w + 4) are half a step apart: while one has products, the
-    // other has weights and codes.
-    const bool ahead = wave < kWaves / 2;
-    auto weights = [&](int e) __attribute__((always_inline)) {
-      if (!idle) weigh<2>(r, st, logit_scale(a, ex, list[e].ks), list[e].vs, pw);
-    };
-    auto stage = [&](int e, uint8_t* k_to, uint8_t* v_to) __attribute__((always_inline)) {
-      put(kr, k_to, kput);     // (past the last page: that again, in arrays that are not read)
-      put(vr, v_to, vput);
-      vr = load(a.v_codes, next);
-      next = page(e + 2);
-      kr = load(a.k_codes, next);
-    };
-#pragma unroll 1
-    for (int e = 0; e <= n; ++e) {
-      const int b = (e & 1) * kTileBytes, c = b ^ kTileBytes;
-      if (!ahead) {
-        if (e > 0) weights(e - 1);
-        if (e < n) stage(e, sk + c, sv + b);
-      }
-      if (!idle) {
-        if (e > 0)
-          wide_values(r, pw, [&](int ks, u32x4 (&y)[4]) __attribute__((always_inline)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = *(const u32x4*)(sv + c + (vbase ^ (32 * ks)) + i * 32 * 2 * kBlk);
-          });
-        if (e < n) wide_logits(sk + b, kbase, q, st);
-      }
-      if (ahead && e < n) {
-        weights(e);
-        stage(e, sk + c, sv + b);
-      }
-      __syncthreads();   // (the last one before the list and the arrays are written again)
-    }
+    if (n) wide_loop(src, n, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), wave < kWaves / 2, q, r, sm);
   }
 }
 
-// Tiles [lo, hi) of rows in bf16: the open block and the chunk.
-__device__ __forceinline__ void wide_rows(const BlockArgs& a, const ChunkStep& s, const Segment& sg, int lo, int hi,
-                                          int pos, int wpos0, int wpos1, int ex, const u32x4 (&q)[8], Running& r,
-                                          uint8_t* lds, int (*sodd)[kWaves]) {
-  uint8_t* const sk = lds;
-  uint8_t* const sv = lds + 2 * kTileBytes;
-  const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lr = lane & 31, lh = lane >> 5;
-  const int last = sg.p.held + sg.p.n - 1;            // the place's last position
-  const int krow = key_of_row(lr);
-  const int kbase = krow * kRowBytes + 16 * (lh ^ swz_k(krow));
-  int vbase[2];
+// Tiles of rows in bf16, of the open block and of the chunk.  A thread has chunk tid % 16 of
+// rows tid / 16 and 32 more; byte offsets in a tile fit 32 bits (checked on the host).
+struct RowSource {
+  const BlockArgs& a;
+  const ChunkStep& s;
+  const Segment& sg;
+  int t0, ex, pos, wpos0, wpos1, last;   // last: the place's last position
+  int lane, wave, fr;
+  int (*sodd)[kWaves];
+  u32x4 kr[2], vr[2];
+  __device__ __forceinline__ void load(const uint16_t* tail, const uint16_t* rows, int64_t stride, int e,
+                                       u32x4 (&x)[2]) const {
+    const int p0 = (t0 + e) * kBlk, c = 16 * (lane & 15);
+    const uint8_t* from = (const uint8_t*)(rows + ((int64_t)sg.start + p0 - sg.p.held) * stride);
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int key = 8 * lh + 4 * j + ((lane >> 2) & 3);
-    vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
+    for (int i = 0; i < 2; ++i) {
+      const int key = min(fr + 32 * i, last - p0);         // (past the last: that again, masked)
+      const uint8_t* at = from + (uint32_t)((uint32_t)key * (uint32_t)(2 * stride) + c);
+      if (p0 < sg.p.held && p0 + key < sg.p.held) at = (const uint8_t*)tail + key * kRowBytes + c;
+      x[i] = *(const u32x4*)at;
+    }
   }
-  const int fr = tid >> 4;                            // a thread has chunk tid % 16 of rows fr and fr + 32
-  const int kput = fr * kRowBytes + 16 * ((tid & 15) ^ swz_k(fr));
-  const int vput = fr * kRowBytes + 16 * ((tid & 15) ^ swz_v(fr));
-  auto load = [&](bool values, int t, u32x4 (&x)[2]) __attribute__((always_inline)) {
+  __device__ __forceinline__ int64_t tail() const { return ((int64_t)sg.seq * a.H_kv + sg.g) * kCodes; }
+  __device__ __forceinline__ void load_k(int e) { load(a.k_tail + tail(), s.k + sg.g * s.k_sh, s.k_st, e, kr); }
+  __device__ __forceinline__ void load_v(int e) { load(a.v_tail + tail(), s.v + sg.g * s.v_sh, s.v_st, e, vr); }
+  __device__ __forceinline__ void put_k(uint8_t* to) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      x[i] = *(const u32x4*)(fresh_row(a, s, sg, values, min(t * kBlk + fr + 32 * i, last)) + 8 * (tid & 15));
-  };
-  u32x4 kr[2], vr[2];
-  load(false, lo, kr);
-  load(true, lo, vr);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) *(u32x4*)(sk + kput + 32 * i * kRowBytes) = kr[i];
-  load(false, min(lo + 1, hi - 1), kr);
-  __syncthreads();
-  f32x16 st[2];
-  u32x4 pw[4];
-  bool mine = false;             // the wave has rows that see keys of the tile before
-#pragma unroll 1
-  for (int t = lo; t <= hi; ++t) {
-    const int p = (t - lo) & 1, b = p * kTileBytes, c = b ^ kTileBytes;
-    if (t < hi) {
-      bool odd = false;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        *(u32x4*)(sk + c + kput + 32 * i * kRowBytes) = kr[i];
-        odd |= take_out(vr[i]);
-        *(u32x4*)(sv + b + vput + 32 * i * kRowBytes) = vr[i];
-      }
-      const int any = __any(odd);
-      if (lane == 0) sodd[p][wave] = any;
-      load(true, min(t + 1, hi - 1), vr);
-      load(false, min(t + 2, hi - 1), kr);
-    }
-    if (mine) {
-      wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                        sv + c + (vbase[0] ^ (64 * i)) + 16 * ks * kRowBytes)));
-          const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                        sv + c + (vbase[1] ^ (64 * i)) + 16 * ks * kRowBytes)));
-          x[i] = (u32x4){y[0], y[1], z[0], z[1]};
-        }
-      });
-      int odd = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) odd |= sodd[p ^ 1][w];
-      if (__builtin_amdgcn_readfirstlane(odd))
-        add_odd(r, [&](int key) { return fresh_row(a, s, sg, true, (t - 1) * kBlk + key); },
-                min(kBlk, pos - (t - 1) * kBlk + 1), lh);
-    }
-    mine = t < hi && t * kBlk <= wpos1;
-    if (mine) {
-      wide_logits(sk + b, kbase, q, st);
-      if (t * kBlk + kBlk - 1 > wpos0) {
-        const int rel = pos - t * kBlk - 8 * lh;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) st[kt][i] = -INFINITY;
-      }
-      weigh<2>(r, st, logit_scale(a, ex, 1.f), 1.f, pw);
-    }
-    __syncthreads();
+      *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_k(fr))) = kr[i];
   }
-}
+  __device__ __forceinline__ void put_v(int e, uint8_t* to) {
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      odd |= take_out(vr[i]);
+      *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_v(fr))) = vr[i];
+    }
+    const int any = __any(odd);
+    if (lane == 0) sodd[e & 1][wave] = any;
+  }
+  __device__ __forceinline__ bool sees(int e) const { return (t0 + e) * kBlk <= wpos1; }
+  __device__ __forceinline__ float logits(int e, f32x16 (&st)[2], float& vs) const {
+    const int p0 = (t0 + e) * kBlk;
+    if (p0 + kBlk - 1 > wpos0) {
+      const int rel = pos - p0 - 8 * (lane >> 5);
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) st[kt][i] = -INFINITY;
+    }
+    vs = 1.f;
+    return logit_scale(a, ex, 1.f);
+  }
+  __device__ __forceinline__ void values(int e, const uint8_t* from, Running& r, const u32x4 (&pw)[4]) const {
+    int vbase[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int key = 8 * (lane >> 5) + 4 * j + ((lane >> 2) & 3);
+      vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
+    }
+    wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                      from + (vbase[0] ^ (64 * i)) + 16 * ks * kRowBytes)));
+        const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                      from + (vbase[1] ^ (64 * i)) + 16 * ks * kRowBytes)));
+        x[i] = (u32x4){y[0], y[1], z[0], z[1]};
+      }
+    });
+    int odd = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) odd |= sodd[e & 1][w];
+    if (__builtin_amdgcn_readfirstlane(odd))
+      add_odd(r, [&](int key) { return fresh_row(a, s, sg, true, (t0 + e) * kBlk + key); },
+              min(kBlk, pos - (t0 + e) * kBlk + 1), lane >> 5);
+  }
+};
 
 __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
-                                            const RowTile& rt, int part, uint8_t* lds, PageRef* list,
+                                            const RowTile& rt, int part, const Shared& sm, PageRef* list,
                                             int (*sodd)[kWaves], int* scnt) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
@@ -712,12 +771,14 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
   Running r;
   clear(r);
   const int n_blk = sg.p.held / kBlk;
-  if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, ex, q, r, lds, list, scnt);
+  if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, ex, q, r, sm, list, scnt);
   if (rt.hi > n_blk) {
     // first and last position of the wave's rows
     const int wpos0 = sg.p.held + rt.pos0 + wave * 32 / a.gqa;
     const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + min(wave * 32 + 31, rt.n_rows - 1) / a.gqa;
-    wide_rows(a, s, sg, max(rt.lo, n_blk), rt.hi, sg.p.held + i_row, wpos0, wpos1, ex, q, r, lds, sodd);
+    const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr);
+    RowSource src = {a, s, sg, t0, ex, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4, sodd};
+    wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), wave < kWaves / 2, q, r, sm);
   }
 
   r.l = half_sum(r.l);
@@ -753,7 +814,8 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
 }  // namespace
 
 __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, ChunkStep s) {
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_k[kLds], lds_v[kLds];
+  const Shared sm = {lds_k, lds_v};
   __shared__ float2 sml[kWaves][32];
   __shared__ PageRef list[kList];
   __shared__ int sodd[2][kWaves], scnt[kWaves];
@@ -762,77 +824,94 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   const int part = (blockIdx.x & 7) * (kChunkParts / 8) + (blockIdx.x >> 3);
   const int64_t total = line_total(a, s, lp), size = lane_of(chunk_part(total), 0);
   const int64_t begin = part * size, end = min(begin + size, total);
+  if (threadIdx.x == 0) s.joins[part].n_rows = 0;
   walk(a, begin, end, s, lp, [&](const Segment& sg) {
     RowTile rt;
-    rt.lo = chunk_key_tile(sg.from);
-    rt.hi = chunk_key_tile(sg.to);
-    if (rt.lo >= rt.hi) return;
+    rt.lo = chunk_key_tile(sg.from, sg.p.rows);
+    rt.hi = chunk_key_tile(sg.to, sg.p.rows);
     rt.pos0 = sg.tile * sg.p.per;
     rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
+    if (thread_here() == 0 && sg.from > 0 && sg.from <= size) {   // the first part to begin inside it
+      const int64_t stop = sg.at + chunk_cost(sg.p, sg.tile);
+      s.joins[part] = {sg.at, stop, size, (int64_t)sg.start + rt.pos0, rt.n_rows, sg.p.rows,
+                       chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
+    }
+    if (rt.lo >= rt.hi) return;
     rt.whole = rt.lo == 0 && rt.hi == chunk_key_tiles(sg.p, sg.tile);
-    if (sg.p.rows < 256) attend_few(a, s, sg, rt, part, lds, sml);
-    else attend_many(a, s, sg, rt, part, lds, list, sodd, scnt);
+    if (sg.p.rows < 256) attend_few(a, s, sg, rt, part, sm, sml);
+    else attend_many(a, s, sg, rt, part, sm, list, sodd, scnt);
   });
 }
 
 // Joins the row tiles that more than one part served: workgroup (w, r) takes rows 8 r .. + 7
-// of the row tile in which part w begins, if w is the first part that begins inside it.
+// of the one that part w begins inside, if it is the first to do so.
 namespace {
-constexpr int kMergeRows = 8;
+constexpr int kMergeRows = 8, kMergeRound = 8;
 }
-__global__ __launch_bounds__(kThreads) void k_chunk_merge(BlockArgs a, ChunkStep s) {
-  const int w = blockIdx.x + 1, r = blockIdx.y * kMergeRows + (threadIdx.x >> 5);
-  __shared__ LinePlaces lp;
-  const int64_t total = line_total(a, s, lp), size = lane_of(chunk_part(total), 0);
-  const int64_t x0 = w * size;
-  if (x0 >= total) return;
-  walk(a, x0, x0 + 1, s, lp, [&](const Segment& sg) {
-    if (sg.from == 0) return;                    // the cut is at its start
-    if (x0 - size > sg.at) return;               // an earlier part begins inside it
-    const ChunkPlace& p = sg.p;
-    const int pos0 = sg.tile * p.per, n_rows = (chunk_end(p, sg.tile) - pos0) * a.gqa;
-    if (blockIdx.y * kMergeRows >= n_rows) return;
-    const int v_all = chunk_key_tiles(p, sg.tile);
-    const int64_t stop = sg.at + chunk_cost(p, sg.tile);
-    const int w1 = (int)((stop - 1) / size), c = 4 * (threadIdx.x & 31), rr = min(r, n_rows - 1);
-    float M = -INFINITY, L = 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int i = w - 1; i <= w1; ++i) {
-      const int lo = chunk_key_tile(max(i * size - sg.at, (int64_t)0));
-      const int hi = chunk_key_tile(min(i * size + size, stop) - sg.at);
-      if (lo >= hi) continue;
-      if (lo == 0 && hi == v_all) return;        // written by that part
-      const int64_t slot = (int64_t)chunk_slot(i, lo) * s.slot_rows + rr;
-      const float2 ml = s.part_ml[slot];
-      const f32x4 y = *(const f32x4*)(s.part_o + slot * kHeadDim + c);
-      const float mn = fmaxf(M, ml.x), mu = mn > -INFINITY ? mn : 0.f;
-      const float f0 = __builtin_amdgcn_exp2f(M - mu), f1 = __builtin_amdgcn_exp2f(ml.x - mu);
-      M = mn;
-      L = fmaf(f1, ml.y, f0 * L);
+__global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) {
+  const int w = blockIdx.x + 1;
+  const ChunkJoin jn = s.joins[w];
+  const int r0 = blockIdx.y * kMergeRows, r = r0 + (threadIdx.x >> 5);
+  if (r0 >= jn.n_rows) return;
+  const int c = 4 * (threadIdx.x & 31), rr = min(r, jn.n_rows - 1);
+  float M = -INFINITY, L = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int i0 = w - 1; i0 <= jn.last; i0 += kMergeRound) {
+    // a round of parts, all loads first
+    float2 ml[kMergeRound];
+    f32x4 y[kMergeRound];
+    bool there[kMergeRound];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = fmaf(f1, y[j], f0 * x[j]);
+    for (int k = 0; k < kMergeRound; ++k) {
+      const int i = min(i0 + k, jn.last);
+      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.rows);
+      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.rows);
+      there[k] = i0 + k <= jn.last && lo < hi;
+      if (lo == 0 && hi == jn.key_tiles) return;         // written by that part
+      if (!there[k]) continue;
+      const int64_t slot = (int64_t)chunk_slot(i, lo) * s.slot_rows + rr;
+      ml[k] = s.part_ml[slot];
+      y[k] = *(const f32x4*)(s.part_o + slot * kHeadDim + c);
     }
-    if (r < n_rows) {
-      uint16_t* op = s.out + (sg.start + pos0 + r / a.gqa) * s.o_st + (sg.g * a.gqa + r % a.gqa) * s.o_sh + c;
-      *(u32x2*)op = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
+    float mn = M;
+#pragma unroll
+    for (int k = 0; k < kMergeRound; ++k)
+      if (there[k]) mn = fmaxf(mn, ml[k].x);
+    const float mu = mn > -INFINITY ? mn : 0.f, f0 = __builtin_amdgcn_exp2f(M - mu);
+    M = mn;
+    L *= f0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= f0;
+#pragma unroll
+    for (int k = 0; k < kMergeRound; ++k) {
+      if (!there[k]) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[k].x - mu);
+      L = fmaf(f, ml[k].y, L);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = fmaf(f, y[k][j], x[j]);
     }
-  });
+  }
+  if (r >= jn.n_rows) return;
+  uint16_t* op = s.out + (jn.row + r / gqa) * s.o_st + (jn.head + r % gqa) * s.o_sh + c;
+  *(u32x2*)op = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
 }
 
 // Rows of a partial result: those of the largest row tile a call of `total` rows can have.
 static int slot_rows(int64_t total, int gqa) { return chunk_rows(total * gqa); }
 int64_t block_chunk_workspace_bytes(int64_t total, int gqa) {
-  return (int64_t)2 * kChunkParts * slot_rows(total, gqa) * (kHeadDim * sizeof(float) + sizeof(float2));
+  return (int64_t)2 * kChunkParts * slot_rows(total, gqa) * (kHeadDim * sizeof(float) + sizeof(float2)) +
+         kChunkParts * sizeof(ChunkJoin);
 }
 
 hipError_t launch_chunk_attend(const BlockArgs& a, ChunkStep s, void* workspace, hipStream_t st) {
   s.slot_rows = slot_rows(s.total, a.gqa);
   s.part_o = (float*)workspace;
   s.part_ml = (float2*)(s.part_o + (int64_t)2 * kChunkParts * s.slot_rows * kHeadDim);
+  s.joins = (ChunkJoin*)(s.part_ml + (int64_t)2 * kChunkParts * s.slot_rows);
   k_chunk_attend<<<dim3(kChunkParts), kChunkThreads, 0, st>>>(a, s);
   if (hipError_t e = hipGetLastError()) return e;
   const int rows = (int)std::min<int64_t>(s.slot_rows, (int64_t)s.total * a.gqa);
-  k_chunk_merge<<<dim3(kChunkParts - 1, (rows + kMergeRows - 1) / kMergeRows), kThreads, 0, st>>>(a, s);
+  k_chunk_merge<<<dim3(kChunkParts - 1, (rows + kMergeRows - 1) / kMergeRows), kThreads, 0, st>>>(a.gqa, s);
   return hipGetLastError();
 }
 

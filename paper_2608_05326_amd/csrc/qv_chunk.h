@@ -2,10 +2,10 @@
 // (place, KV head) pair are its (position, head) pairs, row = position G + head; a row tile
 // is as many whole positions as fit the rows that a workgroup holds.  Row tile t of a place
 // with L tokens held sees the keys up to its last position, in tiles of 64 keys.  All row
-// tiles, in the order place, KV head, tile, are laid on one line, each as long as the keys
-// that it sees and kChunkCost more (what a segment costs beside its keys); the line is cut
-// into equal parts, one per workgroup.  Lengths are linear in t, so a place's sum has a
-// closed form and nothing is tabulated.  Arithmetic only, so that it also compiles for the
+// tiles, in the order place, KV head, tile, are laid on one line, each as long as its time is
+// expected to be: a weight for every key that it sees, and what it costs beside them.  The
+// line is cut into equal parts, one per workgroup.  Lengths are linear in t, so a place's sum
+// has a closed form and nothing is tabulated.  Arithmetic only, so that it also compiles for the
 // host.
 #pragma once
 #include "qv_layout.h"
@@ -13,11 +13,13 @@
 namespace qv {
 
 constexpr int kChunkParts = 256;    // one workgroup of eight waves to a compute unit
-constexpr int kChunkCost = 128;     // keys
-constexpr int kChunkMin = 128;      // the least a part is, in keys
+constexpr int kChunkMin = 4096;     // the least a part is
 
 // Rows of a workgroup for a place with this many in all.
 QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// What a key costs on the line, by rows, and a row tile beside its keys.
+QV_HD int chunk_weight(int rows) { return rows <= 128 ? 3 : 8; }
+QV_HD int chunk_extra(int rows) { return rows <= 128 ? 1536 : 3072; }
 
 struct ChunkPlace {
   int held, n;        // tokens held, new tokens (0: none)
@@ -43,10 +45,13 @@ QV_HD int chunk_end(const ChunkPlace& p, int t) {
 }
 
 // Length of row tile t on the line, and of the t row tiles before it.
-QV_HD int64_t chunk_cost(const ChunkPlace& p, int t) { return (int64_t)p.held + chunk_end(p, t) + kChunkCost; }
+QV_HD int64_t chunk_cost(const ChunkPlace& p, int t) {
+  return ((int64_t)p.held + chunk_end(p, t)) * chunk_weight(p.rows) + chunk_extra(p.rows);
+}
 QV_HD int64_t chunk_before(const ChunkPlace& p, int t) {
-  const int64_t even = (int64_t)t * ((int64_t)p.held + kChunkCost) + (int64_t)p.per * t * (t + 1) / 2;
-  return t < p.tiles || t == 0 ? even : even - ((int64_t)p.tiles * p.per - p.n);
+  int64_t keys = (int64_t)t * p.held + (int64_t)p.per * t * (t + 1) / 2;
+  if (t == p.tiles && t) keys -= (int64_t)p.tiles * p.per - p.n;
+  return keys * chunk_weight(p.rows) + (int64_t)t * chunk_extra(p.rows);
 }
 QV_HD int64_t chunk_pair_cost(const ChunkPlace& p) { return chunk_before(p, p.tiles); }
 
@@ -61,12 +66,23 @@ QV_HD int chunk_tile_at(const ChunkPlace& p, int64_t x) {
   return lo;
 }
 
-// Tiles of 64 keys that row tile t sees, and the first of them at or past point x of it.
+// x / y for 0 <= x < 2^62 with a quotient below 2^30 (a device's 64-bit division is long).
+QV_HD int chunk_quotient(int64_t x, int64_t y) {
+  int q = (int)((double)x / (double)y);
+  if ((int64_t)q * y > x) --q;
+  if ((int64_t)(q + 1) * y <= x) ++q;
+  return q;
+}
+
+// Tiles of 64 keys that row tile t sees, and the first of them at or past point x of a row
+// tile of `rows` rows.
 QV_HD int chunk_key_tiles(const ChunkPlace& p, int t) {
   return (int)(((int64_t)p.held + chunk_end(p, t) + kBlockTokens - 1) / kBlockTokens);
 }
-QV_HD int chunk_key_tile(int64_t x) {
-  return x <= kChunkCost ? 0 : (int)((x - kChunkCost + kBlockTokens - 1) / kBlockTokens);
+QV_HD int chunk_key_tile(int64_t x, int rows) {
+  const int64_t y = x - chunk_extra(rows);
+  const int step = kBlockTokens * chunk_weight(rows);
+  return y <= 0 ? 0 : chunk_quotient(y + step - 1, step);
 }
 
 // Length of a part, given the line's.

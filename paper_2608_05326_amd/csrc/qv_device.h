@@ -235,6 +235,14 @@ struct BlockStep {          // a decode step on the block cache
   float2* part_ml;          // [kParts + 2 B H_kv][gqa] (maximum in log2 units, sum)
 };
 
+struct ChunkJoin {          // a row tile that several parts serve, by the first that begins inside it
+  int64_t at, stop, size;   // the row tile on the line, the length of a part
+  int64_t row;              // its first row of the packed tensors
+  int32_t n_rows;           // (position, head) rows; 0: nothing to join
+  int32_t rows, key_tiles;  // rows of its workgroups, tiles of all its keys
+  int32_t head, last;       // first query head, last part
+};
+
 struct ChunkStep {          // attention of new tokens over the block cache and themselves
   const uint16_t* q;        // rows [total] x heads, strides in elements
   const uint16_t* k;
@@ -246,6 +254,7 @@ struct ChunkStep {          // attention of new tokens over the block cache and 
   int32_t slot_rows;        // rows of a partial result
   float* part_o;            // [2 parts][slot_rows][d]
   float2* part_ml;          // [2 parts][slot_rows] (maximum in log2 units, sum)
+  ChunkJoin* joins;         // [parts]
 };
 
 struct ScorePowArgs {       // p-norm ranking: prompt scores raised to the power p

@@ -1727,6 +1727,8 @@ qevict_status qevict_block_attend_chunk(const qevict_block_config* cfg, const qe
       (s = check_rows("v", v, n, a.H_kv, rows->v_token_stride, rows->v_head_stride, false)) ||
       (s = check_rows("out", out, n, a.H_q, rows->out_token_stride, rows->out_head_stride, true)))
     return s;
+  if (rows->k_token_stride >= (1 << 23) || rows->v_token_stride >= (1 << 23))   // 32-bit offsets in a tile
+    return fail(QEVICT_ERR_UNSUPPORTED, "token strides of k and v must be below 2^23");
   if (!workspace || ((uintptr_t)workspace & 255))
     return fail(QEVICT_ERR_WORKSPACE, "workspace must be a 256-byte aligned device pointer");
   const int64_t need = block_chunk_workspace_bytes(n, a.gqa);

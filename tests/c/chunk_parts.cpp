@@ -66,12 +66,13 @@ int main() {
           const int64_t c = chunk_cost(places[s], t);
           CHECK(c > 0);
           CHECK(chunk_tile_at(places[s], in_pair) == t && chunk_tile_at(places[s], in_pair + c - 1) == t);
-          CHECK(chunk_key_tile(c) == chunk_key_tiles(places[s], t));
+          CHECK(chunk_key_tile(c, places[s].rows) == chunk_key_tiles(places[s], t));
           tiles.push_back({s, g, t, chunk_key_tiles(places[s], t), at, at + c});
           at += c;
           in_pair += c;
         }
         CHECK(in_pair == chunk_pair_cost(places[s]));
+        if (in_pair) CHECK(chunk_quotient((g + 1) * in_pair - 1, in_pair) == g && chunk_quotient(g * in_pair, in_pair) == g);
       }
     CHECK(at == total);
 
@@ -85,7 +86,8 @@ int main() {
       while (x < end) {
         while (tiles[i].stop <= x) ++i;
         const int64_t stop = std::min(end, tiles[i].stop);
-        const int lo = chunk_key_tile(x - tiles[i].at), hi = chunk_key_tile(stop - tiles[i].at);
+        const int rows = places[tiles[i].s].rows;
+        const int lo = chunk_key_tile(x - tiles[i].at, rows), hi = chunk_key_tile(stop - tiles[i].at, rows);
         if (lo < hi) {
           int slot = -1;
           if (lo > 0 || hi < tiles[i].v) {
@@ -113,9 +115,10 @@ int main() {
         if (x0 >= total || x0 <= t.at || x0 >= t.stop || x0 - size > t.at) continue;
         std::vector<Served> got;
         bool whole = false;
-        for (int k = w - 1; k <= (int)((t.stop - 1) / size); ++k) {
-          const int lo = chunk_key_tile(std::max<int64_t>(k * size - t.at, 0));
-          const int hi = chunk_key_tile(std::min(k * size + size, t.stop) - t.at);
+        CHECK(x0 - t.at <= size);   // (what the attention kernel goes by)
+        for (int k = w - 1; k <= chunk_quotient(t.stop - 1, size); ++k) {
+          const int lo = chunk_key_tile(std::max<int64_t>(k * size - t.at, 0), places[t.s].rows);
+          const int hi = chunk_key_tile(std::min(k * size + size, t.stop) - t.at, places[t.s].rows);
           if (lo >= hi) continue;
           if (lo == 0 && hi == t.v) whole = true;
           got.push_back({k, lo, hi, chunk_slot(k, lo)});

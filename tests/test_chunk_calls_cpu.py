@@ -156,6 +156,8 @@ def test_append_refuses(kw, status):
     (dict(rows=dict(total_tokens=1 << 28)), m.ERR_UNSUPPORTED),
     (dict(rows=dict(q_token_stride=-8)), m.ERR_INVALID_ARG),
     (dict(rows=dict(v_head_stride=4)), m.ERR_INVALID_ARG),
+    (dict(rows=dict(k_token_stride=1 << 23)), m.ERR_UNSUPPORTED),
+    (dict(rows=dict(v_token_stride=1 << 24)), m.ERR_UNSUPPORTED),
     (dict(rows=dict(out_token_stride=512)), m.ERR_INVALID_ARG),
 ])
 def test_attend_chunk_refuses(kw, status):
