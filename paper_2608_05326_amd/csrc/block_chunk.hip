@@ -59,13 +59,13 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w0, uint32_t w1) {
   return (u32x4){a[0], a[1], b[0], b[1]};
 }
 
-// threadIdx.x, not to be seen through: what is derived from it is computed where it is used
+// A value, or threadIdx.x, not to be seen through: what is derived from it is computed where it is used
 // (hoisted out of the walk over segments, it would fill the registers that the products need).
-__device__ __forceinline__ int thread_here() {
-  int t = threadIdx.x;
-  asm volatile("" : "+v"(t));
-  return t;
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
+__device__ __forceinline__ int thread_here() { return here(threadIdx.x); }
 
 // The place in lane, with its length on the line.
 __device__ __forceinline__ ChunkPlace lane_place(const BlockArgs& a, const ChunkStep& s, int place, int* start) {
@@ -197,12 +197,19 @@ __device__ __forceinline__ int load_query(const uint16_t* p, int lh, u32x4 (&q)[
     }
   return ex - kQueryExp;
 }
-// Log2 units per raw logit of keys with the scale ks: scale_log2 2^ex ks.  The power of two
-// comes last: products of small queries and large keys are logits of ordinary size.
-__device__ __forceinline__ float logit_scale(const BlockArgs& a, int ex, float ks) {
-  const float x = ldexpf(__builtin_amdgcn_frexp_mantf(a.scale_log2) * ks,
-                         __builtin_amdgcn_frexp_expf(a.scale_log2) + ex);
-  return x == INFINITY ? __FLT_MAX__ : x;   // (a product of zero is a logit of zero)
+// Log2 units per raw logit of keys with the scale ks: scale_log2 2^ex ks, held as a mantissa
+// and a power of two that comes last: products of small queries and large keys are logits of
+// ordinary size.
+struct LogitScale {
+  float m;
+  int e;
+  __device__ __forceinline__ float operator()(float ks) const {
+    const float x = ldexpf(m * ks, e);
+    return x == INFINITY ? __FLT_MAX__ : x;   // (a product of zero is a logit of zero)
+  }
+};
+__device__ __forceinline__ LogitScale logit_scale(const BlockArgs& a, int ex) {
+  return {__builtin_amdgcn_frexp_mantf(a.scale_log2), __builtin_amdgcn_frexp_expf(a.scale_log2) + ex};
 }
 
 // Running maximum (log2 units), sum and output of one row: o[c][i] is channel
@@ -326,6 +333,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   int page = page_at(rt.lo + kg);
   u32x4 q[8];
   const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + row % a.gqa) * s.q_sh, lh, q);
+  const LogitScale scale = logit_scale(a, ex);
   Running r;
   clear(r);
   // row lr of an A operand is this key of 32; a lane's logits st[i] are those of keys 16 lh + i
@@ -369,7 +377,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
       const int j = __builtin_ctzll(live);
       live &= live - 1;
       e = entry(live ? __builtin_ctzll(live) : j);     // (after the last: that again)
-      const float sc = logit_scale(a, ex, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)));
+      const float sc = scale(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks_l), j)));
       const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs_l), j));
       f32x16 st[2];
       u32x4 pw[4];
@@ -447,7 +455,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (k0 + 16 * lh + i > pos) sr[0][i] = -INFINITY;
-      weigh<1>(r, sr, logit_scale(a, ex, 1.f), 1.f, pr);
+      weigh<1>(r, sr, scale(1.f), 1.f, pr);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // this wave's rows are in LDS
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
@@ -524,32 +532,28 @@ __device__ __forceinline__ int swz_c(int channel) { return (channel >> 1) & 7; }
 __device__ __forceinline__ int key_of_row(int lr) {
   return 16 * (lr >> 4) + 8 * ((lr >> 2) & 1) + 4 * ((lr >> 3) & 1) + (lr & 3);
 }
-// st = K Q^T of a staged tile.  Operands are read three steps ahead of their products: a read
-// takes longer than the products of one step.
-__device__ __forceinline__ void wide_logits(const uint8_t* from, int kbase, const u32x4 (&q)[8], f32x16 (&st)[2]) {
+// st = K Q^T of a staged tile; read(ks, x) reads the two A operands of k-step ks.  Operands are
+// read three steps ahead of their products: a read takes longer than the products of one step.
+template <class Read>
+__device__ __forceinline__ void wide_logits(const u32x4 (&q)[8], f32x16 (&st)[2], Read read) {
   constexpr int kAhead = 3;
   u32x4 kk[kAhead][2];
-  auto read = [&](int ks) __attribute__((always_inline)) {
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-      kk[ks % kAhead][kt] = *(const u32x4*)(from + (kbase ^ (32 * ks)) + 32 * kt * kRowBytes);
-  };
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
 #pragma unroll
-  for (int ks = 0; ks < kAhead; ++ks) read(ks);
+  for (int ks = 0; ks < kAhead; ++ks) read(ks, kk[ks]);
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) st[kt] = mfma32(kk[ks % kAhead][kt], q[ks], st[kt]);
     __builtin_amdgcn_sched_barrier(0);
-    if (ks + kAhead < 8) read(ks + kAhead);
+    if (ks + kAhead < 8) read(ks + kAhead, kk[ks % kAhead]);
   }
 }
-// o += V^T P^T, read(ks, x): the A operands of k-step ks.
+// o += V^T P^T; read(ks, x) reads the four A operands of k-step ks.
 template <class Read>
 __device__ __forceinline__ void wide_values(Running& r, const u32x4 (&pw)[4], Read read) {
   u32x4 vv[2][4];
@@ -570,18 +574,26 @@ __device__ __forceinline__ void wide_values(Running& r, const u32x4 (&pw)[4], Re
 // before, and the loads of those behind them start.  One step more ends with the last tile's
 // values.  The waves of a SIMD (w and w + 4) are half a step apart: while one has products,
 // the other has weights and stages.
+//   src.peek(e, f), src.look()       starts to read what is known: of tile e for logits(), of f
+//                                    for the loads after look(); both come long before their use
 //   src.load_k(e), src.load_v(e)     into registers
 //   src.put_k(to), src.put_v(e, to)  from there into LDS
 //   src.sees(e)                      the wave has rows that see keys of tile e
-//   src.logits(e, st)                what is left to do with raw logits, returns their scale
-//   src.values(e, ...)               the operands of the second product
+//   src.logits(e, st, vs)            what is left to do with raw logits; their scale, the values'
+//   src.read_v(from, ks, x)          the operands of the second product
+//   src.after(e, r)                  what is left to do after it
 template <class Source>
 __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ahead, const u32x4 (&q)[8], Running& r,
                                           const Shared& sm) {
+  src.peek(0, 0);
+  src.look();
   src.load_k(0);
   src.load_v(0);
+  src.peek(0, min(1, n - 1));
   src.put_k(sm.k);
+  src.look();
   src.load_k(min(1, n - 1));
+  src.peek(0, min(2, n - 1));
   __syncthreads();
   f32x16 st[2];
   u32x4 pw[4];
@@ -595,6 +607,7 @@ __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ah
     src.put_k(sm.k + c);           // (past the last tile: that again, in an array that is not read)
     src.put_v(e, sm.v + b);
     src.load_v(min(e + 1, n - 1));
+    src.look();
     src.load_k(min(e + 2, n - 1));
   };
 #pragma unroll 1
@@ -604,8 +617,17 @@ __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ah
       if (e > 0) weights(e - 1);
       if (e < n) stage(e, b, c);
     }
-    if (e > 0 && src.sees(e - 1)) src.values(e - 1, sm.v + c, r, pw);
-    if (e < n && src.sees(e)) wide_logits(sm.k + b, kbase, q, st);
+    const int kb = here(kbase), vb = here(src.vbase);
+    src.peek(min(e, n - 1), min(ahead ? e + 2 : e + 3, n - 1));
+    if (e > 0 && src.sees(e - 1)) {
+      wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) { src.read_v(sm.v + c, vb, ks, x); });
+      src.after(e - 1, r);
+    }
+    if (e < n && src.sees(e))
+      wide_logits(q, st, [&](int ks, u32x4 (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) x[kt] = *(const u32x4*)(sm.k + b + (kb ^ (32 * ks)) + 32 * kt * kRowBytes);
+      });
     if (ahead && e < n) {
       weights(e);
       stage(e, b, c);
@@ -617,32 +639,39 @@ __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ah
 struct PageSource {
   const BlockArgs& a;
   const PageRef* list;
-  int g, ex, tid, kput, vput, vbase;
+  LogitScale scale;
+  int g, tid, kput, vput, vbase;
   bool idle;
+  int page;                  // of the tile looked at last
   u32x4 kr, vr;
-  __device__ __forceinline__ u32x4 load(const int8_t* codes, int e) const {
-    const int page = __builtin_amdgcn_readfirstlane(list[e].page);
-    return *(const u32x4*)(codes + ((int64_t)page * a.H_kv + g) * kCodes + (uint32_t)(16 * tid));
+  PageRef known;             // its scales: of the tile whose logits are next
+  __device__ __forceinline__ void peek(int e, int f) {
+    known.ks = list[e].ks;
+    known.vs = list[e].vs;
+    known.page = list[f].page;
+  }
+  __device__ __forceinline__ void look() { page = __builtin_amdgcn_readfirstlane(known.page); }
+  __device__ __forceinline__ u32x4 load(const int8_t* codes, int p) const {
+    return *(const u32x4*)(codes + ((int64_t)p * a.H_kv + g) * kCodes + (uint32_t)(16 * tid));
   }
   __device__ __forceinline__ void put(const u32x4& x, uint8_t* to, int at) const {
     *(u32x4*)(to + at) = codes_bf16(x[0], x[1]);
     *(u32x4*)(to + (at ^ 16)) = codes_bf16(x[2], x[3]);
   }
-  __device__ __forceinline__ void load_k(int e) { kr = load(a.k_codes, e); }
-  __device__ __forceinline__ void load_v(int e) { vr = load(a.v_codes, e); }
+  __device__ __forceinline__ void load_k(int) { kr = load(a.k_codes, page); }
+  __device__ __forceinline__ void load_v(int) { vr = load(a.v_codes, page); }
   __device__ __forceinline__ void put_k(uint8_t* to) const { put(kr, to, kput); }
   __device__ __forceinline__ void put_v(int, uint8_t* to) const { put(vr, to, vput); }
   __device__ __forceinline__ bool sees(int) const { return !idle; }
-  __device__ __forceinline__ float logits(int e, f32x16 (&)[2], float& vs) const {
-    vs = list[e].vs;
-    return logit_scale(a, ex, list[e].ks);
+  __device__ __forceinline__ float logits(int, f32x16 (&)[2], float& vs) const {
+    vs = known.vs;
+    return scale(known.ks);
   }
-  __device__ __forceinline__ void values(int, const uint8_t* from, Running& r, const u32x4 (&pw)[4]) const {
-    wide_values(r, pw, [&](int ks, u32x4 (&y)[4]) __attribute__((always_inline)) {
+  __device__ __forceinline__ void read_v(const uint8_t* from, int at, int ks, u32x4 (&x)[4]) const {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = *(const u32x4*)(from + (vbase ^ (32 * ks)) + i * 32 * 2 * kBlk);
-    });
+    for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(from + (at ^ (32 * ks)) + i * 32 * 2 * kBlk);
   }
+  __device__ __forceinline__ void after(int, Running&) const {}
 };
 
 // The pages of tiles [lo, hi), all of whose keys every row sees.
@@ -651,7 +680,7 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
                                            int* scnt) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5, krow = key_of_row(lr);
-  PageSource src = {a, list, sg.g, ex, tid,
+  PageSource src = {a, list, logit_scale(a, ex), sg.g, tid,
                     (tid >> 3) * kRowBytes + 16 * ((2 * (tid & 7)) ^ swz_k(tid >> 3)),
                     (tid >> 2) * (2 * kBlk) + 16 * ((2 * (tid & 3)) ^ swz_c(tid >> 2)),
                     lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr)), idle};
@@ -685,8 +714,9 @@ struct RowSource {
   const BlockArgs& a;
   const ChunkStep& s;
   const Segment& sg;
-  int t0, ex, pos, wpos0, wpos1, last;   // last: the place's last position
-  int lane, wave, fr;
+  LogitScale scale;
+  int t0, pos, wpos0, wpos1, last;   // last: the place's last position
+  int lane, wave, fr, vbase;
   int (*sodd)[kWaves];
   u32x4 kr[2], vr[2];
   __device__ __forceinline__ void load(const uint16_t* tail, const uint16_t* rows, int64_t stride, int e,
@@ -731,25 +761,22 @@ struct RowSource {
           if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) st[kt][i] = -INFINITY;
     }
     vs = 1.f;
-    return logit_scale(a, ex, 1.f);
+    return scale(1.f);
   }
-  __device__ __forceinline__ void values(int e, const uint8_t* from, Running& r, const u32x4 (&pw)[4]) const {
-    int vbase[2];
+  // (chunks of keys 8 lh .. + 3 and of + 4 .. + 7 differ by the bit of 16 bytes in their swizzle)
+  __device__ __forceinline__ void read_v(const uint8_t* from, int at, int ks, u32x4 (&x)[4]) const {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int key = 8 * (lane >> 5) + 4 * j + ((lane >> 2) & 3);
-      vbase[j] = key * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(key)) + 8 * (lane & 1);
+    for (int i = 0; i < 4; ++i) {
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                    from + (at ^ (64 * i)) + 16 * ks * kRowBytes)));
+      const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                    from + (at ^ (64 * i) ^ 16) + (16 * ks + 4) * kRowBytes)));
+      x[i] = (u32x4){y[0], y[1], z[0], z[1]};
     }
-    wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                      from + (vbase[0] ^ (64 * i)) + 16 * ks * kRowBytes)));
-        const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                      from + (vbase[1] ^ (64 * i)) + 16 * ks * kRowBytes)));
-        x[i] = (u32x4){y[0], y[1], z[0], z[1]};
-      }
-    });
+  }
+  __device__ __forceinline__ void peek(int, int) const {}
+  __device__ __forceinline__ void look() const {}
+  __device__ __forceinline__ void after(int e, Running& r) const {
     int odd = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) odd |= sodd[e & 1][w];
@@ -776,8 +803,10 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
     // first and last position of the wave's rows
     const int wpos0 = sg.p.held + rt.pos0 + wave * 32 / a.gqa;
     const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + min(wave * 32 + 31, rt.n_rows - 1) / a.gqa;
-    const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr);
-    RowSource src = {a, s, sg, t0, ex, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4, sodd};
+    const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr), vkey = 8 * lh + ((lane >> 2) & 3);
+    RowSource src = {a, s, sg, logit_scale(a, ex), t0, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4,
+                     vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1),
+                     sodd};
     wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), wave < kWaves / 2, q, r, sm);
   }
 
