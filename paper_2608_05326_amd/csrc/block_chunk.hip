@@ -16,7 +16,7 @@ namespace qv {
 namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kChunkThreads = 512, kWaves = 8;
+constexpr int kWaves = kChunkWaves, kChunkThreads = 64 * kWaves;
 constexpr int kRowBytes = 2 * kHeadDim;
 // the running maximum is raised (and the output rescaled) only when a tile exceeds it by
 // this many powers of two: P stays below 256
@@ -72,7 +72,7 @@ __device__ __forceinline__ ChunkPlace lane_place(const BlockArgs& a, const Chunk
   const int i = min(place, a.B - 1);
   const int b = min(max(s.cu[i], 0), s.total), e = min(max(s.cu[i + 1], b), s.total);
   *start = b;
-  return chunk_place(place < a.B ? a.lens[i] : -1, e - b, a.gqa, a.max_context);
+  return chunk_place(place < a.B ? a.lens[i] : -1, e - b, a.gqa, a.H_kv, a.max_context);
 }
 __device__ __forceinline__ int64_t wave_scan(int64_t x) {   // inclusive
   const int lane = thread_here() & 63;
@@ -94,6 +94,7 @@ __device__ __forceinline__ int64_t lane_of(int64_t x, int lane) {
 struct Segment {
   ChunkPlace p;
   int seq, start, g, tile;   // start: the place's first row
+  int heads;                 // KV heads g .. of a place of solo row tiles (else 1)
   int64_t at;                // the row tile's start on the line
   int64_t from, to;
 };
@@ -130,13 +131,28 @@ __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end,
       g.seq = s0 + w;
       g.start = __builtin_amdgcn_readfirstlane(lp.start[w]);
       const int held = __builtin_amdgcn_readfirstlane(lp.held[w]), n = __builtin_amdgcn_readfirstlane(lp.n[w]);
-      g.p = chunk_place(held, n, a.gqa, a.max_context);
+      g.p = chunk_place(held, n, a.gqa, a.H_kv, a.max_context);
       g.p.per = __builtin_amdgcn_readfirstlane(g.p.per);       // (divisions leave them in vector registers)
       g.p.tiles = __builtin_amdgcn_readfirstlane(g.p.tiles);
       const int64_t pair = chunk_pair_cost(g.p), last = lane_of(lp.incl[w], 0);
       const int64_t first = last - pair * a.H_kv;
+      g.heads = 1;
       for (g.g = __builtin_amdgcn_readfirstlane(chunk_quotient(x - first, pair)); g.g < a.H_kv && x < end; ++g.g) {
         const int64_t at = first + g.g * pair;
+        if (g.p.solo && x == at && end - x >= 2 * pair) {   // whole KV heads, one to a wave
+          const int most = min(kWaves, a.H_kv - g.g);
+          g.heads = 1;
+          while (g.heads < most && end - x >= (g.heads + 1) * pair) ++g.heads;
+          g.tile = 0;
+          g.at = at;
+          g.from = 0;
+          g.to = pair;
+          f(g);
+          x += g.heads * pair;
+          g.g += g.heads - 1;
+          g.heads = 1;
+          continue;
+        }
         for (g.tile = __builtin_amdgcn_readfirstlane(chunk_tile_at(g.p, x - at)); g.tile < g.p.tiles && x < end; ++g.tile) {
           g.at = at + chunk_before(g.p, g.tile);
           const int64_t stop = min(end, g.at + chunk_cost(g.p, g.tile));
@@ -287,17 +303,41 @@ __device__ __forceinline__ void add_odd(Running& r, Row row, int n, int lh) {   
 
 // Keys (values) of position p of a place, a row in bf16: of the open block or of the chunk.
 __device__ __forceinline__ const uint16_t* fresh_row(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
-                                                     bool values, int p) {
+                                                     int g, bool values, int p) {
   if (p < sg.p.held)
-    return (values ? a.v_tail : a.k_tail) + ((int64_t)sg.seq * a.H_kv + sg.g) * kCodes + (p % kBlk) * kHeadDim;
+    return (values ? a.v_tail : a.k_tail) + ((int64_t)sg.seq * a.H_kv + g) * kCodes + (p % kBlk) * kHeadDim;
   const int64_t row = sg.start + (p - sg.p.held);
-  return values ? s.v + row * s.v_st + sg.g * s.v_sh : s.k + row * s.k_st + sg.g * s.k_sh;
+  return values ? s.v + row * s.v_st + g * s.v_sh : s.k + row * s.k_st + g * s.k_sh;
 }
+
+// A row's output (all lanes, the two halves of a row together; `there`: it is stored).
+__device__ __forceinline__ void store_row(const Running& r, uint16_t* row, bool there, int lh) {
+  const float inv = 1.f / r.l;
+  uint16_t* op = row + 8 * lh;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {   // channels 8 e .. 8 e + 15: eight to each lane half
+      uint32_t y[2], z[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(
+            pack_bf16(r.o[c][4 * e + 2 * j] * inv, r.o[c][4 * e + 2 * j + 1] * inv),
+            pack_bf16(r.o[c][4 * e + 4 + 2 * j] * inv, r.o[c][4 * e + 5 + 2 * j] * inv), false, false);
+        y[j] = sw[0];
+        z[j] = sw[1];
+      }
+      if (there) *(u32x4*)(op + 32 * c + 8 * e) = (u32x4){y[0], y[1], z[0], z[1]};
+    }
+}
+
+__device__ __forceinline__ int by_gqa(const ChunkStep& s, int row) { return (uint32_t)row * s.gqa_inv >> 16; }
 
 // Address of a row's output in `out`.
 __device__ __forceinline__ uint16_t* out_row(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
-                                             const RowTile& rt, int row) {
-  return s.out + (sg.start + rt.pos0 + row / a.gqa) * s.o_st + (sg.g * a.gqa + row % a.gqa) * s.o_sh;
+                                             const RowTile& rt, int g, int row) {
+  const int i = by_gqa(s, row);
+  return s.out + (sg.start + rt.pos0 + i) * s.o_st + (g * a.gqa + row - i * a.gqa) * s.o_sh;
 }
 
 // LDS of a workgroup, in two arrays: reads of one do not wait for the loads on their way into
@@ -316,30 +356,34 @@ __device__ __forceinline__ void dma16(const void* g, uint8_t* to) {
   __builtin_amdgcn_global_load_lds(g, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-// ---- few rows: RS sets of 32 rows, the other waves of a set take the key tiles in turn,
-// pages straight into registers
+// ---- few rows: a wave has 32 rows and pages of its own
 __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
                                            const RowTile& rt, int part, const Shared& sm, float2 (*sml)[32]) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  const int rs = sg.p.rows >> 5;                      // 1, 2 or 4
-  const int rw = wave & (rs - 1), kg = wave / rs, n_kg = kWaves / rs;
-  const int row = min(rw * 32 + lr, rt.n_rows - 1), i_row = rt.pos0 + row / a.gqa;
+  // sets of 32 rows (1, 2 or 4); the other waves of a set take the key tiles in turn.  Solo: a
+  // KV head to a wave.
+  const bool solo = sg.heads > 1;
+  const int log_rs = sg.p.rows == 32 ? 0 : sg.p.rows == 64 ? 1 : 2, rs = 1 << log_rs;
+  const int rw = wave & (rs - 1), kg = solo ? 0 : wave >> log_rs, n_kg = solo ? 1 : kWaves >> log_rs;
+  const bool idle = solo ? wave >= sg.heads : rw * 32 >= rt.n_rows;
+  const int g = solo && !idle ? sg.g + wave : sg.g;
+  const int row = min(rw * 32 + lr, rt.n_rows - 1), i_row = rt.pos0 + by_gqa(s, row);
+  const int head = g * a.gqa + row - (i_row - rt.pos0) * a.gqa;
   const int pos = sg.p.held + i_row;                  // this lane's position
   const int last = sg.p.held + sg.p.n - 1;            // the place's last position
-  const int n_blk = sg.p.held / kBlk, page_end = rw * 32 < rt.n_rows ? min(rt.hi, n_blk) : 0;
+  const int n_blk = sg.p.held / kBlk, page_end = idle ? 0 : min(rt.hi, n_blk);
   // page (-1: none) of block t0 + n_kg lane; the first look-up goes before the query's loads
   auto page_at = [&](int t0) { return t0 + lane * n_kg < page_end ? page_of(a, sg.seq, t0 + lane * n_kg) : -1; };
   int page = page_at(rt.lo + kg);
   u32x4 q[8];
-  const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + row % a.gqa) * s.q_sh, lh, q);
+  const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
   const LogitScale scale = logit_scale(a, ex);
   Running r;
   clear(r);
   // row lr of an A operand is this key of 32; a lane's logits st[i] are those of keys 16 lh + i
   const int krow = 16 * ((lr >> 2) & 1) + 4 * (lr >> 3) + (lr & 3);
 
-  const bool idle = rw * 32 >= rt.n_rows;
   uint8_t* const sk = sm.k + wave * kCodes;   // a page's keys [64][128] and values [128][64], codes
   uint8_t* const sv = sm.v + wave * kCodes;
   // A wave's load of 1 KB fills LDS in lane order.  16-byte chunks of a row are swizzled
@@ -356,10 +400,10 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
     uint64_t live = __ballot(page >= 0);
     if (!live) continue;
     if (page >= 0) {
-      ks_l = a.k_scale[(int64_t)page * a.H_kv + sg.g];
-      vs_l = a.v_scale[(int64_t)page * a.H_kv + sg.g];
+      ks_l = a.k_scale[(int64_t)page * a.H_kv + g];
+      vs_l = a.v_scale[(int64_t)page * a.H_kv + g];
     }
-    auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + sg.g) * kCodes; };
+    auto entry = [&](int j) { return ((int64_t)__builtin_amdgcn_readlane(page, j) * a.H_kv + g) * kCodes; };
     auto load_k = [&](int64_t e) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -432,7 +476,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   for (int t = first + (kg >= skip ? kg - skip : kg - skip + n_kg); !idle && t < rt.hi; t += n_kg)
 #pragma unroll 1
     for (int k0 = t * kBlk; k0 < t * kBlk + kBlk && k0 <= last; k0 += 32) {
-      auto at = [&](bool values, int key) { return fresh_row(a, s, sg, values, min(k0 + key, last)); };
+      auto at = [&](bool values, int key) { return fresh_row(a, s, sg, g, values, min(k0 + key, last)); };
       uint8_t* mine = sv;   // 32 rows of 256 bytes
       u32x4 vb[8], kb[8];
 #pragma unroll
@@ -476,8 +520,13 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 
-  // ---- join the waves of a row set
   r.l = half_sum(r.l);
+  if (solo) {
+    if (!idle) store_row(r, out_row(a, s, sg, rt, g, row), lr < rt.n_rows, lh);
+    __syncthreads();
+    return;
+  }
+  // ---- join the waves of a row set
   __syncthreads();
   sml[wave][lr] = make_float2(r.m, r.l);
 #pragma unroll
@@ -502,7 +551,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
       for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
     }
     if (rt.whole) {
-      *(u32x2*)(out_row(a, s, sg, rt, rr) + c) = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
+      *(u32x2*)(out_row(a, s, sg, rt, g, rr) + c) = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
     } else {
       const int64_t slot = (int64_t)chunk_slot(part, rt.lo) * s.slot_rows + rr;
       *(f32x4*)(s.part_o + slot * kHeadDim + c) = x;
@@ -781,7 +830,7 @@ struct RowSource {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) odd |= sodd[e & 1][w];
     if (__builtin_amdgcn_readfirstlane(odd))
-      add_odd(r, [&](int key) { return fresh_row(a, s, sg, true, (t0 + e) * kBlk + key); },
+      add_odd(r, [&](int key) { return fresh_row(a, s, sg, sg.g, true, (t0 + e) * kBlk + key); },
               min(kBlk, pos - (t0 + e) * kBlk + 1), lane >> 5);
   }
 };
@@ -791,18 +840,19 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
                                             int (*sodd)[kWaves], int* scnt) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  const int row = wave * 32 + lr, rowc = min(row, rt.n_rows - 1), i_row = rt.pos0 + rowc / a.gqa;
+  const int row = wave * 32 + lr, rowc = min(row, rt.n_rows - 1), i_row = rt.pos0 + by_gqa(s, rowc);
+  const int head = sg.g * a.gqa + rowc - (i_row - rt.pos0) * a.gqa;
   const bool idle = wave * 32 >= rt.n_rows;
   u32x4 q[8];
-  const int ex = load_query<true>(s.q + (sg.start + i_row) * s.q_st + (sg.g * a.gqa + rowc % a.gqa) * s.q_sh, lh, q);
+  const int ex = load_query<true>(s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
   Running r;
   clear(r);
   const int n_blk = sg.p.held / kBlk;
   if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, ex, q, r, sm, list, scnt);
   if (rt.hi > n_blk) {
     // first and last position of the wave's rows
-    const int wpos0 = sg.p.held + rt.pos0 + wave * 32 / a.gqa;
-    const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + min(wave * 32 + 31, rt.n_rows - 1) / a.gqa;
+    const int wpos0 = sg.p.held + rt.pos0 + by_gqa(s, wave * 32);
+    const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + by_gqa(s, min(wave * 32 + 31, rt.n_rows - 1));
     const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr), vkey = 8 * lh + ((lane >> 2) & 3);
     RowSource src = {a, s, sg, logit_scale(a, ex), t0, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4,
                      vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1),
@@ -812,23 +862,7 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
 
   r.l = half_sum(r.l);
   if (rt.whole) {
-    const float inv = 1.f / r.l;
-    uint16_t* op = out_row(a, s, sg, rt, rowc) + 8 * lh;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; e += 2) {   // channels 8 e .. 8 e + 15: eight to each lane half
-        uint32_t y[2], z[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const auto sw = __builtin_amdgcn_permlane32_swap(
-              pack_bf16(r.o[c][4 * e + 2 * j] * inv, r.o[c][4 * e + 2 * j + 1] * inv),
-              pack_bf16(r.o[c][4 * e + 4 + 2 * j] * inv, r.o[c][4 * e + 5 + 2 * j] * inv), false, false);
-          y[j] = sw[0];
-          z[j] = sw[1];
-        }
-        if (row < rt.n_rows) *(u32x4*)(op + 32 * c + 8 * e) = (u32x4){y[0], y[1], z[0], z[1]};
-      }
+    store_row(r, out_row(a, s, sg, rt, sg.g, rowc), row < rt.n_rows, lh);
   } else if (row < rt.n_rows) {
     const int64_t slot = (int64_t)chunk_slot(part, rt.lo) * s.slot_rows + row;
 #pragma unroll
@@ -856,14 +890,14 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   if (threadIdx.x == 0) s.joins[part].n_rows = 0;
   walk(a, begin, end, s, lp, [&](const Segment& sg) {
     RowTile rt;
-    rt.lo = chunk_key_tile(sg.from, sg.p.rows);
-    rt.hi = chunk_key_tile(sg.to, sg.p.rows);
+    rt.lo = chunk_key_tile(sg.from, sg.p.rows, sg.p.extra);
+    rt.hi = chunk_key_tile(sg.to, sg.p.rows, sg.p.extra);
     rt.pos0 = sg.tile * sg.p.per;
     rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
     if (thread_here() == 0 && sg.from > 0 && sg.from <= size) {   // the first part to begin inside it
       const int64_t stop = sg.at + chunk_cost(sg.p, sg.tile);
       s.joins[part] = {sg.at, stop, size, (int64_t)sg.start + rt.pos0, rt.n_rows, sg.p.rows,
-                       chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
+                       sg.p.extra, chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
     }
     if (rt.lo >= rt.hi) return;
     rt.whole = rt.lo == 0 && rt.hi == chunk_key_tiles(sg.p, sg.tile);
@@ -893,8 +927,8 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
 #pragma unroll
     for (int k = 0; k < kMergeRound; ++k) {
       const int i = min(i0 + k, jn.last);
-      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.rows);
-      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.rows);
+      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.rows, jn.extra);
+      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.rows, jn.extra);
       there[k] = i0 + k <= jn.last && lo < hi;
       if (lo == 0 && hi == jn.key_tiles) return;         // written by that part
       if (!there[k]) continue;
@@ -933,6 +967,7 @@ int64_t block_chunk_workspace_bytes(int64_t total, int gqa) {
 }
 
 hipError_t launch_chunk_attend(const BlockArgs& a, ChunkStep s, void* workspace, hipStream_t st) {
+  s.gqa_inv = (65536 + a.gqa - 1) / a.gqa;
   s.slot_rows = slot_rows(s.total, a.gqa);
   s.part_o = (float*)workspace;
   s.part_ml = (float2*)(s.part_o + (int64_t)2 * kChunkParts * s.slot_rows * kHeadDim);

@@ -13,30 +13,35 @@
 namespace qv {
 
 constexpr int kChunkParts = 256;    // one workgroup of eight waves to a compute unit
-constexpr int kChunkMin = 4096;     // the least a part is
+constexpr int kChunkMin = 1024;     // the least a part is
+constexpr int kSoloTiles = 16;      // key tiles that a wave takes alone (attend_few)
+constexpr int kChunkWaves = 8;
 
 // Rows of a workgroup for a place with this many in all.
 QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
-// What a key costs on the line, by rows, and a row tile beside its keys.
-QV_HD int chunk_weight(int rows) { return rows <= 128 ? 3 : 8; }
-QV_HD int chunk_extra(int rows) { return rows <= 128 ? 1536 : 3072; }
 
 struct ChunkPlace {
   int held, n;        // tokens held, new tokens (0: none)
   int rows, per;      // rows of a workgroup, positions of a row tile
   int tiles;          // row tiles of a KV head
+  int extra;          // length of a row tile on the line beside its keys'
+  bool solo;          // a row tile is one wave's: a workgroup takes up to eight KV heads at once
 };
 
 // A place with `len` tokens held that is given `rows` new ones; max_context limits both.
-QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, int max_context) {
+QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, int H_kv, int max_context) {
   ChunkPlace p;
   p.held = len;
   p.n = len < 0 || len >= max_context ? 0 : rows < max_context - len ? rows : max_context - len;
   p.rows = chunk_rows((int64_t)p.n * gqa);
   p.per = p.rows / gqa;
   p.tiles = (p.n + p.per - 1) / p.per;
+  p.solo = p.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
+  p.extra = p.rows > 128 ? 3072 : !p.solo ? 2304 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
   return p;
 }
+// log2 of what a key costs on the line, by the rows of its workgroup.
+QV_HD int chunk_weight(int rows) { return rows <= 128 ? 1 : 3; }
 
 // New tokens up to the end of row tile t.
 QV_HD int chunk_end(const ChunkPlace& p, int t) {
@@ -46,12 +51,12 @@ QV_HD int chunk_end(const ChunkPlace& p, int t) {
 
 // Length of row tile t on the line, and of the t row tiles before it.
 QV_HD int64_t chunk_cost(const ChunkPlace& p, int t) {
-  return ((int64_t)p.held + chunk_end(p, t)) * chunk_weight(p.rows) + chunk_extra(p.rows);
+  return (((int64_t)p.held + chunk_end(p, t)) << chunk_weight(p.rows)) + p.extra;
 }
 QV_HD int64_t chunk_before(const ChunkPlace& p, int t) {
   int64_t keys = (int64_t)t * p.held + (int64_t)p.per * t * (t + 1) / 2;
   if (t == p.tiles && t) keys -= (int64_t)p.tiles * p.per - p.n;
-  return keys * chunk_weight(p.rows) + (int64_t)t * chunk_extra(p.rows);
+  return (keys << chunk_weight(p.rows)) + (int64_t)t * p.extra;
 }
 QV_HD int64_t chunk_pair_cost(const ChunkPlace& p) { return chunk_before(p, p.tiles); }
 
@@ -74,15 +79,16 @@ QV_HD int chunk_quotient(int64_t x, int64_t y) {
   return q;
 }
 
+static_assert(kBlockTokens == 64, "key tiles");
 // Tiles of 64 keys that row tile t sees, and the first of them at or past point x of a row
-// tile of `rows` rows.
+// tile of a place with these rows and extra.
 QV_HD int chunk_key_tiles(const ChunkPlace& p, int t) {
   return (int)(((int64_t)p.held + chunk_end(p, t) + kBlockTokens - 1) / kBlockTokens);
 }
-QV_HD int chunk_key_tile(int64_t x, int rows) {
-  const int64_t y = x - chunk_extra(rows);
-  const int step = kBlockTokens * chunk_weight(rows);
-  return y <= 0 ? 0 : chunk_quotient(y + step - 1, step);
+QV_HD int chunk_key_tile(int64_t x, int rows, int extra) {
+  const int64_t y = x - extra;
+  const int shift = 6 + chunk_weight(rows);
+  return y <= 0 ? 0 : (int)((y + (1 << shift) - 1) >> shift);
 }
 
 // Length of a part, given the line's.

@@ -239,7 +239,8 @@ struct ChunkJoin {          // a row tile that several parts serve, by the first
   int64_t at, stop, size;   // the row tile on the line, the length of a part
   int64_t row;              // its first row of the packed tensors
   int32_t n_rows;           // (position, head) rows; 0: nothing to join
-  int32_t rows, key_tiles;  // rows of its workgroups, tiles of all its keys
+  int32_t rows, extra;      // of its place
+  int32_t key_tiles;        // of all its keys
   int32_t head, last;       // first query head, last part
 };
 
@@ -252,6 +253,7 @@ struct ChunkStep {          // attention of new tokens over the block cache and 
   const int32_t* cu;        // [B + 1] first row of each place, then the end of the last
   int32_t total;
   int32_t slot_rows;        // rows of a partial result
+  uint32_t gqa_inv;         // 2^16 / gqa, rounded up: (r gqa_inv) >> 16 is r / gqa for r < 256
   float* part_o;            // [2 parts][slot_rows][d]
   float2* part_ml;          // [2 parts][slot_rows] (maximum in log2 units, sum)
   ChunkJoin* joins;         // [parts]
