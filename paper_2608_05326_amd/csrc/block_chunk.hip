@@ -361,10 +361,10 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
                                            const RowTile& rt, int part, const Shared& sm, float2 (*sml)[32]) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  // sets of 32 rows (1, 2 or 4); the other waves of a set take the key tiles in turn.  Solo: a
+  // one or two sets of 32 rows; the other waves of a set take the key tiles in turn.  Solo: a
   // KV head to a wave.
   const bool solo = sg.heads > 1;
-  const int log_rs = sg.p.rows == 32 ? 0 : sg.p.rows == 64 ? 1 : 2, rs = 1 << log_rs;
+  const int log_rs = sg.p.rows == 32 ? 0 : 1, rs = 1 << log_rs;
   const int rw = wave & (rs - 1), kg = solo ? 0 : wave >> log_rs, n_kg = solo ? 1 : kWaves >> log_rs;
   const bool idle = solo ? wave >= sg.heads : rw * 32 >= rt.n_rows;
   const int g = solo && !idle ? sg.g + wave : sg.g;

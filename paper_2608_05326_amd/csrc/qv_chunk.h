@@ -18,7 +18,7 @@ constexpr int kSoloTiles = 16;      // key tiles that a wave takes alone (attend
 constexpr int kChunkWaves = 8;
 
 // Rows of a workgroup for a place with this many in all.
-QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 256; }
 
 struct ChunkPlace {
   int held, n;        // tokens held, new tokens (0: none)
@@ -37,11 +37,11 @@ QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, int H_kv, int max_conte
   p.per = p.rows / gqa;
   p.tiles = (p.n + p.per - 1) / p.per;
   p.solo = p.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
-  p.extra = p.rows > 128 ? 3072 : !p.solo ? 2304 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
+  p.extra = p.rows > 64 ? 3072 : !p.solo ? 2304 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
   return p;
 }
 // log2 of what a key costs on the line, by the rows of its workgroup.
-QV_HD int chunk_weight(int rows) { return rows <= 128 ? 1 : 3; }
+QV_HD int chunk_weight(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 3; }
 
 // New tokens up to the end of row tile t.
 QV_HD int chunk_end(const ChunkPlace& p, int t) {
