@@ -136,30 +136,23 @@ __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end,
       g.p.tiles = __builtin_amdgcn_readfirstlane(g.p.tiles);
       const int64_t pair = chunk_pair_cost(g.p), last = lane_of(lp.incl[w], 0);
       const int64_t first = last - pair * a.H_kv;
-      g.heads = 1;
-      for (g.g = __builtin_amdgcn_readfirstlane(chunk_quotient(x - first, pair)); g.g < a.H_kv && x < end; ++g.g) {
+      // a KV head at a time; of a place of solo row tiles, up to eight whole ones, one to a wave
+      for (g.g = __builtin_amdgcn_readfirstlane(chunk_quotient(x - first, pair)); g.g < a.H_kv && x < end;
+           g.g += g.heads) {
         const int64_t at = first + g.g * pair;
-        if (g.p.solo && x == at && end - x >= 2 * pair) {   // whole KV heads, one to a wave
+        g.heads = 1;
+        if (g.p.solo && x == at) {
           const int most = min(kWaves, a.H_kv - g.g);
-          g.heads = 1;
           while (g.heads < most && end - x >= (g.heads + 1) * pair) ++g.heads;
-          g.tile = 0;
-          g.at = at;
-          g.from = 0;
-          g.to = pair;
-          f(g);
-          x += g.heads * pair;
-          g.g += g.heads - 1;
-          g.heads = 1;
-          continue;
         }
-        for (g.tile = __builtin_amdgcn_readfirstlane(chunk_tile_at(g.p, x - at)); g.tile < g.p.tiles && x < end; ++g.tile) {
+        for (g.tile = __builtin_amdgcn_readfirstlane(chunk_tile_at(g.p, x - at)); g.tile < g.p.tiles && x < end;
+             ++g.tile) {
           g.at = at + chunk_before(g.p, g.tile);
           const int64_t stop = min(end, g.at + chunk_cost(g.p, g.tile));
           g.from = x - g.at;
           g.to = stop - g.at;
           f(g);
-          x = stop;
+          x = g.heads > 1 ? at + g.heads * pair : stop;
         }
       }
     }
@@ -242,35 +235,55 @@ __device__ __forceinline__ void clear(Running& r) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) r.o[c][i] = 0.f;
 }
-// Weights exp2(st sc - m), in bf16 with the values' scale vs; m, l and o are kept.
+// The largest of a row's logits, in log2 units.
 template <int KT>
-__device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float sc, float vs, u32x4 (&pw)[2 * KT]) {
+__device__ __forceinline__ float largest(const f32x16 (&st)[KT], float sc) {
   float mt = -INFINITY;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) mt = fmaxf(mt, st[kt][i]);
-  mt = half_max(mt) * sc;
-  if (__any(mt > r.m + kLazy)) {
-    const float mn = fmaxf(r.m, mt);
-    const float al = r.m == mn ? 1.f : __builtin_amdgcn_exp2f(r.m - mn);
-    r.m = mn;
-    r.l *= al;
+  return half_max(mt) * sc;
+}
+__device__ __forceinline__ bool exceeds(const Running& r, float mt) { return __any(mt > r.m + kLazy); }
+// Raises the reference above mt (all rows of the wave at once) by a whole power of two, and
+// rescales: exact, also of weights in bf16 whose values are still to be added.
+template <int N>
+__device__ __forceinline__ void raise(Running& r, float mt, u32x4 (&pw)[N]) {
+  const float up = fmaxf(ceilf(mt - r.m), 0.f);                   // (infinite from the first: m = mt)
+  const float al = __builtin_amdgcn_exp2f(-up);
+  r.m = mt > r.m ? (r.m > -INFINITY ? r.m + up : mt) : r.m;
+  r.l *= al;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+  for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) r.o[c][i] *= al;
-  }
-  const float mu = r.m > -INFINITY ? r.m : 0.f;
+    for (int i = 0; i < 16; ++i) r.o[c][i] *= al;
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
+  for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const float e0 = __builtin_amdgcn_exp2f(fmaf(st[kt][i], sc, -mu));
-      const float e1 = __builtin_amdgcn_exp2f(fmaf(st[kt][i + 1], sc, -mu));
-      r.l += e0 + e1;
-      pw[2 * kt + (i >> 3)][(i & 7) >> 1] = pack_bf16(e0 * vs, e1 * vs);
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = pw[i][j];
+      pw[i][j] = pack_bf16(lo_f32(w) * al, hi_f32(w) * al);
     }
+}
+// Weights exp2(st sc - m) of a k-step, in bf16 with the values' scale vs.
+template <int KT>
+__device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float sc, float vs, int ks, u32x4& pw) {
+  const float mu = r.m > -INFINITY ? r.m : 0.f;
+  float e[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(st[ks >> 1][8 * (ks & 1) + i], sc, -mu));
+  r.l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) pw[i] = pack_bf16(e[2 * i] * vs, e[2 * i + 1] * vs);
+}
+template <int KT>
+__device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float sc, float vs, u32x4 (&pw)[2 * KT]) {
+  const float mt = largest<KT>(st, sc);
+  u32x4 none[1] = {};
+  if (exceeds(r, mt)) raise(r, mt, none);
+#pragma unroll
+  for (int ks = 0; ks < 2 * KT; ++ks) weigh<KT>(r, st, sc, vs, ks, pw[ks]);
 }
 
 // A value that is not finite must not reach a row that its key is masked for, through
@@ -581,107 +594,166 @@ __device__ __forceinline__ int swz_c(int channel) { return (channel >> 1) & 7; }
 __device__ __forceinline__ int key_of_row(int lr) {
   return 16 * (lr >> 4) + 8 * ((lr >> 2) & 1) + 4 * ((lr >> 3) & 1) + (lr & 3);
 }
-// st = K Q^T of a staged tile; read(ks, x) reads the two A operands of k-step ks.  Operands are
-// read three steps ahead of their products: a read takes longer than the products of one step.
-template <class Read>
-__device__ __forceinline__ void wide_logits(const u32x4 (&q)[8], f32x16 (&st)[2], Read read) {
-  constexpr int kAhead = 3;
-  u32x4 kk[kAhead][2];
+// The order in which what stands between two scheduling barriers is issued: a product, then
+// LDS reads, vector instructions and exponentials beside it, n times over.  A wave issues in
+// order, and a product keeps the matrix unit for eight issue slots: what does not stand
+// between two products waits for all of them.
+template <int N, int READS, int VALU, int TRANS>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (READS) __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    if constexpr (VALU) __builtin_amdgcn_sched_group_barrier(0x002, VALU, 0);
+    if constexpr (TRANS) __builtin_amdgcn_sched_group_barrier(0x400, TRANS, 0);
+  }
+}
+// Operands on their way from LDS: read kAhead ahead of their products, since a read takes longer
+// than some products.
+constexpr int kAhead = 5;
+struct Operands {
+  u32x4 x[kAhead + 1];
+};
+// st = K Q^T of a staged tile; read(n) reads operand n: keys 32 (n % 2) .. of k-step n / 2.
+// beside(ks) goes with the products of k-step ks.
+template <class Read, class Beside>
+__device__ __forceinline__ void wide_logits(const u32x4 (&q)[8], f32x16 (&st)[2], Read read, Beside beside) {
+  Operands k;
 #pragma unroll
   for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) st[kt][i] = 0.f;
 #pragma unroll
-  for (int ks = 0; ks < kAhead; ++ks) read(ks, kk[ks]);
+  for (int n = 0; n < kAhead; ++n) k.x[n] = read(n);
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks) {
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt) st[kt] = mfma32(kk[ks % kAhead][kt], q[ks], st[kt]);
+    for (int kt = 0; kt < 2; ++kt) {
+      const int n = 2 * ks + kt;
+      if (n + kAhead < 16) k.x[(n + kAhead) % (kAhead + 1)] = read(n + kAhead);
+      st[kt] = mfma32(k.x[n % (kAhead + 1)], q[ks], st[kt]);
+    }
+    beside(ks);
+    interleave<2, 1, 7, 0>();
     __builtin_amdgcn_sched_barrier(0);
-    if (ks + kAhead < 8) read(ks + kAhead, kk[ks % kAhead]);
   }
 }
-// o += V^T P^T; read(ks, x) reads the four A operands of k-step ks.
-template <class Read>
-__device__ __forceinline__ void wide_values(Running& r, const u32x4 (&pw)[4], Read read) {
-  u32x4 vv[2][4];
-  read(0, vv[0]);
+// o += V^T P^T; read(n) reads operand n: channels 32 (n % 4) .. of k-step n / 4; beside(ks) goes
+// with the products of k-step ks and may change pw[ks].
+template <class Read, class Beside>
+__device__ __forceinline__ void wide_values(Running& r, u32x4 (&pw)[4], Read read, Beside beside) {
+  Operands v;
+#pragma unroll
+  for (int n = 0; n < kAhead; ++n) v.x[n] = read(n);
 #pragma unroll
   for (int ks = 0; ks < 4; ++ks) {
-    if (ks < 3) read(ks + 1, vv[(ks + 1) & 1]);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int c = 0; c < 4; ++c) r.o[c] = mfma32(vv[ks & 1][c], pw[ks], r.o[c]);
+    for (int c = 0; c < 4; ++c) {
+      const int n = 4 * ks + c;
+      if (n + kAhead < 16) v.x[(n + kAhead) % (kAhead + 1)] = read(n + kAhead);
+      r.o[c] = mfma32(v.x[n % (kAhead + 1)], pw[ks], r.o[c]);
+    }
+    beside(ks);
+    interleave<4, 1, 7, 2>();
     __builtin_amdgcn_sched_barrier(0);
   }
 }
 
 // Key tiles 0 .. n - 1 of a source (pages or rows in bf16).  Step e of the loop: the products
-// of the values of the tile before and of its own keys, then its weights; meanwhile the next
-// tile's keys and its own values are put into the arrays that were last read in the step
-// before, and the loads of those behind them start.  One step more ends with the last tile's
-// values.  The waves of a SIMD (w and w + 4) are half a step apart: while one has products,
-// the other has weights and stages.
+// of tile e's keys, and beside them the next tile's keys and its own values are put into the
+// arrays that were last read in the step before and the loads of those behind them start; then
+// the products of the values of the tile before, and beside them the weights of tile e.  One step more ends with the last tile's values.
 //   src.peek(e, f), src.look()       starts to read what is known: of tile e for logits(), of f
 //                                    for the loads after look(); both come long before their use
 //   src.load_k(e), src.load_v(e)     into registers
-//   src.put_k(to), src.put_v(e, to)  from there into LDS
-//   src.sees(e)                      the wave has rows that see keys of tile e
+//   src.put_k(i, to), src.put_v(i, e, to)   half i of it from there into LDS
+//   src.sees(n)                      of n tiles, how many hold keys that a row of the wave sees
 //   src.logits(e, st, vs)            what is left to do with raw logits; their scale, the values'
-//   src.read_v(from, ks, x)          the operands of the second product
+//   src.read_v(from, at, ks, c)      an operand of the second product
 //   src.after(e, r)                  what is left to do after it
 template <class Source>
-__device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, bool ahead, const u32x4 (&q)[8], Running& r,
+__device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, const u32x4 (&q)[8], Running& r,
                                           const Shared& sm) {
   src.peek(0, 0);
   src.look();
   src.load_k(0);
   src.load_v(0);
   src.peek(0, min(1, n - 1));
-  src.put_k(sm.k);
+  src.put_k(0, sm.k);
+  src.put_k(1, sm.k);
   src.look();
   src.load_k(min(1, n - 1));
   src.peek(0, min(2, n - 1));
   __syncthreads();
-  f32x16 st[2];
   u32x4 pw[4];
-  auto weights = [&](int e) __attribute__((always_inline)) {
-    if (!src.sees(e)) return;
-    float vs;
-    const float sc = src.logits(e, st, vs);
-    weigh<2>(r, st, sc, vs, pw);
-  };
-  auto stage = [&](int e, int b, int c) __attribute__((always_inline)) {
-    src.put_k(sm.k + c);           // (past the last tile: that again, in an array that is not read)
-    src.put_v(e, sm.v + b);
-    src.load_v(min(e + 1, n - 1));
-    src.look();
-    src.load_k(min(e + 2, n - 1));
-  };
-#pragma unroll 1
-  for (int e = 0; e <= n; ++e) {
-    const int b = (e & 1) * kTileBytes, c = b ^ kTileBytes;
-    if (!ahead) {
-      if (e > 0) weights(e - 1);
-      if (e < n) stage(e, b, c);
+  // in six parts (past the last tile: that again, in an array that is not read)
+  auto stage = [&](int e, int b, int c, int part) __attribute__((always_inline)) {
+    if (part < 2) src.put_k(part, sm.k + c);
+    else if (part < 4) src.put_v(part - 2, e, sm.v + b);
+    else if (part == 4) src.load_v(min(e + 1, n - 1));
+    else if (part == 5) {
+      src.look();
+      src.load_k(min(e + 2, n - 1));
     }
-    const int kb = here(kbase), vb = here(src.vbase);
-    src.peek(min(e, n - 1), min(ahead ? e + 2 : e + 3, n - 1));
-    if (e > 0 && src.sees(e - 1)) {
-      wide_values(r, pw, [&](int ks, u32x4 (&x)[4]) __attribute__((always_inline)) { src.read_v(sm.v + c, vb, ks, x); });
-      src.after(e - 1, r);
-    }
-    if (e < n && src.sees(e))
-      wide_logits(q, st, [&](int ks, u32x4 (&x)[2]) __attribute__((always_inline)) {
+  };
+  auto logits = [&](int e, int b, int c, f32x16 (&st)[2]) __attribute__((always_inline)) {
+    const int kb = here(kbase);
+    wide_logits(
+        q, st,
+        [&](int i) __attribute__((always_inline)) {
+          return *(const u32x4*)(sm.k + b + (kb ^ (32 * (i >> 1))) + 32 * (i & 1) * kRowBytes);
+        },
+        [&](int ks) __attribute__((always_inline)) { stage(e, b, c, ks); });
+  };
+  auto known = [&](int e) __attribute__((always_inline)) { src.peek(min(e + 1, n - 1), min(e + 3, n - 1)); };
+  auto stage_all = [&](int e) __attribute__((always_inline)) {
+    const int b = (e & 1) * kTileBytes;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) x[kt] = *(const u32x4*)(sm.k + b + (kb ^ (32 * ks)) + 32 * kt * kRowBytes);
-      });
-    if (ahead && e < n) {
-      weights(e);
-      stage(e, b, c);
+    for (int part = 0; part < 6; ++part) stage(e, b, b ^ kTileBytes, part);
+    known(e);
+  };
+  auto read_v = [&](int e, int at, int i) __attribute__((always_inline)) {
+    return src.read_v(sm.v + (e & 1) * kTileBytes, at, i >> 2, i & 3);
+  };
+  // Every wave comes to n + 1 barriers: one after each step (the last one before the arrays are
+  // written again).
+  const int seen = src.sees(n);
+  int e = 0;
+  if (seen > 0) {
+    f32x16 st[2];
+    logits(0, 0, kTileBytes, st);
+    float vs;
+    const float sc = src.logits(0, st, vs);
+    known(0);
+    weigh<2>(r, st, sc, vs, pw);
+    __syncthreads();
+#pragma unroll 1
+    for (e = 1; e < seen; ++e) {
+      const int b = (e & 1) * kTileBytes, vb = here(src.vbase);
+      logits(e, b, b ^ kTileBytes, st);
+      const float sc = src.logits(e, st, vs), mt = largest<2>(st, sc);
+      known(e);
+      if (exceeds(r, mt)) raise(r, mt, pw);
+      wide_values(
+          r, pw, [&](int i) __attribute__((always_inline)) { return read_v(e - 1, vb, i); },
+          [&](int ks) __attribute__((always_inline)) { weigh<2>(r, st, sc, vs, ks, pw[ks]); });
+      src.after(e - 1, r);
+      __syncthreads();
     }
-    __syncthreads();   // (the last one before the arrays are written again)
+    if (e < n) stage_all(e);
+    const int vb = here(src.vbase);
+    wide_values(
+        r, pw, [&](int i) __attribute__((always_inline)) { return read_v(e - 1, vb, i); }, [](int) {});
+    src.after(e - 1, r);
+    __syncthreads();
+    ++e;
+  }
+#pragma unroll 1
+  for (; e <= n; ++e) {
+    if (e < n) stage_all(e);
+    __syncthreads();
   }
 }
 
@@ -703,22 +775,20 @@ struct PageSource {
   __device__ __forceinline__ u32x4 load(const int8_t* codes, int p) const {
     return *(const u32x4*)(codes + ((int64_t)p * a.H_kv + g) * kCodes + (uint32_t)(16 * tid));
   }
-  __device__ __forceinline__ void put(const u32x4& x, uint8_t* to, int at) const {
-    *(u32x4*)(to + at) = codes_bf16(x[0], x[1]);
-    *(u32x4*)(to + (at ^ 16)) = codes_bf16(x[2], x[3]);
+  __device__ __forceinline__ void put(const u32x4& x, uint8_t* to, int at, int i) const {
+    *(u32x4*)(to + (at ^ (16 * i))) = codes_bf16(x[2 * i], x[2 * i + 1]);
   }
   __device__ __forceinline__ void load_k(int) { kr = load(a.k_codes, page); }
   __device__ __forceinline__ void load_v(int) { vr = load(a.v_codes, page); }
-  __device__ __forceinline__ void put_k(uint8_t* to) const { put(kr, to, kput); }
-  __device__ __forceinline__ void put_v(int, uint8_t* to) const { put(vr, to, vput); }
-  __device__ __forceinline__ bool sees(int) const { return !idle; }
+  __device__ __forceinline__ void put_k(int i, uint8_t* to) const { put(kr, to, kput, i); }
+  __device__ __forceinline__ void put_v(int i, int, uint8_t* to) const { put(vr, to, vput, i); }
+  __device__ __forceinline__ int sees(int n) const { return idle ? 0 : n; }
   __device__ __forceinline__ float logits(int, f32x16 (&)[2], float& vs) const {
     vs = known.vs;
     return scale(known.ks);
   }
-  __device__ __forceinline__ void read_v(const uint8_t* from, int at, int ks, u32x4 (&x)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(from + (at ^ (32 * ks)) + i * 32 * 2 * kBlk);
+  __device__ __forceinline__ u32x4 read_v(const uint8_t* from, int at, int ks, int c) const {
+    return *(const u32x4*)(from + (at ^ (32 * ks)) + c * 32 * 2 * kBlk);
   }
   __device__ __forceinline__ void after(int, Running&) const {}
 };
@@ -753,7 +823,7 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
     n = __builtin_amdgcn_readfirstlane(n);
     if (x.page >= 0) list[at] = x;
     __syncthreads();
-    if (n) wide_loop(src, n, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), wave < kWaves / 2, q, r, sm);
+    if (n) wide_loop(src, n, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), q, r, sm);
   }
 }
 
@@ -766,7 +836,7 @@ struct RowSource {
   LogitScale scale;
   int t0, pos, wpos0, wpos1, last;   // last: the place's last position
   int lane, wave, fr, vbase;
-  int (*sodd)[kWaves];
+  int (*sodd)[2 * kWaves];
   u32x4 kr[2], vr[2];
   __device__ __forceinline__ void load(const uint16_t* tail, const uint16_t* rows, int64_t stride, int e,
                                        u32x4 (&x)[2]) const {
@@ -783,22 +853,15 @@ struct RowSource {
   __device__ __forceinline__ int64_t tail() const { return ((int64_t)sg.seq * a.H_kv + sg.g) * kCodes; }
   __device__ __forceinline__ void load_k(int e) { load(a.k_tail + tail(), s.k + sg.g * s.k_sh, s.k_st, e, kr); }
   __device__ __forceinline__ void load_v(int e) { load(a.v_tail + tail(), s.v + sg.g * s.v_sh, s.v_st, e, vr); }
-  __device__ __forceinline__ void put_k(uint8_t* to) const {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_k(fr))) = kr[i];
+  __device__ __forceinline__ void put_k(int i, uint8_t* to) const {
+    *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_k(fr))) = kr[i];
   }
-  __device__ __forceinline__ void put_v(int e, uint8_t* to) {
-    bool odd = false;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      odd |= take_out(vr[i]);
-      *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_v(fr))) = vr[i];
-    }
-    const int any = __any(odd);
-    if (lane == 0) sodd[e & 1][wave] = any;
+  __device__ __forceinline__ void put_v(int i, int e, uint8_t* to) {
+    const int odd = __any(take_out(vr[i]));
+    *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_v(fr))) = vr[i];
+    if (lane == 0) sodd[e & 1][2 * wave + i] = odd;
   }
-  __device__ __forceinline__ bool sees(int e) const { return (t0 + e) * kBlk <= wpos1; }
+  __device__ __forceinline__ int sees(int n) const { return min(n, max((wpos1 >> 6) - t0 + 1, 0)); }
   __device__ __forceinline__ float logits(int e, f32x16 (&st)[2], float& vs) const {
     const int p0 = (t0 + e) * kBlk;
     if (p0 + kBlk - 1 > wpos0) {
@@ -813,22 +876,19 @@ struct RowSource {
     return scale(1.f);
   }
   // (chunks of keys 8 lh .. + 3 and of + 4 .. + 7 differ by the bit of 16 bytes in their swizzle)
-  __device__ __forceinline__ void read_v(const uint8_t* from, int at, int ks, u32x4 (&x)[4]) const {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                    from + (at ^ (64 * i)) + 16 * ks * kRowBytes)));
-      const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
-                                                    from + (at ^ (64 * i) ^ 16) + (16 * ks + 4) * kRowBytes)));
-      x[i] = (u32x4){y[0], y[1], z[0], z[1]};
-    }
+  __device__ __forceinline__ u32x4 read_v(const uint8_t* from, int at, int ks, int c) const {
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                  from + (at ^ (64 * c)) + 16 * ks * kRowBytes)));
+    const u32x2 z = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(
+                                                  from + (at ^ (64 * c) ^ 16) + (16 * ks + 4) * kRowBytes)));
+    return (u32x4){y[0], y[1], z[0], z[1]};
   }
   __device__ __forceinline__ void peek(int, int) const {}
   __device__ __forceinline__ void look() const {}
   __device__ __forceinline__ void after(int e, Running& r) const {
     int odd = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) odd |= sodd[e & 1][w];
+    for (int w = 0; w < 2 * kWaves; ++w) odd |= sodd[e & 1][w];
     if (__builtin_amdgcn_readfirstlane(odd))
       add_odd(r, [&](int key) { return fresh_row(a, s, sg, sg.g, true, (t0 + e) * kBlk + key); },
               min(kBlk, pos - (t0 + e) * kBlk + 1), lane >> 5);
@@ -837,7 +897,7 @@ struct RowSource {
 
 __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep& s, const Segment& sg,
                                             const RowTile& rt, int part, const Shared& sm, PageRef* list,
-                                            int (*sodd)[kWaves], int* scnt) {
+                                            int (*sodd)[2 * kWaves], int* scnt) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int row = wave * 32 + lr, rowc = min(row, rt.n_rows - 1), i_row = rt.pos0 + by_gqa(s, rowc);
@@ -857,7 +917,7 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
     RowSource src = {a, s, sg, logit_scale(a, ex), t0, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4,
                      vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1),
                      sodd};
-    wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), wave < kWaves / 2, q, r, sm);
+    wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), q, r, sm);
   }
 
   r.l = half_sum(r.l);
@@ -881,7 +941,7 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   const Shared sm = {lds_k, lds_v};
   __shared__ float2 sml[kWaves][32];
   __shared__ PageRef list[kList];
-  __shared__ int sodd[2][kWaves], scnt[kWaves];
+  __shared__ int sodd[2][2 * kWaves], scnt[kWaves];
   __shared__ LinePlaces lp;
   // parts of one KV head on one XCD (workgroup i runs on XCD i % 8)
   const int part = (blockIdx.x & 7) * (kChunkParts / 8) + (blockIdx.x >> 3);
