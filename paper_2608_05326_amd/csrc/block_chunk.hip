@@ -43,9 +43,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   const bf16x2 p = {(__bf16)lo, (__bf16)hi};
   return __builtin_bit_cast(uint32_t, p);
 }
-__device__ __forceinline__ bool nonfinite(uint32_t x) {   // of two bf16
-  return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u;
-}
 // four codes in bf16, where they are exact
 __device__ __forceinline__ u32x2 codes_bf16(uint32_t w) {
   float f[4];
@@ -289,16 +286,19 @@ __device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float 
 // A value that is not finite must not reach a row that its key is masked for, through
 // 0 * infinity: such values of rows in bf16 are left out of the products, and added to the
 // rows that see them afterwards.
+// (take_out: whether any lane of the wave held one.)
 __device__ __forceinline__ bool take_out(u32x4& x) {
-  bool odd = false;
+  // exponents of ones: 0x7F80 + 0x80 in either half
+  uint32_t bad = 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (nonfinite(x[j])) {
-      odd = true;
-      if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
-      if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
-    }
-  return odd;
+  for (int j = 0; j < 4; ++j) bad |= (x[j] & 0x7F807F80u) + 0x00800080u;
+  if (!__any(bad & 0x80008000u)) return false;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if ((x[j] & 0x7F80u) == 0x7F80u) x[j] &= 0xFFFF0000u;
+    if ((x[j] & 0x7F800000u) == 0x7F800000u) x[j] &= 0xFFFFu;
+  }
+  return true;
 }
 template <class Row>
 __device__ __forceinline__ void add_odd(Running& r, Row row, int n, int lh) {   // rows 0 .. n - 1 are seen
@@ -529,7 +529,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
           }
           r.o[c] = mfma32(x, pr[ks], r.o[c]);
         }
-      if (__any(odd)) add_odd(r, [&](int key) { return at(true, key); }, min(32, pos - k0 + 1), lh);
+      if (odd) add_odd(r, [&](int key) { return at(true, key); }, min(32, pos - k0 + 1), lh);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
 
@@ -842,11 +842,17 @@ struct RowSource {
                                        u32x4 (&x)[2]) const {
     const int p0 = (t0 + e) * kBlk, c = 16 * (lane & 15);
     const uint8_t* from = (const uint8_t*)(rows + ((int64_t)sg.start + p0 - sg.p.held) * stride);
+    if (p0 >= sg.p.held && p0 + kBlk - 1 <= last) {
+      const uint32_t off = (uint32_t)fr * (uint32_t)(2 * stride) + c;
+      x[0] = *(const u32x4*)(from + off);
+      x[1] = *(const u32x4*)(from + 64 * stride + off);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int key = min(fr + 32 * i, last - p0);         // (past the last: that again, masked)
       const uint8_t* at = from + (uint32_t)((uint32_t)key * (uint32_t)(2 * stride) + c);
-      if (p0 < sg.p.held && p0 + key < sg.p.held) at = (const uint8_t*)tail + key * kRowBytes + c;
+      if (p0 + key < sg.p.held) at = (const uint8_t*)tail + key * kRowBytes + c;
       x[i] = *(const u32x4*)at;
     }
   }
@@ -857,7 +863,7 @@ struct RowSource {
     *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_k(fr))) = kr[i];
   }
   __device__ __forceinline__ void put_v(int i, int e, uint8_t* to) {
-    const int odd = __any(take_out(vr[i]));
+    const int odd = take_out(vr[i]);
     *(u32x4*)(to + (fr + 32 * i) * kRowBytes + 16 * ((lane & 15) ^ swz_v(fr))) = vr[i];
     if (lane == 0) sodd[e & 1][2 * wave + i] = odd;
   }
