@@ -377,7 +377,7 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   // one or two sets of 32 rows; the other waves of a set take the key tiles in turn.  Solo: a
   // KV head to a wave.
   const bool solo = sg.heads > 1;
-  const int log_rs = sg.p.rows == 32 ? 0 : 1, rs = 1 << log_rs;
+  const int log_rs = sg.p.c.rows == 32 ? 0 : 1, rs = 1 << log_rs;
   const int rw = wave & (rs - 1), kg = solo ? 0 : wave >> log_rs, n_kg = solo ? 1 : kWaves >> log_rs;
   const bool idle = solo ? wave >= sg.heads : rw * 32 >= rt.n_rows;
   const int g = solo && !idle ? sg.g + wave : sg.g;
@@ -892,10 +892,7 @@ struct RowSource {
   __device__ __forceinline__ void peek(int, int) const {}
   __device__ __forceinline__ void look() const {}
   __device__ __forceinline__ void after(int e, Running& r) const {
-    int odd = 0;
-#pragma unroll
-    for (int w = 0; w < 2 * kWaves; ++w) odd |= sodd[e & 1][w];
-    if (__builtin_amdgcn_readfirstlane(odd))
+    if (__any(sodd[e & 1][lane & (2 * kWaves - 1)]))
       add_odd(r, [&](int key) { return fresh_row(a, s, sg, sg.g, true, (t0 + e) * kBlk + key); },
               min(kBlk, pos - (t0 + e) * kBlk + 1), lane >> 5);
   }
@@ -956,18 +953,18 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   if (threadIdx.x == 0) s.joins[part].n_rows = 0;
   walk(a, begin, end, s, lp, [&](const Segment& sg) {
     RowTile rt;
-    rt.lo = chunk_key_tile(sg.from, sg.p.rows, sg.p.extra);
-    rt.hi = chunk_key_tile(sg.to, sg.p.rows, sg.p.extra);
+    rt.lo = chunk_key_tile(sg.from, sg.p.c);
+    rt.hi = chunk_key_tile(sg.to, sg.p.c);
     rt.pos0 = sg.tile * sg.p.per;
     rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
     if (thread_here() == 0 && sg.from > 0 && sg.from <= size) {   // the first part to begin inside it
       const int64_t stop = sg.at + chunk_cost(sg.p, sg.tile);
-      s.joins[part] = {sg.at, stop, size, (int64_t)sg.start + rt.pos0, rt.n_rows, sg.p.rows,
-                       sg.p.extra, chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
+      s.joins[part] = {sg.at, stop, size, (int64_t)sg.start + rt.pos0, rt.n_rows, sg.p.c,
+                       chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
     }
     if (rt.lo >= rt.hi) return;
     rt.whole = rt.lo == 0 && rt.hi == chunk_key_tiles(sg.p, sg.tile);
-    if (sg.p.rows < 256) attend_few(a, s, sg, rt, part, sm, sml);
+    if (sg.p.c.rows < 256) attend_few(a, s, sg, rt, part, sm, sml);
     else attend_many(a, s, sg, rt, part, sm, list, sodd, scnt);
   });
 }
@@ -993,8 +990,8 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
 #pragma unroll
     for (int k = 0; k < kMergeRound; ++k) {
       const int i = min(i0 + k, jn.last);
-      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.rows, jn.extra);
-      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.rows, jn.extra);
+      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.scale);
+      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.scale);
       there[k] = i0 + k <= jn.last && lo < hi;
       if (lo == 0 && hi == jn.key_tiles) return;         // written by that part
       if (!there[k]) continue;

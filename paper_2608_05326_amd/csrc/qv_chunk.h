@@ -20,11 +20,24 @@ constexpr int kChunkWaves = 8;
 // Rows of a workgroup for a place with this many in all.
 QV_HD int chunk_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 256; }
 
+// How the key tiles of a place's row tiles lie on the line: `extra` first, then the complete
+// blocks, then the tiles of rows in bf16.
+struct ChunkScale {
+  int rows;           // rows of a workgroup
+  int extra;          // length beside the keys
+  int blocks;         // complete blocks
+};
+// Length of a key of a complete block, and of one in bf16: many rows at once are bound by their
+// products, few by the bytes of the pages (microseconds a tile of 64 keys, over the whole chip:
+// 256 rows 1.9 and 2.35, 64 rows 1.1, 32 rows 0.5; a row tile costs 9 to 14 beside them).
+QV_HD int chunk_page_key(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
+QV_HD int chunk_row_key(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 4 : 10; }
+
 struct ChunkPlace {
   int held, n;        // tokens held, new tokens (0: none)
-  int rows, per;      // rows of a workgroup, positions of a row tile
+  int per;            // positions of a row tile
   int tiles;          // row tiles of a KV head
-  int extra;          // length of a row tile on the line beside its keys'
+  ChunkScale c;
   bool solo;          // a row tile is one wave's: a workgroup takes up to eight KV heads at once
 };
 
@@ -33,15 +46,15 @@ QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, int H_kv, int max_conte
   ChunkPlace p;
   p.held = len;
   p.n = len < 0 || len >= max_context ? 0 : rows < max_context - len ? rows : max_context - len;
-  p.rows = chunk_rows((int64_t)p.n * gqa);
-  p.per = p.rows / gqa;
+  p.c.rows = chunk_rows((int64_t)p.n * gqa);
+  p.c.blocks = len < 0 ? 0 : len / kBlockTokens;
+  p.per = p.c.rows / gqa;
   p.tiles = (p.n + p.per - 1) / p.per;
-  p.solo = p.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
-  p.extra = p.rows > 64 ? 3072 : !p.solo ? 2304 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
+  p.solo = p.c.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
+  p.c.extra = p.c.rows > 64 ? (p.c.blocks ? 3584 : 2304)
+                            : !p.solo ? 2816 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
   return p;
 }
-// log2 of what a key costs on the line, by the rows of its workgroup.
-QV_HD int chunk_weight(int rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 3; }
 
 // New tokens up to the end of row tile t.
 QV_HD int chunk_end(const ChunkPlace& p, int t) {
@@ -50,13 +63,17 @@ QV_HD int chunk_end(const ChunkPlace& p, int t) {
 }
 
 // Length of row tile t on the line, and of the t row tiles before it.
+QV_HD int64_t chunk_held_cost(const ChunkPlace& p) {
+  return (int64_t)p.c.blocks * (kBlockTokens * chunk_page_key(p.c.rows)) +
+         (p.held - p.c.blocks * kBlockTokens) * chunk_row_key(p.c.rows) + p.c.extra;
+}
 QV_HD int64_t chunk_cost(const ChunkPlace& p, int t) {
-  return (((int64_t)p.held + chunk_end(p, t)) << chunk_weight(p.rows)) + p.extra;
+  return chunk_held_cost(p) + (int64_t)chunk_end(p, t) * chunk_row_key(p.c.rows);
 }
 QV_HD int64_t chunk_before(const ChunkPlace& p, int t) {
-  int64_t keys = (int64_t)t * p.held + (int64_t)p.per * t * (t + 1) / 2;
-  if (t == p.tiles && t) keys -= (int64_t)p.tiles * p.per - p.n;
-  return (keys << chunk_weight(p.rows)) + (int64_t)t * p.extra;
+  int64_t rows = (int64_t)p.per * t * (t + 1) / 2;
+  if (t == p.tiles && t) rows -= (int64_t)p.tiles * p.per - p.n;
+  return t * chunk_held_cost(p) + rows * chunk_row_key(p.c.rows);
 }
 QV_HD int64_t chunk_pair_cost(const ChunkPlace& p) { return chunk_before(p, p.tiles); }
 
@@ -79,16 +96,20 @@ QV_HD int chunk_quotient(int64_t x, int64_t y) {
   return q;
 }
 
-static_assert(kBlockTokens == 64, "key tiles");
 // Tiles of 64 keys that row tile t sees, and the first of them at or past point x of a row
-// tile of a place with these rows and extra.
+// tile.
 QV_HD int chunk_key_tiles(const ChunkPlace& p, int t) {
   return (int)(((int64_t)p.held + chunk_end(p, t) + kBlockTokens - 1) / kBlockTokens);
 }
-QV_HD int chunk_key_tile(int64_t x, int rows, int extra) {
-  const int64_t y = x - extra;
-  const int shift = 6 + chunk_weight(rows);
-  return y <= 0 ? 0 : (int)((y + (1 << shift) - 1) >> shift);
+QV_HD int chunk_key_tile(int64_t x, const ChunkScale& c) {
+  static_assert(kBlockTokens == 64, "shifts");
+  const int64_t y = x - c.extra;
+  if (y <= 0) return 0;
+  const int shift = c.rows <= 32 ? 7 : c.rows <= 64 ? 8 : 9;        // a tile of a block
+  const int64_t z = y - ((int64_t)c.blocks << shift);
+  if (z <= 0) return (int)((y + (1 << shift) - 1) >> shift);
+  if (c.rows <= 64) return c.blocks + (int)((z + (1 << shift) - 1) >> shift);
+  return c.blocks + (int)((uint32_t)((z + 127) >> 7) + 4) / 5;      // 640 a tile
 }
 
 // Length of a part, given the line's.

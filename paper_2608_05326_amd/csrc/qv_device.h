@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "qv_chunk.h"
 #include "qv_layout.h"
 
 namespace qv {
@@ -239,7 +240,7 @@ struct ChunkJoin {          // a row tile that several parts serve, by the first
   int64_t at, stop, size;   // the row tile on the line, the length of a part
   int64_t row;              // its first row of the packed tensors
   int32_t n_rows;           // (position, head) rows; 0: nothing to join
-  int32_t rows, extra;      // of its place
+  ChunkScale scale;         // of its place
   int32_t key_tiles;        // of all its keys
   int32_t head, last;       // first query head, last part
 };

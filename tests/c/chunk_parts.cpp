@@ -45,9 +45,9 @@ int main() {
       room -= n;
       const ChunkPlace p = chunk_place(held, n, gqa, H_kv, max_context);
       CHECK(p.n >= 0 && p.n <= n && (p.n == 0 || (held >= 0 && (int64_t)held + p.n <= max_context)));
-      CHECK(p.per >= 1 && p.per * gqa <= p.rows && (int64_t)p.tiles * p.per >= p.n);
+      CHECK(p.per >= 1 && p.per * gqa <= p.c.rows && (int64_t)p.tiles * p.per >= p.n);
       CHECK(p.tiles == 0 || (int64_t)(p.tiles - 1) * p.per < p.n);
-      CHECK(p.extra > 0 && (!p.solo || (p.rows == 32 && p.tiles <= 1)));
+      CHECK(p.c.extra > 0 && (!p.solo || (p.c.rows == 32 && p.tiles <= 1)));
       for (int r = 0; r < 256; ++r) CHECK(((uint32_t)r * ((65536 + gqa - 1) / gqa)) >> 16 == (uint32_t)(r / gqa));
       places.push_back(p);
       before.push_back(total);
@@ -68,7 +68,7 @@ int main() {
           const int64_t c = chunk_cost(places[s], t);
           CHECK(c > 0);
           CHECK(chunk_tile_at(places[s], in_pair) == t && chunk_tile_at(places[s], in_pair + c - 1) == t);
-          CHECK(chunk_key_tile(c, places[s].rows, places[s].extra) == chunk_key_tiles(places[s], t));
+          CHECK(chunk_key_tile(c, places[s].c) == chunk_key_tiles(places[s], t));
           tiles.push_back({s, g, t, chunk_key_tiles(places[s], t), at, at + c});
           at += c;
           in_pair += c;
@@ -88,8 +88,8 @@ int main() {
       while (x < end) {
         while (tiles[i].stop <= x) ++i;
         const int64_t stop = std::min(end, tiles[i].stop);
-        const int rows = places[tiles[i].s].rows, extra = places[tiles[i].s].extra;
-        const int lo = chunk_key_tile(x - tiles[i].at, rows, extra), hi = chunk_key_tile(stop - tiles[i].at, rows, extra);
+        const ChunkScale& sc = places[tiles[i].s].c;
+        const int lo = chunk_key_tile(x - tiles[i].at, sc), hi = chunk_key_tile(stop - tiles[i].at, sc);
         if (lo < hi) {
           int slot = -1;
           if (lo > 0 || hi < tiles[i].v) {
@@ -119,8 +119,8 @@ int main() {
         bool whole = false;
         CHECK(x0 - t.at <= size);   // (what the attention kernel goes by)
         for (int k = w - 1; k <= chunk_quotient(t.stop - 1, size); ++k) {
-          const int lo = chunk_key_tile(std::max<int64_t>(k * size - t.at, 0), places[t.s].rows, places[t.s].extra);
-          const int hi = chunk_key_tile(std::min(k * size + size, t.stop) - t.at, places[t.s].rows, places[t.s].extra);
+          const int lo = chunk_key_tile(std::max<int64_t>(k * size - t.at, 0), places[t.s].c);
+          const int hi = chunk_key_tile(std::min(k * size + size, t.stop) - t.at, places[t.s].c);
           if (lo >= hi) continue;
           if (lo == 0 && hi == t.v) whole = true;
           got.push_back({k, lo, hi, chunk_slot(k, lo)});
