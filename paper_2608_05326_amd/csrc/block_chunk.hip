@@ -69,7 +69,7 @@ __device__ __forceinline__ ChunkPlace lane_place(const BlockArgs& a, const Chunk
   const int i = min(place, a.B - 1);
   const int b = min(max(s.cu[i], 0), s.total), e = min(max(s.cu[i + 1], b), s.total);
   *start = b;
-  return chunk_place(place < a.B ? a.lens[i] : -1, e - b, a.gqa, a.H_kv, a.max_context);
+  return chunk_place(place < a.B ? a.lens[i] : -1, e - b, a.gqa, s.gqa_inv, a.H_kv, a.max_context);
 }
 __device__ __forceinline__ int64_t wave_scan(int64_t x) {   // inclusive
   const int lane = thread_here() & 63;
@@ -128,7 +128,7 @@ __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end,
       g.seq = s0 + w;
       g.start = __builtin_amdgcn_readfirstlane(lp.start[w]);
       const int held = __builtin_amdgcn_readfirstlane(lp.held[w]), n = __builtin_amdgcn_readfirstlane(lp.n[w]);
-      g.p = chunk_place(held, n, a.gqa, a.H_kv, a.max_context);
+      g.p = chunk_place(held, n, a.gqa, s.gqa_inv, a.H_kv, a.max_context);
       g.p.per = __builtin_amdgcn_readfirstlane(g.p.per);       // (divisions leave them in vector registers)
       g.p.tiles = __builtin_amdgcn_readfirstlane(g.p.tiles);
       const int64_t pair = chunk_pair_cost(g.p), last = lane_of(lp.incl[w], 0);
@@ -156,8 +156,8 @@ __device__ __forceinline__ void walk(const BlockArgs& a, int64_t x, int64_t end,
   }
 }
 // The line's length; the first 64 places are put in lp (the whole workgroup).
-__device__ __forceinline__ int64_t line_total(const BlockArgs& a, const ChunkStep& s, LinePlaces& lp) {
-  if (threadIdx.x < 64) put_places(a, s, 0, 0, lp);
+__device__ __forceinline__ int64_t line_total(const BlockArgs& a, const ChunkStep& s, LinePlaces& lp, int zero) {
+  if (threadIdx.x < 64) put_places(a, s, zero, 0, lp);
   __syncthreads();
   int64_t total = lane_of(lp.incl[63], 0);
   if (a.B > 64) {
@@ -948,7 +948,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   __shared__ LinePlaces lp;
   // parts of one KV head on one XCD (workgroup i runs on XCD i % 8)
   const int part = (blockIdx.x & 7) * (kChunkParts / 8) + (blockIdx.x >> 3);
-  const int64_t total = line_total(a, s, lp), size = lane_of(chunk_part(total), 0);
+  const int64_t total = line_total(a, s, lp, touch_kernargs<sizeof(BlockArgs) + sizeof(ChunkStep)>());
+  const int64_t size = lane_of(chunk_part(total), 0);
   const int64_t begin = part * size, end = min(begin + size, total);
   if (threadIdx.x == 0) s.joins[part].n_rows = 0;
   walk(a, begin, end, s, lp, [&](const Segment& sg) {
@@ -1030,7 +1031,7 @@ int64_t block_chunk_workspace_bytes(int64_t total, int gqa) {
 }
 
 hipError_t launch_chunk_attend(const BlockArgs& a, ChunkStep s, void* workspace, hipStream_t st) {
-  s.gqa_inv = (65536 + a.gqa - 1) / a.gqa;
+  s.gqa_inv = chunk_inverse(a.gqa);
   s.slot_rows = slot_rows(s.total, a.gqa);
   s.part_o = (float*)workspace;
   s.part_ml = (float2*)(s.part_o + (int64_t)2 * kChunkParts * s.slot_rows * kHeadDim);

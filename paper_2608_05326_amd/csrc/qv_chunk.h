@@ -41,15 +41,18 @@ struct ChunkPlace {
   bool solo;          // a row tile is one wave's: a workgroup takes up to eight KV heads at once
 };
 
+// 2^16 / gqa, rounded up: (r * this) >> 16 is r / gqa for r <= 256 and gqa <= 16.
+QV_HD uint32_t chunk_inverse(int gqa) { return (65536u + gqa - 1) / gqa; }
+
 // A place with `len` tokens held that is given `rows` new ones; max_context limits both.
-QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, int H_kv, int max_context) {
+QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, uint32_t gqa_inv, int H_kv, int max_context) {
   ChunkPlace p;
   p.held = len;
   p.n = len < 0 || len >= max_context ? 0 : rows < max_context - len ? rows : max_context - len;
   p.c.rows = chunk_rows((int64_t)p.n * gqa);
   p.c.blocks = len < 0 ? 0 : len / kBlockTokens;
-  p.per = p.c.rows / gqa;
-  p.tiles = (p.n + p.per - 1) / p.per;
+  p.per = (int)((uint32_t)p.c.rows * gqa_inv >> 16);
+  p.tiles = p.n <= p.per ? p.n > 0 : (p.n + p.per - 1) / p.per;
   p.solo = p.c.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
   p.c.extra = p.c.rows > 64 ? (p.c.blocks ? 3584 : 2304)
                             : !p.solo ? 2816 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
@@ -88,11 +91,12 @@ QV_HD int chunk_tile_at(const ChunkPlace& p, int64_t x) {
   return lo;
 }
 
-// x / y for 0 <= x < 2^62 with a quotient below 2^30 (a device's 64-bit division is long).
+// x / y for 0 <= x < 2^62, y > 0 and a quotient below 2^30: a device's 64-bit division is long,
+// an fp32 one is right to 2^-22 of it (small quotients: to one).
 QV_HD int chunk_quotient(int64_t x, int64_t y) {
-  int q = (int)((double)x / (double)y);
-  if ((int64_t)q * y > x) --q;
-  if ((int64_t)(q + 1) * y <= x) ++q;
+  int q = (int)((float)x / (float)y);
+  while ((int64_t)q * y > x) --q;
+  while ((int64_t)(q + 1) * y <= x) ++q;
   return q;
 }
 

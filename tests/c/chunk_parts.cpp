@@ -43,12 +43,12 @@ int main() {
       const int held = pick(0, 9) == 0 ? -1 : (int)pick(0, most[pick(0, 3)]);
       const int n = (int)std::min<int64_t>(room, pick(0, 1) ? pick(0, 8) : pick(0, 3000));
       room -= n;
-      const ChunkPlace p = chunk_place(held, n, gqa, H_kv, max_context);
+      const ChunkPlace p = chunk_place(held, n, gqa, chunk_inverse(gqa), H_kv, max_context);
       CHECK(p.n >= 0 && p.n <= n && (p.n == 0 || (held >= 0 && (int64_t)held + p.n <= max_context)));
       CHECK(p.per >= 1 && p.per * gqa <= p.c.rows && (int64_t)p.tiles * p.per >= p.n);
       CHECK(p.tiles == 0 || (int64_t)(p.tiles - 1) * p.per < p.n);
       CHECK(p.c.extra > 0 && (!p.solo || (p.c.rows == 32 && p.tiles <= 1)));
-      for (int r = 0; r < 256; ++r) CHECK(((uint32_t)r * ((65536 + gqa - 1) / gqa)) >> 16 == (uint32_t)(r / gqa));
+      for (int r = 0; r <= 256; ++r) CHECK(((uint32_t)r * chunk_inverse(gqa)) >> 16 == (uint32_t)(r / gqa));
       places.push_back(p);
       before.push_back(total);
       total += chunk_pair_cost(p) * H_kv;
