@@ -66,8 +66,8 @@ __device__ __forceinline__ uint32_t amax_bits(uint32_t pair) { return max(pair <
 // page (all 256 threads): thread (m, c) = (tid / 16, tid % 16) holds channels 8 c .. + 7 of
 // tokens 4 m .. + 3.
 struct CloseLds {
-  uint32_t vt[kHeadDim][kBlk / 4 + 1];   // value codes, four tokens a word
   uint32_t amax[kThreads / 64];
+  uint32_t vt[kHeadDim][kBlk / 4 + 1];   // value codes, four tokens a word (keys: not used)
 };
 template <bool VALUES>
 __device__ __forceinline__ void close_rows(const u32x4 (&x)[4], int8_t* codes, float* scale, CloseLds& sm) {

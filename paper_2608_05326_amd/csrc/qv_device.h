@@ -225,6 +225,8 @@ struct AppendRows {         // packed new tokens of a block cache
   const int32_t* counts;    // [B] rows of each place that are taken; null: all
   int32_t total;
   int32_t rotate;           // keys are rotated on the way
+  int32_t heads;            // KV heads of a workgroup that rotates keys
+  int32_t key_groups;       // workgroups that take keys, before those that take values
 };
 
 struct BlockStep {          // a decode step on the block cache

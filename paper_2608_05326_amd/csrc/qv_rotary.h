@@ -42,12 +42,16 @@ __device__ __forceinline__ float2 cos_sin(uint32_t u) {
                      __uint_as_float(__float_as_uint(b) ^ (quarter << 30 & 0x80000000u)));
 }
 
+// The angle at position p of a pair with F = turns, in 2^-32 turns (rounded).
+__device__ __forceinline__ uint32_t turned(uint64_t turns, int32_t p) {
+  return (uint32_t)(((uint64_t)(int64_t)p * turns + 0x80000000u) >> 32);
+}
+
 // cos and sin of pair i for a token with the positions p[axis]
 __device__ __forceinline__ float2 pair_cos_sin(const RotaryArgs& r, int i, const int32_t (&p)[kMaxAxes]) {
   const int a = r.axis[i];
   const int32_t at = a < 2 ? (a ? p[1] : p[0]) : (a == 2 ? p[2] : p[3]);
-  const uint64_t t = (uint64_t)(int64_t)at * r.turns[i] + 0x80000000u;
-  return cos_sin((uint32_t)(t >> 32));
+  return cos_sin(turned(r.turns[i], at));
 }
 
 __device__ __forceinline__ void row_positions(const RotaryArgs& r, int64_t row, int32_t (&p)[kMaxAxes]) {
@@ -62,6 +66,22 @@ __device__ __forceinline__ uint32_t pack_rne(float lo, float hi) {
 // (x, y) turned by the angle of cs
 __device__ __forceinline__ float turn_x(float x, float y, float2 cs) { return fmaf(x, cs.x, -(y * cs.y)); }
 __device__ __forceinline__ float turn_y(float x, float y, float2 cs) { return fmaf(y, cs.x, x * cs.y); }
+
+// Two channels of a word that are a pair
+__device__ __forceinline__ uint32_t turn_word(uint32_t w, float c, float s) {
+  const float x = __uint_as_float(w << 16), y = __uint_as_float(w & 0xFFFF0000u);
+  return pack_rne(turn_x(x, y, make_float2(c, s)), turn_y(x, y, make_float2(c, s)));
+}
+// Two channels whose other channels are in another word: the second (turn_y) or first (turn_x)
+// of their pairs; cs the two angles.
+__device__ __forceinline__ uint32_t turn_halves(uint32_t own, uint32_t other, f32x4 cs, bool second) {
+  const uint32_t flip = second ? 0 : 0x80000000u;
+  auto f = [&](uint32_t x, uint32_t y, float c, float s) {
+    const float b = __uint_as_float(y) * s;
+    return fmaf(__uint_as_float(x), c, __uint_as_float(__float_as_uint(b) ^ flip));
+  };
+  return pack_rne(f(own << 16, other << 16, cs[0], cs[1]), f(own & 0xFFFF0000u, other & 0xFFFF0000u, cs[2], cs[3]));
+}
 
 // Eight pairs: x, y are their channels in bf16, eight and eight (apart) or in turn
 // (interleaved: x the first four pairs, y the others).

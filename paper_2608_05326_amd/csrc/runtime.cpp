@@ -51,7 +51,7 @@ int64_t block_workspace_bytes(int64_t B, int H_kv, int gqa);
 hipError_t launch_block_attend(const BlockArgs& a, BlockStep s, void* workspace, hipStream_t st);
 hipError_t launch_rotate(RotateArgs a, const RotaryArgs& r, hipStream_t st);
 int64_t block_append_groups(int64_t total, int n_seqs, int H_kv);
-hipError_t launch_block_append(const BlockArgs& a, const AppendRows& r, const RotaryArgs& rot, hipStream_t st);
+hipError_t launch_block_append(const BlockArgs& a, AppendRows r, const RotaryArgs& rot, hipStream_t st);
 int64_t block_chunk_workspace_bytes(int64_t total, int gqa);
 hipError_t launch_chunk_attend(const BlockArgs& a, ChunkStep s, void* workspace, hipStream_t st);
 }  // namespace qv
@@ -1687,7 +1687,7 @@ qevict_status qevict_block_append(const qevict_block_config* cfg, const qevict_b
     return s;
   if (block_append_groups(total_tokens, a.B, a.H_kv) > kMaxGroups)
     return fail(QEVICT_ERR_UNSUPPORTED, "sequences too large for one call");
-  const AppendRows rows = {r.k, r.v, r.k_st, r.k_sh, r.v_st, r.v_sh, r.cu, counts, total_tokens, rotary != nullptr};
+  const AppendRows rows = {r.k, r.v, r.k_st, r.k_sh, r.v_st, r.v_sh, r.cu, counts, total_tokens, rotary != nullptr, 1, 0};
   hipError_t e = launch_block_append(a, rows, rot, (hipStream_t)hip_stream);
   return e == hipSuccess ? QEVICT_OK : hip_fail(e, "block_append launch");
 }
