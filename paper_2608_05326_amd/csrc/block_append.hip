@@ -25,8 +25,9 @@ union AppendLds {
 };
 __device__ __forceinline__ int angle_at(int row, int pair) { return pair ^ (row & 7) << 1; }
 }  // namespace
-__global__ __launch_bounds__(kThreads) void k_block_append(BlockArgs a, AppendRows r, RotaryArgs rot) {
+__global__ __launch_bounds__(kThreads, 4) void k_block_append(BlockArgs a, AppendRows r, RotaryArgs rot) {
   __shared__ AppendLds sm;
+  __shared__ RotaryLds tables;
   const bool values = (int)blockIdx.x >= r.key_groups;
   const int heads = values ? 1 : r.heads, sets = (a.H_kv + heads - 1) / heads;
   const int idx = values ? blockIdx.x - r.key_groups : blockIdx.x;
@@ -56,50 +57,60 @@ __global__ __launch_bounds__(kThreads) void k_block_append(BlockArgs a, AppendRo
   auto find_angles = [&](int p0) {
     const int i = threadIdx.x & 63;
     if (i >= rot.n_pairs) return;
-    const uint64_t turns = rot.turns[i];
-    const int32_t* pos = rot.pos + ((int64_t)w.start - held) * rot.p_st + rot.axis[i] * rot.p_sa;
+    const uint64_t turns = tables.turns[i];
+    const int axis = tables.axis[i >> 2] >> 8 * (i & 3) & 0xFF;
+    const int32_t* pos = rot.pos + ((int64_t)w.start - held) * rot.p_st + axis * rot.p_sa;
 #pragma unroll 4
     for (int k = 0; k < kBlk; k += kThreads / 64) {
       const int t = k + (threadIdx.x >> 6), p = p0 + t;
       if (p >= held && p < held + n) sm.keys.cs[t][angle_at(t, i)] = cos_sin(turned(turns, pos[p * rot.p_st]));
     }
   };
-  // chunk c of KV head g of the new token at position p
-  auto new_row = [&](int p, int g) -> u32x4 {
-    const uint16_t* x = rows + p * st + g * sh;
-    u32x4 u = *(const u32x4*)(x + 8 * c);
-    if (rotate) {
-      auto cs = [&](int i) { return *(const f32x4*)&sm.keys.cs[p % kBlk][angle_at(p % kBlk, i)]; };
-      if (rot.interleaved) {
+  // chunk c of the token at position p in KV head g, as it is in memory
+  auto row = [&](int p, int g) -> u32x4 {
+    return *(const u32x4*)((p < held ? tails + g * kCodes + p % kBlk * kHeadDim : rows + p * st + g * sh) + 8 * c);
+  };
+  // u, chunk c of the new token at position p, turned; all lanes that have the token's chunks call it
+  auto turn = [&](int p, u32x4 u) -> u32x4 {
+    auto cs = [&](int i) { return *(const f32x4*)&sm.keys.cs[p % kBlk][angle_at(p % kBlk, i)]; };
+    if (rot.interleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          const f32x4 t = cs(4 * c + i);
-          u[i] = turn_word(u[i], t[0], t[1]);
-          u[i + 1] = turn_word(u[i + 1], t[2], t[3]);
-        }
-      } else {
-        const u32x4 v = *(const u32x4*)(x + 8 * other);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = turn_halves(u[i], v[i], cs(pair0 + 2 * i), second);
+      for (int i = 0; i < 4; i += 2) {
+        const f32x4 t = cs(4 * c + i);
+        u[i] = turn_word(u[i], t[0], t[1]);
+        u[i + 1] = turn_word(u[i + 1], t[2], t[3]);
       }
+    } else {
+      u32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = __shfl((int)u[i], other, 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = turn_halves(u[i], v[i], cs(pair0 + 2 * i), second);
     }
     return u;
   };
 
+  if (r.rotate && !values) {
+    stage_rotary(rot, tables);
+    __syncthreads();
+  }
   const bool whole = held + n >= (blk + 1) * kBlk;
   const int page = whole ? page_of(a, w.seq, blk) : -1;
   if (page >= 0) {
     const int p0 = blk * kBlk + 4 * m;
+    u32x4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = row(p0 + i, g0);
     if (r.rotate && !values) {
       find_angles(blk * kBlk);
       __syncthreads();
     }
     for (int g = g0; g < g1; ++g) {
-      u32x4 y[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        y[i] = p0 + i < held ? *(const u32x4*)(tails + g * kCodes + (p0 + i) % kBlk * kHeadDim + 8 * c)
-                             : new_row(p0 + i, g);
+      for (int i = 0; i < 4; ++i) y[i] = rotate && p0 + i >= held ? turn(p0 + i, x[i]) : x[i];
+      if (g + 1 < g1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = row(p0 + i, g + 1);
       const int64_t e = (int64_t)page * a.H_kv + g;
       if (values) close_rows<true>(y, a.v_codes + e * kCodes, a.v_scale + e, sm.close);
       else close_rows<false>(y, a.k_codes + e * kCodes, a.k_scale + e, sm.close);
@@ -114,7 +125,10 @@ __global__ __launch_bounds__(kThreads) void k_block_append(BlockArgs a, AppendRo
     __syncthreads();
   }
   for (int p = max(held, last * kBlk) + m; p < held + n; p += kThreads / 16)
-    for (int g = g0; g < g1; ++g) *(u32x4*)(tails + g * kCodes + p % kBlk * kHeadDim + 8 * c) = new_row(p, g);
+    for (int g = g0; g < g1; ++g) {
+      const u32x4 u = row(p, g);
+      *(u32x4*)(tails + g * kCodes + p % kBlk * kHeadDim + 8 * c) = rotate ? turn(p, u) : u;
+    }
 }
 
 // Blocks that a call may touch (an upper bound), and workgroups.

@@ -12,7 +12,7 @@ constexpr int kMaxPairs = kHeadDim / 2, kMaxAxes = 4;
 
 struct RotaryArgs {
   uint64_t turns[kMaxPairs];   // F_i (the inverse rotation: -F_i)
-  uint8_t axis[kMaxPairs];
+  uint32_t axis[kMaxPairs / 4];   // four pairs a word
   int32_t n_pairs;             // a multiple of 8; channels past 2 n_pairs are left as they are
   int32_t n_axes;
   int32_t interleaved;         // pairs (2 i, 2 i + 1), else (i, i + n_pairs)
@@ -47,9 +47,32 @@ __device__ __forceinline__ uint32_t turned(uint64_t turns, int32_t p) {
   return (uint32_t)(((uint64_t)(int64_t)p * turns + 0x80000000u) >> 32);
 }
 
+// The pairs' tables in LDS, staged by 256 threads (a barrier follows).  Scalar loads: a launch's
+// arguments are in memory that vector loads read anew for every wave.
+struct alignas(16) RotaryLds {
+  uint64_t turns[kMaxPairs];
+  uint32_t axis[kMaxPairs / 4];
+};
+__device__ __forceinline__ void stage_rotary(const RotaryArgs& r, RotaryLds& t) {
+  static_assert(kMaxPairs % 16 == 0);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (w >= kMaxPairs / 16) return;
+  uint64_t f[16];
+  uint32_t ax[4];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = r.turns[16 * w + i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ax[i] = r.axis[4 * w + i];
+  if (threadIdx.x & 63) return;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t.turns[16 * w + i] = f[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t.axis[4 * w + i] = ax[i];
+}
+
 // cos and sin of pair i for a token with the positions p[axis]
-__device__ __forceinline__ float2 pair_cos_sin(const RotaryArgs& r, int i, const int32_t (&p)[kMaxAxes]) {
-  const int a = r.axis[i];
+__device__ __forceinline__ float2 pair_cos_sin(const RotaryLds& r, int i, const int32_t (&p)[kMaxAxes]) {
+  const int a = r.axis[i >> 2] >> 8 * (i & 3) & 0xFF;
   const int32_t at = a < 2 ? (a ? p[1] : p[0]) : (a == 2 ? p[2] : p[3]);
   return cos_sin(turned(r.turns[i], at));
 }

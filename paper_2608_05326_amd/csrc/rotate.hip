@@ -14,18 +14,22 @@ constexpr int kRotThreads = 256, kTokens = kRotThreads / 8;
 }
 
 __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a, RotaryArgs r) {
+  __shared__ RotaryLds tables;
+  stage_rotary(r, tables);
+  __syncthreads();
   const int j = threadIdx.x & 7;
-  const int64_t row = (int64_t)blockIdx.x * kTokens + (threadIdx.x >> 3);
+  const int sets = (a.H_q + a.H_k + a.heads - 1) / a.heads;
+  const int64_t row = (int64_t)(blockIdx.x / sets) * kTokens + (threadIdx.x >> 3);
   if (row >= a.total) return;
   int32_t p[kMaxAxes];
   row_positions(r, row, p);
   const bool turned = 8 * j < r.n_pairs;
   float2 cs[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = turned ? pair_cos_sin(r, 8 * j + i, p) : make_float2(1.f, 0.f);
+  for (int i = 0; i < 8; ++i) cs[i] = turned ? pair_cos_sin(tables, 8 * j + i, p) : make_float2(1.f, 0.f);
   const bool apart = turned && !r.interleaved;
   const int cx = apart ? 8 * j : 16 * j, cy = apart ? 8 * j + r.n_pairs : 16 * j + 8;
-  const int h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, a.H_q + a.H_k);
+  const int h0 = blockIdx.x % sets * a.heads, h1 = min(h0 + a.heads, a.H_q + a.H_k);
   for (int h = h0; h < h1; ++h) {
     const bool q = h < a.H_q;
     const uint16_t* x = q ? a.q + row * a.q_st + h * a.q_sh : a.k + row * a.k_st + (h - a.H_q) * a.k_sh;
@@ -38,9 +42,11 @@ __global__ __launch_bounds__(kRotThreads) void k_rotate(RotateArgs a, RotaryArgs
 }
 
 hipError_t launch_rotate(RotateArgs a, const RotaryArgs& r, hipStream_t st) {
+  const int64_t n = (a.total + kTokens - 1) / kTokens;
+  const int H = a.H_q + a.H_k;
   a.heads = 8;
-  const dim3 grid((uint32_t)((a.total + kTokens - 1) / kTokens), (uint32_t)((a.H_q + a.H_k + a.heads - 1) / a.heads));
-  k_rotate<<<grid, kRotThreads, 0, st>>>(a, r);
+  while (a.heads > 1 && n * H < 512 * a.heads) a.heads /= 2;
+  k_rotate<<<(uint32_t)(n * ((H + a.heads - 1) / a.heads)), kRotThreads, 0, st>>>(a, r);
   return hipGetLastError();
 }
 

@@ -1602,7 +1602,8 @@ static qevict_status rotary_args(const qevict_rotary* rot, const int32_t* positi
   for (int i = 0; i < kMaxPairs; ++i) {
     const bool used = i < rot->num_pairs;
     r->turns[i] = !used ? 0 : inverse ? 0 - rot->turns[i] : rot->turns[i];
-    r->axis[i] = used ? rot->axis[i] : 0;
+    const uint32_t before = i & 3 ? r->axis[i >> 2] : 0;
+    r->axis[i >> 2] = before | (used ? (uint32_t)rot->axis[i] << 8 * (i & 3) : 0);
   }
   r->n_pairs = rot->num_pairs;
   r->n_axes = rot->num_axes;
