@@ -283,6 +283,43 @@ __device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float 
   for (int ks = 0; ks < 2 * KT; ++ks) weigh<KT>(r, st, sc, vs, ks, pw[ks]);
 }
 
+// The same for many rows, with vs in the exponent: w = exp2(st sc - (m - log2 vs)), and the sum of
+// weights from the rounded w, as (sum w) / vs: two vector instructions a weight less.  It misses
+// weights below 2^-126 / vs, 2^-46 of the largest for scales from kFoldMin on; those of smaller
+// ones (inv = 0) are summed by themselves, in unfolded().
+constexpr float kFoldMin = 0x1p-80f;
+struct ValueScale {
+  float log2, inv;
+};
+__device__ __forceinline__ ValueScale value_scale(float vs) {
+  return {__builtin_amdgcn_logf(vs), vs >= kFoldMin ? 1.f / vs : 0.f};
+}
+__device__ __forceinline__ float reference(const Running& r) { return r.m > -INFINITY ? r.m : 0.f; }
+template <int KT>
+__device__ __forceinline__ void weigh(Running& r, const f32x16 (&st)[KT], float sc, float mu, float inv, int ks,
+                                      u32x4& pw) {
+  const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = 8 * (ks & 1) + 2 * i;
+    const uint32_t w = pack_bf16(__builtin_amdgcn_exp2f(fmaf(st[ks >> 1][j], sc, -mu)),
+                                 __builtin_amdgcn_exp2f(fmaf(st[ks >> 1][j + 1], sc, -mu)));
+    sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, sum, false);
+    pw[i] = w;
+  }
+  r.l = fmaf(sum, inv, r.l);
+}
+template <int KT>
+__device__ __forceinline__ void unfolded(Running& r, const f32x16 (&st)[KT], float sc, float inv) {
+  if (__builtin_amdgcn_readfirstlane(__float_as_uint(inv))) return;
+  const float mu = reference(r);
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r.l += __builtin_amdgcn_exp2f(fmaf(st[kt][i], sc, -mu));
+}
+
 // A value that is not finite must not reach a row that its key is masked for, through
 // 0 * infinity: such values of rows in bf16 are left out of the products, and added to the
 // rows that see them afterwards.
@@ -577,7 +614,8 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
 // ---- many rows: eight sets of 32 rows share the key tiles, which are expanded into LDS
 struct PageRef {
   int page;
-  float ks, vs;
+  float ks;
+  ValueScale vs;
 };
 constexpr int kList = kChunkThreads;   // pages looked up at once
 // bytes of a tile's keys [64][128] or values (of a page [128][64], else [64][128]), bf16
@@ -724,10 +762,17 @@ __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, const u
   if (seen > 0) {
     f32x16 st[2];
     logits(0, 0, kTileBytes, st);
-    float vs;
-    const float sc = src.logits(0, st, vs);
-    known(0);
-    weigh<2>(r, st, sc, vs, pw);
+    ValueScale vs;
+    {
+      const float sc = src.logits(0, st, vs), mt = largest<2>(st, sc);
+      known(0);
+      u32x4 none[1] = {};
+      if (exceeds(r, mt)) raise(r, mt, none);
+      unfolded(r, st, sc, vs.inv);
+      const float mu = reference(r) - vs.log2;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) weigh<2>(r, st, sc, mu, vs.inv, ks, pw[ks]);
+    }
     __syncthreads();
 #pragma unroll 1
     for (e = 1; e < seen; ++e) {
@@ -736,9 +781,11 @@ __device__ __forceinline__ void wide_loop(Source& src, int n, int kbase, const u
       const float sc = src.logits(e, st, vs), mt = largest<2>(st, sc);
       known(e);
       if (exceeds(r, mt)) raise(r, mt, pw);
+      unfolded(r, st, sc, vs.inv);
+      const float mu = reference(r) - vs.log2;
       wide_values(
           r, pw, [&](int i) __attribute__((always_inline)) { return read_v(e - 1, vb, i); },
-          [&](int ks) __attribute__((always_inline)) { weigh<2>(r, st, sc, vs, ks, pw[ks]); });
+          [&](int ks) __attribute__((always_inline)) { weigh<2>(r, st, sc, mu, vs.inv, ks, pw[ks]); });
       src.after(e - 1, r);
       __syncthreads();
     }
@@ -783,7 +830,7 @@ struct PageSource {
   __device__ __forceinline__ void put_k(int i, uint8_t* to) const { put(kr, to, kput, i); }
   __device__ __forceinline__ void put_v(int i, int, uint8_t* to) const { put(vr, to, vput, i); }
   __device__ __forceinline__ int sees(int n) const { return idle ? 0 : n; }
-  __device__ __forceinline__ float logits(int, f32x16 (&)[2], float& vs) const {
+  __device__ __forceinline__ float logits(int, f32x16 (&)[2], ValueScale& vs) const {
     vs = known.vs;
     return scale(known.ks);
   }
@@ -805,11 +852,11 @@ __device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg
                     lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr)), idle};
   for (int t0 = lo; t0 < hi; t0 += kList) {
     // ---- the next pages (blocks without one are left out)
-    PageRef x = {-1, 0.f, 0.f};
+    PageRef x = {-1, 0.f, {0.f, 0.f}};
     if (t0 + tid < hi) x.page = page_of(a, sg.seq, t0 + tid);
     if (x.page >= 0) {
       x.ks = a.k_scale[(int64_t)x.page * a.H_kv + sg.g];
-      x.vs = a.v_scale[(int64_t)x.page * a.H_kv + sg.g];
+      x.vs = value_scale(a.v_scale[(int64_t)x.page * a.H_kv + sg.g]);
     }
     const uint64_t mask = __ballot(x.page >= 0);
     if (lane == 0) scnt[wave] = __builtin_popcountll(mask);
@@ -868,7 +915,7 @@ struct RowSource {
     if (lane == 0) sodd[e & 1][2 * wave + i] = odd;
   }
   __device__ __forceinline__ int sees(int n) const { return min(n, max((wpos1 >> 6) - t0 + 1, 0)); }
-  __device__ __forceinline__ float logits(int e, f32x16 (&st)[2], float& vs) const {
+  __device__ __forceinline__ float logits(int e, f32x16 (&st)[2], ValueScale& vs) const {
     const int p0 = (t0 + e) * kBlk;
     if (p0 + kBlk - 1 > wpos0) {
       const int rel = pos - p0 - 8 * (lane >> 5);
@@ -878,7 +925,7 @@ struct RowSource {
         for (int i = 0; i < 16; ++i)
           if (32 * kt + 16 * (i >> 3) + (i & 7) > rel) st[kt][i] = -INFINITY;
     }
-    vs = 1.f;
+    vs = {0.f, 1.f};
     return scale(1.f);
   }
   // (chunks of keys 8 lh .. + 3 and of + 4 .. + 7 differ by the bit of 16 bytes in their swizzle)
@@ -971,9 +1018,10 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
 }
 
 // Joins the row tiles that more than one part served: workgroup (w, r) takes rows 8 r .. + 7
-// of the one that part w begins inside, if it is the first to do so.
+// of the one that part w begins inside, if it is the first to do so.  Most are of two or three
+// parts: a round is four (67 MB of parts 15 us; with eight, of which most pass by, 36 us).
 namespace {
-constexpr int kMergeRows = 8, kMergeRound = 8;
+constexpr int kMergeRows = 8, kMergeRound = 4;
 }
 __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) {
   const int w = blockIdx.x + 1;
@@ -983,22 +1031,25 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
   const int c = 4 * (threadIdx.x & 31), rr = min(r, jn.n_rows - 1);
   float M = -INFINITY, L = 0.f;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int i0 = w - 1; i0 <= jn.last; i0 += kMergeRound) {
+  int lo = 0;   // first key tile of part i
+  for (int i = w - 1; i <= jn.last;) {
     // a round of parts, all loads first
     float2 ml[kMergeRound];
     f32x4 y[kMergeRound];
     bool there[kMergeRound];
 #pragma unroll
-    for (int k = 0; k < kMergeRound; ++k) {
-      const int i = min(i0 + k, jn.last);
-      const int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.scale);
-      const int hi = chunk_key_tile(min(i * jn.size + jn.size, jn.stop) - jn.at, jn.scale);
-      there[k] = i0 + k <= jn.last && lo < hi;
+    for (int k = 0; k < kMergeRound; ++k, ++i) {
+      there[k] = false;
+      if (i > jn.last) continue;
+      const int hi = chunk_key_tile(min((i + 1) * jn.size, jn.stop) - jn.at, jn.scale);
       if (lo == 0 && hi == jn.key_tiles) return;         // written by that part
-      if (!there[k]) continue;
-      const int64_t slot = (int64_t)chunk_slot(i, lo) * s.slot_rows + rr;
-      ml[k] = s.part_ml[slot];
-      y[k] = *(const f32x4*)(s.part_o + slot * kHeadDim + c);
+      there[k] = lo < hi;
+      if (there[k]) {
+        const int64_t slot = (int64_t)chunk_slot(i, lo) * s.slot_rows + rr;
+        ml[k] = s.part_ml[slot];
+        y[k] = *(const f32x4*)(s.part_o + slot * kHeadDim + c);
+      }
+      lo = hi;
     }
     float mn = M;
 #pragma unroll
@@ -1019,7 +1070,8 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
     }
   }
   if (r >= jn.n_rows) return;
-  uint16_t* op = s.out + (jn.row + r / gqa) * s.o_st + (jn.head + r % gqa) * s.o_sh + c;
+  const int i = by_gqa(s, r);
+  uint16_t* op = s.out + (jn.row + i) * s.o_st + (jn.head + r - i * gqa) * s.o_sh + c;
   *(u32x2*)op = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
 }
 

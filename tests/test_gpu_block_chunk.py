@@ -290,6 +290,33 @@ def test_logits_and_scales_of_every_size(lens):
     _check(b, held, lens, q, k, v, out)
 
 
+@pytest.mark.parametrize("lens", [[5, 3], [90, 40], [300, 260]])
+def test_value_scales_far_apart(lens):
+    """Values of a block 2^79 to 2^100 smaller than those of the next, blocks of zeros (with the
+    smallest scale, or a scale of zero): their keys weigh in a row's sum as all others do."""
+    import torch
+    held = [700, 260]
+    bc = _cache(held, 8, 2, sum(lens), seed=50, extra=400, fill=0.0)
+    small = [1.0, 2.0 ** -79, 2.0 ** -81, 0.0, 2.0 ** -100]
+    for s in range(2):
+        pages = bc.table[s, :held[s] // N].long()
+        for i, p in enumerate(pages.tolist()):
+            bc.v_scale[0, p] *= small[i % 5]
+    _run(bc, held, lens, seed=51)
+    _run(bc, held, lens, seed=52, scale=8.0)
+    bc.v_scale.fill_(2.0 ** -100)
+    bc.v_codes.zero_()
+    _run(bc, held, lens, seed=53)
+    bc = _cache(held, 8, 2, sum(lens), seed=54, extra=400, fill=0.0)
+    bc.v_scale *= 2.0 ** -90                  # all of a place's values
+    bc.v_tail.copy_(bc.v_tail.float() * 2.0 ** -90)
+    q, k, v = _rows(sum(lens), 8, 2, seed=55)
+    v = (v.float() * 2.0 ** -90).bfloat16()
+    out = torch.full_like(q, 7.0)
+    bc.attend_chunk(0, q, k, v, _cu(lens), out)
+    _check(bc, held, lens, q, k, v, out)
+
+
 def test_softmax_scale():
     import paper_2608_05326_amd as qv
     import torch
