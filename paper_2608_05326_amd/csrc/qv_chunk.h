@@ -29,7 +29,7 @@ struct ChunkScale {
 };
 // Length of a key of a complete block, and of one in bf16: many rows at once are bound by their
 // products, few by the bytes of the pages (microseconds a tile of 64 keys, over the whole chip:
-// 256 rows 1.9 and 2.35, 64 rows 1.1, 32 rows 0.5; a row tile costs 9 to 14 beside them).
+// 256 rows 1.8 and 2.3, 64 rows 1.1, 32 rows 0.5; a row tile costs 10 to 16 beside them).
 QV_HD int chunk_page_key(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 4 : 8; }
 QV_HD int chunk_row_key(int rows) { return rows <= 32 ? 2 : rows <= 64 ? 4 : 10; }
 
@@ -54,7 +54,7 @@ QV_HD ChunkPlace chunk_place(int len, int rows, int gqa, uint32_t gqa_inv, int H
   p.per = (int)((uint32_t)p.c.rows * gqa_inv >> 16);
   p.tiles = p.n <= p.per ? p.n > 0 : (p.n + p.per - 1) / p.per;
   p.solo = p.c.rows == 32 && p.tiles == 1 && (int64_t)p.held + p.n <= kSoloTiles * kBlockTokens;
-  p.c.extra = p.c.rows > 64 ? (p.c.blocks ? 3584 : 2304)
+  p.c.extra = p.c.rows > 64 ? (p.c.blocks ? 4480 : 2944)
                             : !p.solo ? 2816 : 1536 / (H_kv < kChunkWaves ? H_kv : kChunkWaves);
   return p;
 }
