@@ -588,9 +588,10 @@ qevict_status qevict_block_append(const qevict_block_config *cfg, const qevict_b
  *   workspace  device memory of qevict_block_chunk_workspace_size bytes for total_tokens or
  *              more, 256-byte aligned, overwritten: calls that may overlap need one each
  * Accuracy as qevict_prompt_attend's (the weights beside codes are rounded to bf16 with
- * their block's value scale; a weight below 2^-126 of the row's largest may count as zero).  A value that is not finite reaches the rows that attend to it
- * and no other.  The sums run in an order that depends on the lengths only: a call is bitwise
- * repeatable.  total_tokens * H_q <= 2^30; token strides of k and v below 2^23. */
+ * their block's value scale; a weight below 2^-126 of the row's largest may count as zero).
+ * A value that is not finite reaches the rows that attend to it and no other.  The sums run
+ * in an order that depends on the lengths only: a call is bitwise repeatable.
+ * total_tokens * H_q <= 2^30; token strides of k and v below 2^23. */
 typedef struct {
   int32_t abi_version;
   int32_t total_tokens;      /* rows of the packed tensors */

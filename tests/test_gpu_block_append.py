@@ -100,6 +100,22 @@ def test_append_rotated(held, lens, kw):
     assert torch.equal(k, before)
 
 
+@pytest.mark.parametrize("hkv,places", [(8, 40), (3, 115)])
+@pytest.mark.parametrize("kw", [dict(), dict(dim=80, interleaved=True)], ids=lambda k: "-".join(k) or "plain")
+def test_append_rotated_many(hkv, places, kw):
+    """Calls large enough that a workgroup takes several heads, an odd number of them too."""
+    import paper_2608_05326_amd as qv
+    import torch
+    r = qv.Rotary(**kw)
+    held = [(0, 3, 63, 64, 37)[s % 5] for s in range(places)]
+    lens = [(130, 125, 1, 64, 190)[s % 5] for s in range(places)]
+    bc = _fresh(held, hkv, 260, seed=places)
+    k, v = _rows(sum(lens), hkv, seed=7)
+    pos = torch.arange(sum(lens), dtype=torch.int32).cuda() * 3
+    kept, _ = qv.rotate(k, None, pos, r)
+    _append(bc, held, lens, k, v, kept=kept, rotary=r, positions=pos)
+
+
 def test_pieces_give_what_a_store_gives():
     """A prompt appended in pieces of any size is the prompt stored at once, and rotated too."""
     import paper_2608_05326_amd as qv
