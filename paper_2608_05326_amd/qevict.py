@@ -645,16 +645,19 @@ def rotate(q, k, positions, rotary: Rotary, q_out=None, k_out=None, inverse: boo
         hk = k.shape[1]
     elif k_out is not None:
         raise ValueError("k_out without k")
-    if q_out is None or (k is not None and k_out is None):
-        # from the pool of the stream that writes them: elsewhere pending work may still use them
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
-            if q_out is None:
-                q_out = torch.empty((T, hq, d), dtype=torch.bfloat16, device=q.device)
-            if k is not None and k_out is None:
-                k_out = torch.empty((T, hk, d), dtype=torch.bfloat16, device=q.device)
-    qop, qo_st, qo_sh = _rows(q_out, torch, index, "q_out", hq, T, d)
+    # (from the pool of the stream that writes them: elsewhere pending work may still use them)
+    def result(out, x, name, heads):
+        if out is not None:
+            return out, *_rows(out, torch, index, name, heads, T, d)
+        if stream is None:
+            out = x.new_empty((T, heads, d))
+        else:
+            with torch.cuda.stream(stream):
+                out = x.new_empty((T, heads, d))
+        return out, out.data_ptr(), heads * d, d
+    q_out, qop, qo_st, qo_sh = result(q_out, q, "q_out", hq)
     if k is not None:
-        kop, ko_st, ko_sh = _rows(k_out, torch, index, "k_out", hk, T, d)
+        k_out, kop, ko_st, ko_sh = result(k_out, k, "k_out", hk)
     pos, p_st, p_sa = rotary._positions(positions, torch, index, T)
     c = _RotateConfig(ABI_VERSION, T, hq, hk, d, int(bool(inverse)), p_st, p_sa, q_st, q_sh, k_st, k_sh,
                       qo_st, qo_sh, ko_st, ko_sh)
