@@ -984,6 +984,15 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
     if (lh == 0) s.part_ml[slot] = make_float2(r.m, r.l);
   }
 }
+
+// The join's groups of 32 threads that share a row, for a row tile of this many parts: fewer than
+// the parts, so that the workgroups of those that begin inside it have room for all rows.
+constexpr int kMergeRows = 8, kMergeRound = 4, kMergeGroups = kThreads / 32;
+__device__ __forceinline__ int join_groups(int parts) {
+  int log_g = 0;
+  while (2 * kMergeRound << log_g < parts && 1 << log_g < kMergeGroups) ++log_g;
+  return log_g;
+}
 }  // namespace
 
 __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, ChunkStep s) {
@@ -1005,10 +1014,11 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
     rt.hi = chunk_key_tile(sg.to, sg.p.c);
     rt.pos0 = sg.tile * sg.p.per;
     rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
-    if (thread_here() == 0 && sg.from > 0 && sg.from <= size) {   // the first part to begin inside it
+    if (thread_here() == 0 && sg.from > 0) {
       const int64_t stop = sg.at + chunk_cost(sg.p, sg.tile);
-      s.joins[part] = {sg.at, stop, size, (int64_t)sg.start + rt.pos0, rt.n_rows, sg.p.c,
-                       chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa, chunk_quotient(stop - 1, size)};
+      const int col = chunk_quotient(sg.from - 1, size), first = part - col - 1, last = chunk_quotient(stop - 1, size);
+      s.joins[part] = {rt.n_rows, col, join_groups(last - first + 1), first, last, sg.at, stop, size,
+                       (int64_t)sg.start + rt.pos0, sg.p.c, chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa};
     }
     if (rt.lo >= rt.hi) return;
     rt.whole = rt.lo == 0 && rt.hi == chunk_key_tiles(sg.p, sg.tile);
@@ -1017,22 +1027,22 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
   });
 }
 
-// Joins the row tiles that more than one part served: workgroup (w, r) takes rows 8 r .. + 7
-// of the one that part w begins inside, if it is the first to do so.  Most are of two or three
-// parts: a round is four (67 MB of parts 15 us; with eight, of which most pass by, 36 us).
+// Joins the row tiles that more than one part served.  The workgroups (w, y) of all parts w that
+// begin inside a row tile share its rows.  Two to four parts are the rule, read in one round (67 MB
+// of parts 15 us; with rounds of eight 36 us); more than eight are read by up to eight groups of 32
+// threads (128 parts of 64 rows 30 -> 6 us; from five parts on, row tiles of four to five took 14
+// us instead of 10.5).  Most workgroups find nothing to do: what they read is one record.
 namespace {
-constexpr int kMergeRows = 8, kMergeRound = 4;
-}
-__global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) {
-  const int w = blockIdx.x + 1;
-  const ChunkJoin jn = s.joins[w];
-  const int r0 = blockIdx.y * kMergeRows, r = r0 + (threadIdx.x >> 5);
-  if (r0 >= jn.n_rows) return;
-  const int c = 4 * (threadIdx.x & 31), rr = min(r, jn.n_rows - 1);
-  float M = -INFINITY, L = 0.f;
-  f32x4 x = {0.f, 0.f, 0.f, 0.f};
-  int lo = 0;   // first key tile of part i
-  for (int i = w - 1; i <= jn.last;) {
+struct Joined {
+  float m, l;
+  f32x4 x;
+  bool whole;   // one part had all key tiles, and wrote the rows
+};
+// Parts [i, end) of row rr, channels c .. + 3.
+__device__ __forceinline__ Joined join_parts(const ChunkStep& s, const ChunkJoin& jn, int i, int end, int rr, int c) {
+  Joined o = {-INFINITY, 0.f, {0.f, 0.f, 0.f, 0.f}, false};
+  int lo = chunk_key_tile(max(i * jn.size - jn.at, (int64_t)0), jn.scale);   // first key tile of part i
+  while (i < end) {
     // a round of parts, all loads first
     float2 ml[kMergeRound];
     f32x4 y[kMergeRound];
@@ -1040,10 +1050,11 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
 #pragma unroll
     for (int k = 0; k < kMergeRound; ++k, ++i) {
       there[k] = false;
-      if (i > jn.last) continue;
+      if (i >= end) continue;
       const int hi = chunk_key_tile(min((i + 1) * jn.size, jn.stop) - jn.at, jn.scale);
-      if (lo == 0 && hi == jn.key_tiles) return;         // written by that part
-      there[k] = lo < hi;
+      const bool all = lo == 0 && hi == jn.key_tiles;
+      o.whole |= all;
+      there[k] = lo < hi && !all;
       if (there[k]) {
         const int64_t slot = (int64_t)chunk_slot(i, lo) * s.slot_rows + rr;
         ml[k] = s.part_ml[slot];
@@ -1051,28 +1062,64 @@ __global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) 
       }
       lo = hi;
     }
-    float mn = M;
+    float mn = o.m;
 #pragma unroll
     for (int k = 0; k < kMergeRound; ++k)
       if (there[k]) mn = fmaxf(mn, ml[k].x);
-    const float mu = mn > -INFINITY ? mn : 0.f, f0 = __builtin_amdgcn_exp2f(M - mu);
-    M = mn;
-    L *= f0;
+    const float mu = mn > -INFINITY ? mn : 0.f, f0 = __builtin_amdgcn_exp2f(o.m - mu);
+    o.m = mn;
+    o.l *= f0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] *= f0;
+    for (int j = 0; j < 4; ++j) o.x[j] *= f0;
 #pragma unroll
     for (int k = 0; k < kMergeRound; ++k) {
       if (!there[k]) continue;
       const float f = __builtin_amdgcn_exp2f(ml[k].x - mu);
-      L = fmaf(f, ml[k].y, L);
+      o.l = fmaf(f, ml[k].y, o.l);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = fmaf(f, y[k][j], x[j]);
+      for (int j = 0; j < 4; ++j) o.x[j] = fmaf(f, y[k][j], o.x[j]);
     }
   }
-  if (r >= jn.n_rows) return;
+  return o;
+}
+}  // namespace
+__global__ __launch_bounds__(kThreads) void k_chunk_merge(int gqa, ChunkStep s) {
+  const int w = blockIdx.x + 1;
+  const ChunkJoin jn = s.joins[w];
+  if (jn.n_rows == 0) return;   // (the rest of the record is not written)
+  const int log_g = jn.log_g;
+  const int r0 = (jn.col * gridDim.y + blockIdx.y) * (kMergeRows >> log_g);
+  if (r0 >= jn.n_rows) return;
+  const int group = threadIdx.x >> 5, c = 4 * (threadIdx.x & 31);
+  const int r = r0 + (group >> log_g), rr = min(r, jn.n_rows - 1);
+  Joined o;
+  if (log_g == 0) {
+    o = join_parts(s, jn, jn.first, jn.last + 1, rr, c);
+  } else {
+    __shared__ f32x4 xs[kMergeGroups][32];
+    __shared__ float2 mls[kMergeGroups];
+    const int g = 1 << log_g, at = group & (g - 1), each = (jn.last - jn.first + g) >> log_g;
+    o = join_parts(s, jn, jn.first + at * each, min(jn.first + (at + 1) * each, jn.last + 1), rr, c);
+    xs[group][threadIdx.x & 31] = o.x;
+    if (c == 0) mls[group] = make_float2(o.m, o.l);
+    o.whole = __syncthreads_or(o.whole);
+    if (at) return;
+    for (int k = 1; k < g; ++k) o.m = fmaxf(o.m, mls[group + k].x);
+    const float mu = o.m > -INFINITY ? o.m : 0.f;
+    o.l = 0.f;
+    o.x = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < g; ++k) {
+      const float f = __builtin_amdgcn_exp2f(mls[group + k].x - mu);
+      const f32x4 y = xs[group + k][threadIdx.x & 31];
+      o.l = fmaf(f, mls[group + k].y, o.l);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o.x[j] = fmaf(f, y[j], o.x[j]);
+    }
+  }
+  if (o.whole || r >= jn.n_rows) return;
   const int i = by_gqa(s, r);
   uint16_t* op = s.out + (jn.row + i) * s.o_st + (jn.head + r - i * gqa) * s.o_sh + c;
-  *(u32x2*)op = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
+  *(u32x2*)op = (u32x2){pack_bf16(o.x[0] / o.l, o.x[1] / o.l), pack_bf16(o.x[2] / o.l, o.x[3] / o.l)};
 }
 
 // Rows of a partial result: those of the largest row tile a call of `total` rows can have.

@@ -238,13 +238,16 @@ struct BlockStep {          // a decode step on the block cache
   float2* part_ml;          // [kParts + 2 B H_kv][gqa] (maximum in log2 units, sum)
 };
 
-struct ChunkJoin {          // a row tile that several parts serve, by the first that begins inside it
+struct ChunkJoin {          // the row tile that a part begins inside
+  int32_t n_rows;           // (position, head) rows; 0: the part begins inside none
+  int32_t col;              // parts that begin inside it before this one
+  int32_t log_g;            // threads in groups of 32 that share a row: 2^log_g
+  int32_t first, last;      // parts that serve it
   int64_t at, stop, size;   // the row tile on the line, the length of a part
   int64_t row;              // its first row of the packed tensors
-  int32_t n_rows;           // (position, head) rows; 0: nothing to join
   ChunkScale scale;         // of its place
   int32_t key_tiles;        // of all its keys
-  int32_t head, last;       // first query head, last part
+  int32_t head;             // first query head
 };
 
 struct ChunkStep {          // attention of new tokens over the block cache and themselves

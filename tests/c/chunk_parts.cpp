@@ -110,30 +110,34 @@ int main() {
         next = v.hi;
       }
       CHECK(next == t.v);
-      // the join: by the first part that begins inside the row tile
-      int joins = 0;
+      // the join: every part that begins inside the row tile knows the first one that serves it
+      int joins = 0, joined = 0;
       for (int w = 1; w < kChunkParts; ++w) {
         const int64_t x0 = w * size;
-        if (x0 >= total || x0 <= t.at || x0 >= t.stop || x0 - size > t.at) continue;
+        if (x0 >= total || x0 <= t.at || x0 >= t.stop) continue;
+        const int col = chunk_quotient(x0 - t.at - 1, size), first = w - col - 1;
+        const int last = chunk_quotient(t.stop - 1, size);
+        CHECK(first >= 0 && first * size <= t.at && (first + 1) * size > t.at && w <= last && last < kChunkParts);
+        CHECK(col == joins);
+        ++joins;
         std::vector<Served> got;
         bool whole = false;
-        CHECK(x0 - t.at <= size);   // (what the attention kernel goes by)
-        for (int k = w - 1; k <= chunk_quotient(t.stop - 1, size); ++k) {
+        for (int k = first; k <= last; ++k) {
           const int lo = chunk_key_tile(std::max<int64_t>(k * size - t.at, 0), places[t.s].c);
           const int hi = chunk_key_tile(std::min(k * size + size, t.stop) - t.at, places[t.s].c);
           if (lo >= hi) continue;
           if (lo == 0 && hi == t.v) whole = true;
           got.push_back({k, lo, hi, chunk_slot(k, lo)});
         }
-        ++joins;
         CHECK(got.size() == served[j].size());
         for (size_t k = 0; k < got.size(); ++k) {
           CHECK(got[k].part == served[j][k].part && got[k].lo == served[j][k].lo && got[k].hi == served[j][k].hi);
           CHECK(whole ? served[j][k].slot < 0 : got[k].slot == served[j][k].slot);
         }
+        if (col == 0) joined = last - first;
       }
-      CHECK(joins <= 1);
-      if (served[j].size() > 1) CHECK(joins == 1);
+      CHECK(joins == joined);   // parts that share the rows: all but the first
+      if (served[j].size() > 1) CHECK(joins > 0);
     }
   }
   printf("ok\n");

@@ -127,6 +127,17 @@ def test_rows_of_a_workgroup(rows, hq):
     _run(_cache([300, 1100], hq, 1, sum(lens), seed=rows, extra=1200), [300, 1100], lens, seed=rows + hq)
 
 
+@pytest.mark.parametrize("held,lens", [([30001], [3]), ([30001], [9]), ([20000, 7], [60, 2]), ([12000, 9000], [1, 33]),
+                                       ([1500], [100])])
+@pytest.mark.parametrize("hq,hkv", [(6, 1), (2, 2)])
+def test_many_parts(held, lens, hq, hkv):
+    """Row tiles that many workgroups serve, with anything at all in the workspace."""
+    bc = _cache(held, hq, hkv, sum(lens), seed=60)
+    for byte in (0x7f, 0x80, 0xff, 0x01):
+        bc.chunk_workspace.fill_(byte)
+        _run(bc, held, lens, seed=61)
+
+
 def test_many_places():
     """300 places (more than a wave's 64 lanes see at once), some empty, a few long."""
     rng = np.random.default_rng(7)
