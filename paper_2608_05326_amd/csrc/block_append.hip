@@ -8,11 +8,15 @@
 namespace qv {
 
 // One workgroup per (block that the new tokens touch, KV head, keys or values); keys that are
-// rotated may take several heads, one behind the other.  The angles of a block's rows and pairs
+// rotated may take two heads, one behind the other.  The angles of a block's rows and pairs
 // are computed once, by all threads, and kept in LDS: a pair's cosine and sine cost some 30
-// vector instructions, as much as the rest of its work in six heads.  The place's last, open
+// vector instructions.  The first head's rows are on their way meanwhile.  A channel then is one
+// product and one fused product, with the same roundings as k_rotate's.  The place's last, open
 // block is written by the workgroup of the first one, after it has read the old open block: both
 // are in the same rows.
+// A token and head is 512 bytes read and 256 written.  Bound by the chain of a workgroup (place,
+// positions, angles, rows, largest magnitude, codes; four workgroups of it to a unit), not yet by
+// memory: 11770 tokens of 8 heads 28 us (25 without the rotation), 18503 45 us, 2.5 TB/s.
 namespace {
 // The angles (cosine and sine of pair i at angle_at(row, i)) are in the place of the values'
 // codes: four workgroups a compute unit.
@@ -137,6 +141,8 @@ int64_t block_append_groups(int64_t total, int n_seqs, int H_kv) { return 2 * to
 
 hipError_t launch_block_append(const BlockArgs& a, AppendRows r, const RotaryArgs& rot, hipStream_t st) {
   const int64_t n = touched(r.total, a.B);
+  // two heads where the workgroups are many all the same (18503 tokens: one head 58 us, two 49,
+  // four 54)
   r.heads = 1;
   if (r.rotate)
     while (r.heads < 2 && r.heads < a.H_kv && n * a.H_kv / (2 * r.heads) >= 512) r.heads *= 2;

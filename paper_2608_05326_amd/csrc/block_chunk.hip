@@ -6,6 +6,20 @@
 //
 // The keys of a sequence are its tiles of 64 positions: complete blocks are pages (int8 codes
 // with a scale), the others are rows in bf16, of the open block and then of the chunk.
+//
+// One pass with a running maximum and sum, S^T = K Q^T and O^T = V^T P^T by 32x32x16 bf16
+// products, in which codes are exact.  256 workgroups take equal parts of all the work (how it is
+// cut: qv_chunk.h), partial rows are joined by a second launch.  By the rows (position, head) of
+// a place and KV head:
+//   to 32 or 64   (drafted tokens) bound by the pages' bytes: a wave has its own pages, straight
+//                 from memory to LDS; 31 places, 63 tokens over 950 MB of cache 187 us and 7
+//                 for the join (5.0 TB/s).  64 rows a wave pair cost twice 32.
+//   more          (pieces of prompts) bound by the products and the exponentials between them:
+//                 eight waves of 32 rows share tiles that are expanded once, into LDS; 4096
+//                 tokens of 64 / 8 heads over 61440 take 7.6 to 8.0 ms (1.07 to 1.12 PFLOP/s; a
+//                 large matrix product reaches 1.39), the matrix unit busy 53% at 1.98 GHz.
+// The reference of a row's weights is raised by whole powers of two, so that weights in bf16 that
+// are in flight scale exactly.
 #include <algorithm>
 
 #include "qv_block.h"
@@ -56,8 +70,8 @@ __device__ __forceinline__ u32x4 codes_bf16(uint32_t w0, uint32_t w1) {
   return (u32x4){a[0], a[1], b[0], b[1]};
 }
 
-// A value, or threadIdx.x, not to be seen through: what is derived from it is computed where it is used
-// (hoisted out of the walk over segments, it would fill the registers that the products need).
+// A value, or threadIdx.x, not to be seen through: what is derived from it is computed where it is
+// used (hoisted out of the walk over segments, it would fill the registers that the products need).
 __device__ __forceinline__ int here(int x) {
   asm volatile("" : "+v"(x));
   return x;
@@ -601,7 +615,8 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
       for (int i = 0; i < 4; ++i) x[i] = fmaf(f, y[i], x[i]);
     }
     if (rt.whole) {
-      *(u32x2*)(out_row(a, s, sg, rt, g, rr) + c) = (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
+      *(u32x2*)(out_row(a, s, sg, rt, g, rr) + c) =
+          (u32x2){pack_bf16(x[0] / L, x[1] / L), pack_bf16(x[2] / L, x[3] / L)};
     } else {
       const int64_t slot = (int64_t)chunk_slot(part, rt.lo) * s.slot_rows + rr;
       *(f32x4*)(s.part_o + slot * kHeadDim + c) = x;
@@ -702,7 +717,8 @@ __device__ __forceinline__ void wide_values(Running& r, u32x4 (&pw)[4], Read rea
 // Key tiles 0 .. n - 1 of a source (pages or rows in bf16).  Step e of the loop: the products
 // of tile e's keys, and beside them the next tile's keys and its own values are put into the
 // arrays that were last read in the step before and the loads of those behind them start; then
-// the products of the values of the tile before, and beside them the weights of tile e.  One step more ends with the last tile's values.
+// the products of the values of the tile before, and beside them the weights of tile e.  One step
+// more ends with the last tile's values.
 //   src.peek(e, f), src.look()       starts to read what is known: of tile e for logits(), of f
 //                                    for the loads after look(); both come long before their use
 //   src.load_k(e), src.load_v(e)     into registers
@@ -964,9 +980,10 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
     const int wpos0 = sg.p.held + rt.pos0 + by_gqa(s, wave * 32);
     const int wpos1 = idle ? -1 : sg.p.held + rt.pos0 + by_gqa(s, min(wave * 32 + 31, rt.n_rows - 1));
     const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr), vkey = 8 * lh + ((lane >> 2) & 3);
-    RowSource src = {a, s, sg, logit_scale(a, ex), t0, sg.p.held + i_row, wpos0, wpos1, sg.p.held + sg.p.n - 1, lane, wave, tid >> 4,
-                     vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1),
-                     sodd};
+    const int vbase =
+        vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1);
+    RowSource src = {a,     s,     sg,                    logit_scale(a, ex), t0,   sg.p.held + i_row,
+                     wpos0, wpos1, sg.p.held + sg.p.n - 1, lane,               wave, tid >> 4,          vbase, sodd};
     wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), q, r, sm);
   }
 
@@ -1016,7 +1033,8 @@ __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, 
     rt.n_rows = (chunk_end(sg.p, sg.tile) - rt.pos0) * a.gqa;
     if (thread_here() == 0 && sg.from > 0) {
       const int64_t stop = sg.at + chunk_cost(sg.p, sg.tile);
-      const int col = chunk_quotient(sg.from - 1, size), first = part - col - 1, last = chunk_quotient(stop - 1, size);
+      const int col = chunk_quotient(sg.from - 1, size), first = part - col - 1;
+      const int last = chunk_quotient(stop - 1, size);
       s.joins[part] = {rt.n_rows, col, join_groups(last - first + 1), first, last, sg.at, stop, size,
                        (int64_t)sg.start + rt.pos0, sg.p.c, chunk_key_tiles(sg.p, sg.tile), sg.g * a.gqa};
     }
