@@ -96,6 +96,22 @@ def test_heads(hq, hk, T):
         assert ko is None
 
 
+@pytest.mark.parametrize("T,hq,hk", [(1500, 40, 3), (4200, 20, 3), (9001, 20, 3), (3000, 64, 8)])
+def test_more_tokens_take_more_heads_a_workgroup(T, hq, hk):
+    import paper_2608_05326_amd as qv
+    import torch
+    r = qv.Rotary(sections=(16, 24, 24))
+    q, k = _bf16(T, hq, D, seed=hq), _bf16(T, hk, D, seed=hk)
+    pos = _positions(T, 3, seed=hq)
+    qo, ko = qv.rotate(q, k, pos, r)
+    rows = slice(T - 300, None)
+    _check(qo[rows], q[rows], pos[rows], r)
+    _check(ko[rows], k[rows], pos[rows], r)
+    for x, o in ((q, qo), (k, ko)):       # every row: its own call, in pieces of few tokens, gives the same bits
+        parts = [qv.rotate(x[i:i + 250], None, pos[i:i + 250], r)[0] for i in range(0, T, 250)]
+        assert torch.equal(torch.cat(parts), o)
+
+
 def test_positions_of_every_size():
     """The whole range of 32 bits, where an fp32 angle would be off by turns."""
     import paper_2608_05326_amd as qv
