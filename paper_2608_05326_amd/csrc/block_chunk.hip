@@ -12,8 +12,8 @@
 // cut: qv_chunk.h), partial rows are joined by a second launch.  By the rows (position, head) of
 // a place and KV head:
 //   to 32 or 64   (drafted tokens) bound by the pages' bytes: a wave has its own pages, straight
-//                 from memory to LDS; 28 places, 113 tokens over 966 MB of cache 190 us and 6
-//                 for the join (5.0 TB/s).  64 rows a wave pair cost twice 32.
+//                 from memory to LDS; 28 places, 113 tokens over 966 MB of cache 185 us and 6
+//                 for the join (5.2 TB/s).  64 rows a wave pair cost twice 32.
 //   more          (pieces of prompts) bound by the products and the exponentials between them:
 //                 eight waves of 32 rows share tiles that are expanded once, into LDS; 4096
 //                 tokens of 64 / 8 heads over 61440 take 7.6 to 8.0 ms (1.07 to 1.12 PFLOP/s; a
