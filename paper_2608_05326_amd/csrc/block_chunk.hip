@@ -481,7 +481,9 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
       for (int i = 0; i < 8; ++i) dma16(a.v_codes + e + v_from + 1024 * i, sv + 1024 * i);
     };
     int64_t e = entry(__builtin_ctzll(live));
+    // (the waits below count loads: the keys' are the older eight, here too)
     load_k(e);
+    asm volatile("; values behind keys" ::: "memory");
     load_v(e);
     while (live) {
       const int j = __builtin_ctzll(live);
