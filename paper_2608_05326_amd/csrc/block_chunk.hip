@@ -35,9 +35,6 @@ constexpr int kRowBytes = 2 * kHeadDim;
 // the running maximum is raised (and the output rescaled) only when a tile exceeds it by
 // this many powers of two: P stays below 256
 constexpr float kLazy = 8.f;
-// a row's query is scaled by a power of two that takes its largest entry to [2^-20, 2^-19):
-// products with the largest keys, of codes or bf16, and their sums stay in range
-constexpr int kQueryExp = -20;
 
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
@@ -192,11 +189,11 @@ struct RowTile {
   bool whole;                // all of the row tile's keys
 };
 
-// The query of one row as the B operand of eight k-steps, scaled (a power of two) into
-// bf16's range; returns the power of two that takes the products back.  WIDE: k-step ks
+// The query of one row as the B operand of eight k-steps, scaled by a power of two (bf16 stays
+// bf16); returns the power of two that takes the products back.  WIDE: k-step ks
 // covers channels 16 ks + 8 lh + 0 .. 7, else 32 (ks / 2) + 16 lh + 8 (ks % 2) + 0 .. 7.
 template <bool WIDE>
-__device__ __forceinline__ int load_query(const uint16_t* p, int lh, u32x4 (&q)[8]) {
+__device__ __forceinline__ int load_query(const BlockArgs& a, const uint16_t* p, int lh, u32x4 (&q)[8]) {
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks)
     q[ks] = *(const u32x4*)(p + (WIDE ? 16 * ks + 8 * lh : 32 * (ks >> 1) + 16 * lh + 8 * (ks & 1)));
@@ -207,17 +204,18 @@ __device__ __forceinline__ int load_query(const uint16_t* p, int lh, u32x4 (&q)[
   const auto swapped = __builtin_amdgcn_permlane32_swap(am, am, false, false);
   const uint32_t am0 = swapped[0], am1 = swapped[1];
   am = max(am0, am1);
-  const int ex = max((int)(am >> 23), 1) - 127;    // (a row of subnormals keeps its scale)
+  // (a row of subnormals: their scale)
+  const int shift = chunk_query_shift(max((int)(am >> 23), 1) - 127, __builtin_amdgcn_frexp_expf(a.scale_log2));
 #pragma unroll
   for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const uint32_t w = q[ks][j];
-      q[ks][j] = pack_bf16(ldexpf(lo_f32(w), kQueryExp - ex), ldexpf(hi_f32(w), kQueryExp - ex));
+      q[ks][j] = pack_bf16(ldexpf(lo_f32(w), -shift), ldexpf(hi_f32(w), -shift));
     }
-  return ex - kQueryExp;
+  return shift;
 }
-// Log2 units per raw logit of keys with the scale ks: scale_log2 2^ex ks, held as a mantissa
+// Log2 units per raw logit of keys with the scale ks: scale_log2 2^shift ks, held as a mantissa
 // and a power of two that comes last: products of small queries and large keys are logits of
 // ordinary size.
 struct LogitScale {
@@ -228,8 +226,8 @@ struct LogitScale {
     return x == INFINITY ? __FLT_MAX__ : x;   // (a product of zero is a logit of zero)
   }
 };
-__device__ __forceinline__ LogitScale logit_scale(const BlockArgs& a, int ex) {
-  return {__builtin_amdgcn_frexp_mantf(a.scale_log2), __builtin_amdgcn_frexp_expf(a.scale_log2) + ex};
+__device__ __forceinline__ LogitScale logit_scale(const BlockArgs& a, int shift) {
+  return {__builtin_amdgcn_frexp_mantf(a.scale_log2), __builtin_amdgcn_frexp_expf(a.scale_log2) + shift};
 }
 
 // Running maximum (log2 units), sum and output of one row: o[c][i] is channel
@@ -441,8 +439,8 @@ __device__ __forceinline__ void attend_few(const BlockArgs& a, const ChunkStep& 
   auto page_at = [&](int t0) { return t0 + lane * n_kg < page_end ? page_of(a, sg.seq, t0 + lane * n_kg) : -1; };
   int page = page_at(rt.lo + kg);
   u32x4 q[8];
-  const int ex = load_query<false>(s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
-  const LogitScale scale = logit_scale(a, ex);
+  const int shift = load_query<false>(a, s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
+  const LogitScale scale = logit_scale(a, shift);
   Running r;
   clear(r);
   // row lr of an A operand is this key of 32; a lane's logits st[i] are those of keys 16 lh + i
@@ -882,12 +880,12 @@ struct PageSource {
 };
 
 // The pages of tiles [lo, hi), all of whose keys every row sees.
-__device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg, int lo, int hi, bool idle, int ex,
-                                           const u32x4 (&q)[8], Running& r, const Shared& sm, PageRef* list,
-                                           int* scnt) {
+__device__ __forceinline__ void wide_pages(const BlockArgs& a, const Segment& sg, int lo, int hi, bool idle,
+                                           int shift, const u32x4 (&q)[8], Running& r, const Shared& sm,
+                                           PageRef* list, int* scnt) {
   const int tid = thread_here(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 31, lh = lane >> 5, krow = key_of_row(lr);
-  PageSource src = {a, list, logit_scale(a, ex), sg.g, tid,
+  PageSource src = {a, list, logit_scale(a, shift), sg.g, tid,
                     (tid >> 3) * kRowBytes + 16 * ((2 * (tid & 7)) ^ swz_k(tid >> 3)),
                     (tid >> 2) * (2 * kBlk) + 16 * ((2 * (tid & 3)) ^ swz_c(tid >> 2)),
                     lr * (2 * kBlk) + 16 * (lh ^ swz_c(lr)), idle};
@@ -995,11 +993,11 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
   const int head = sg.g * a.gqa + rowc - (i_row - rt.pos0) * a.gqa;
   const bool idle = wave * 32 >= rt.n_rows;
   u32x4 q[8];
-  const int ex = load_query<true>(s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
+  const int shift = load_query<true>(a, s.q + (sg.start + i_row) * s.q_st + head * s.q_sh, lh, q);
   Running r;
   clear(r);
   const int n_blk = sg.p.held / kBlk;
-  if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, ex, q, r, sm, list, scnt);
+  if (rt.lo < n_blk) wide_pages(a, sg, rt.lo, min(rt.hi, n_blk), idle, shift, q, r, sm, list, scnt);
   if (rt.hi > n_blk) {
     // first and last position of the wave's rows
     const int wpos0 = sg.p.held + rt.pos0 + by_gqa(s, wave * 32);
@@ -1007,8 +1005,8 @@ __device__ __forceinline__ void attend_many(const BlockArgs& a, const ChunkStep&
     const int t0 = max(rt.lo, n_blk), krow = key_of_row(lr), vkey = 8 * lh + ((lane >> 2) & 3);
     const int vbase =
         vkey * kRowBytes + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_v(vkey)) + 8 * (lane & 1);
-    RowSource src = {a,     s,     sg,                    logit_scale(a, ex), t0,   sg.p.held + i_row,
-                     wpos0, wpos1, sg.p.held + sg.p.n - 1, lane,               wave, tid >> 4,          vbase, sodd};
+    RowSource src = {a,     s,     sg,                     logit_scale(a, shift), t0,   sg.p.held + i_row,
+                     wpos0, wpos1, sg.p.held + sg.p.n - 1, lane,                  wave, tid >> 4,          vbase, sodd};
     wide_loop(src, rt.hi - t0, krow * kRowBytes + 16 * (lh ^ swz_k(krow)), q, r, sm);
   }
 

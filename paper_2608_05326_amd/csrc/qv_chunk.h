@@ -116,6 +116,16 @@ QV_HD int chunk_key_tile(int64_t x, const ChunkScale& c) {
   return c.blocks + (int)((uint32_t)((z + 127) >> 7) + 4) / 5;      // 640 a tile
 }
 
+// A row's query, its largest magnitude in [2^ex, 2^(ex + 1)), is taken times 2^-shift, which comes
+// back with the logits' scale m 2^scale_exp, 1/2 <= m < 1, as 2^shift.  Into [2^-20, 2^-19):
+// products with the largest keys, of codes or bf16, and their sums stay in range.  A row of small
+// numbers or zeros only so far that the scale of its logits stays a normal number: masked ones
+// are -infinity, which times zero were no number.
+QV_HD int chunk_query_shift(int ex, int scale_exp) {
+  const int s = ex + 20, least = -125 - scale_exp;
+  return s < least ? least : s;
+}
+
 // Length of a part, given the line's.
 QV_HD int64_t chunk_part(int64_t total) {
   const int64_t s = (total + kChunkParts - 1) / kChunkParts;
