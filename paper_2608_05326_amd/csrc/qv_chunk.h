@@ -120,10 +120,12 @@ QV_HD int chunk_key_tile(int64_t x, const ChunkScale& c) {
 // back with the logits' scale m 2^scale_exp, 1/2 <= m < 1, as 2^shift.  Into [2^-20, 2^-19):
 // products with the largest keys, of codes or bf16, and their sums stay in range.  A row of small
 // numbers or zeros only so far that the scale of its logits stays a normal number: masked ones
-// are -infinity, which times zero were no number.
+// are -infinity, which times zero were no number.  A row of large numbers only so far that the
+// scale stays below 2^100: keys as small as it is large give logits of ordinary size, from
+// products that are normal numbers (where products are out of range, their logits are, too).
 QV_HD int chunk_query_shift(int ex, int scale_exp) {
-  const int s = ex + 20, least = -125 - scale_exp;
-  return s < least ? least : s;
+  const int s = ex + 20, least = -125 - scale_exp, most = 100 - scale_exp;
+  return s < least ? least : s > most ? most : s;
 }
 
 // Length of a part, given the line's.

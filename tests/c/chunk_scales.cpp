@@ -1,5 +1,6 @@
 // The power of two that a row's query is taken by in the chunk attention, for every exponent of its
-// largest entry and every softmax scale: the scale of its logits is a normal number.
+// largest entry and every softmax scale: the scale of its logits is a normal number, and small enough
+// that products of logits of ordinary size are normal numbers, too.
 #include <cmath>
 #include <cstdio>
 #include <initializer_list>
@@ -27,11 +28,13 @@ int main() {
       for (int ex = -126; ex <= 127; ++ex) {
         const int shift = chunk_query_shift(ex, scale_exp);
         const float sc = std::ldexp(m, scale_exp + shift);
-        CHECK(sc >= 0x1p-126f);
+        CHECK(sc >= 0x1p-126f && sc < 0x1p100f);
         // the largest entries of such a row (the smallest of all with ex = -126), and the smallest
         const float most = ex == -126 ? 0x1p-133f : std::ldexp(1.f, ex);
         CHECK(std::ldexp(std::ldexp(most, -shift), shift) == most);
-        CHECK(std::ldexp(1.9921875f * most, -shift) <= 0x1p-19f || shift > ex + 20);
+        // where products with the largest keys are out of range, logits of them are
+        const double row = std::ldexp(1.9921875 * most, -shift);
+        CHECK(row <= 0x1p-19 || (row * 128 * 127 < 0x1p127 && sc >= 1.f));
       }
     }
   printf("ok\n");

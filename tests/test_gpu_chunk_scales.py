@@ -55,3 +55,31 @@ def test_small_queries_beside_large_keys_at_small_scales(lens):
         out = torch.full_like(q, 7.0)
         bc.attend_chunk(0, q, k, v, _cu(lens), out)
         _check(bc, held, lens, q, k, v, out, scale=scale)
+
+
+def _keys(shape, e, seed):
+    """+-[1, 2) 2^e in bf16: no subnormal numbers among small keys."""
+    import torch
+    g = torch.Generator().manual_seed(seed)
+    x = 1.0 + torch.rand(*shape, generator=g) * 0.99
+    return (x * (torch.randint(0, 2, shape, generator=g) * 2 - 1) * 2.0 ** e).bfloat16().cuda()
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("log_scale,e,pages", [(-3.5, 112, True), (-3.5, 120, True), (-3.5, 124, False), (64, 0, True),
+                                               (64, 40, True), (64, 59, False), (10, 90, True)])
+def test_large_queries_beside_small_keys(lens, log_scale, e, pages):
+    """Logits of ordinary size from queries of 2^e: keys as much smaller, past the scale as well."""
+    import torch
+    held = [200, 77] if pages else [40, 33]
+    T, scale = sum(lens), 2.0 ** log_scale
+    down = -e if log_scale < 0 else -e - log_scale
+    bc = _scaled(_cache(held, 4, 2, T, seed=74, extra=400, fill=0.0), scale, T)
+    bc.k_scale *= 2.0 ** down
+    bc.k_tail.copy_(_keys(bc.k_tail.shape, down, seed=75))
+    q, _, v = _rows(T, 4, 2, seed=76)
+    q = (q.float().clamp(-4, 4) * 2.0 ** (e - 2)).bfloat16()
+    k = _keys(v.shape, down, seed=77)
+    out = torch.full_like(q, 7.0)
+    bc.attend_chunk(0, q, k, v, _cu(lens), out)
+    _check(bc, held, lens, q, k, v, out, scale=scale)
