@@ -861,16 +861,19 @@ class BlockCache:
         self._call(self.lib.qevict_block_append, layer, *rows, cu, n, T,
                    None if rotary is None else ctypes.byref(rotary._c), *pos)
 
-    def advance(self, cu_tokens=None, counts=None):
+    def advance(self, cu_tokens=None, counts=None, total_tokens=None):
         """After a step's last layer: lens + 1 where a place holds a sequence that has room;
-        with cu_tokens (and counts) lens + the tokens that append() took."""
+        with cu_tokens (and counts) lens + the tokens that append() took.  total_tokens: the rows
+        of append()'s k and v, to which it cuts bounds that lie past them; without it cu_tokens
+        has to lie within the rows (bounds below zero are zero either way)."""
         t = self.torch
         with self._on_stream():
             live = (self.lens >= 0) & (self.lens < self.cfg.max_context)
             if cu_tokens is None:
                 self.lens += live.to(self.lens.dtype)
                 return
-            n = (cu_tokens[1:] - cu_tokens[:-1]).clamp_(min=0)
+            cu = cu_tokens.clamp(0, total_tokens)
+            n = (cu[1:] - cu[:-1]).clamp_(min=0)
             if counts is not None:
                 n = t.minimum(n, counts.clamp(min=0))
             self.lens += t.where(live, t.minimum(n, self.cfg.max_context - self.lens), 0).to(self.lens.dtype)
