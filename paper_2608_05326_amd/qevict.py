@@ -867,14 +867,19 @@ class BlockCache:
         of append()'s k and v, to which it cuts bounds that lie past them; without it cu_tokens
         has to lie within the rows (bounds below zero are zero either way)."""
         t = self.torch
+        if cu_tokens is None and (counts is not None or total_tokens is not None):
+            raise ValueError("counts and total_tokens are for cu_tokens")
         with self._on_stream():
             live = (self.lens >= 0) & (self.lens < self.cfg.max_context)
             if cu_tokens is None:
                 self.lens += live.to(self.lens.dtype)
                 return
+            index, B = self.lens.get_device(), self.cfg.batch
+            _int32(cu_tokens, t, index, "cu_tokens", B + 1)   # (others would be broadcast)
             cu = cu_tokens.clamp(0, total_tokens)
             n = (cu[1:] - cu[:-1]).clamp_(min=0)
             if counts is not None:
+                _int32(counts, t, index, "counts", B)
                 n = t.minimum(n, counts.clamp(min=0))
             self.lens += t.where(live, t.minimum(n, self.cfg.max_context - self.lens), 0).to(self.lens.dtype)
 

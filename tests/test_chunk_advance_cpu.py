@@ -47,3 +47,29 @@ def test_rows_and_room():
     cu = [-1, 50, 60, 70, 80, 1 << 30]
     c.advance(torch.tensor(cu, dtype=torch.int32), total_tokens=75)
     assert c.lens.tolist() == [a + n for a, n in zip(lens, _taken(cu, 75, None, lens, 300))]
+
+
+@pytest.mark.parametrize("cu,counts", [
+    ([0, 5], None), ([0, 1, 2], None), ([0, 1, 2, 3, 4], None), ([0, 1, 2, 3], [1]), ([0, 1, 2, 3], [1, 1]),
+    ([0, 1, 2, 3], [[1, 1, 1]]), ([[0, 1, 2, 3]], None), ([0.0, 1.0, 2.0, 3.0], None), ([0, 1, 2, 3], [True] * 3),
+], ids=str)
+def test_refusals(cu, counts):
+    """As append() refuses them; broadcast, they would move every place."""
+    c = _Lens([10, 0, 90], 300)
+    x = torch.tensor(cu)
+    x = x if x.is_floating_point() else x.to(torch.int32)
+    y = None if counts is None else torch.tensor(counts)
+    y = y if y is None or y.dtype is torch.bool else y.to(torch.int32)
+    with pytest.raises(ValueError):
+        c.advance(x, y)
+    with pytest.raises(ValueError):
+        c.advance(torch.arange(4), None)       # int64
+    assert c.lens.tolist() == [10, 0, 90]
+
+
+def test_counts_without_bounds_are_refused():
+    c = _Lens([10, 0, 90], 300)
+    for kw in (dict(counts=torch.tensor([1, 1, 1], dtype=torch.int32)), dict(total_tokens=3)):
+        with pytest.raises(ValueError):
+            c.advance(**kw)
+    assert c.lens.tolist() == [10, 0, 90]
