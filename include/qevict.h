@@ -587,10 +587,12 @@ qevict_status qevict_block_append(const qevict_block_config *cfg, const qevict_b
  *   q, out [total, H_q, d], k, v [total, H_kv, d] bf16 packed
  *   workspace  device memory of qevict_block_chunk_workspace_size bytes for total_tokens or
  *              more, 256-byte aligned, overwritten: calls that may overlap need one each
- * Accuracy as qevict_prompt_attend's (the weights beside codes are rounded to bf16 with
- * their block's value scale; a weight below 2^-126 of the row's largest may count as zero).
+ * Accuracy as qevict_prompt_attend's: a weight is rounded to bf16 (2^-8 of itself), beside codes
+ * with its block's value scale s in it, where qevict_block_attend rounds to fp16 (2^-11).  A
+ * weight below 2^-126 of the row's largest may count as zero, beside codes below 2^-126 / s
+ * (2^-26 for the smallest scale of a stored block, 2^-100: values below 2^-93).
  * A value that is not finite reaches the rows that attend to it and no other.  The sums run
- * in an order that depends on the lengths only: a call is bitwise repeatable.
+ * in an order that depends on the lengths and the table only: a call is bitwise repeatable.
  * total_tokens * H_q <= 2^30; token strides of k and v below 2^23. */
 typedef struct {
   int32_t abi_version;

@@ -20,6 +20,12 @@
 //                 large matrix product reaches 1.39), the matrix unit busy 53% at 1.98 GHz.
 // The reference of a row's weights is raised by whole powers of two, so that weights in bf16 that
 // are in flight scale exactly.
+//
+// Weights are rounded to bf16 (2^-8 of themselves) and not to fp16 (2^-11), as a single token's
+// are beside codes: they carry their block's value scale, which needs bf16's range, so that pages
+// and rows in bf16 add to the same 64 sums a lane.  (With the scale left to the products, as there,
+// each of the sums takes another fused product a block.)  Logits, maximum, sums and outputs are
+// fp32.
 #include <algorithm>
 
 #include "qv_block.h"

@@ -825,7 +825,8 @@ class BlockCache:
         tokens held and to its chunk's rows up to itself.  q, out: bf16 [T, H_q, d]; k, v: bf16
         [T, H_kv, d]; strides as in prompt_attend; T at most the config's chunk_tokens.  Nothing
         is stored: append() does, afterwards.  Rows of places that hold no sequence (a negative
-        length), and those past max_context, are left as they were."""
+        length), and those past max_context, are left as they were.  Weights are rounded to bf16
+        as prompt_attend's are; attend(), for single tokens, rounds those beside codes to fp16."""
         t, c, i = self.torch, self.cfg, self.device.index
         T = q.shape[0]
         if T > c.chunk_tokens:

@@ -83,3 +83,37 @@ def test_large_queries_beside_small_keys(lens, log_scale, e, pages):
     out = torch.full_like(q, 7.0)
     bc.attend_chunk(0, q, k, v, _cu(lens), out)
     _check(bc, held, lens, q, k, v, out, scale=scale)
+
+
+@pytest.mark.parametrize("lens", LENS, ids=str)
+@pytest.mark.parametrize("log_s", [-80, -81, -100])
+def test_values_of_the_smallest_scales(lens, log_s):
+    """Weights are rounded with their block's value scale s in them: one below 2^-126 / s of the row's
+    largest may count as zero, which n keys bring to n 2^-126 / s max |v|.  Queries of 4: sum |q k|
+    scale below 2^6, a logit off by 2^-24 x 128 x 2^6 = 2^-11, twice."""
+    import torch
+    held, T, s = [6400, 130], sum(lens), 2.0 ** log_s
+    bc = _cache(held, 4, 2, T, seed=78, extra=400, fill=0.0)
+    bc.v_scale.fill_(s)
+    bc.v_tail.copy_(bc.v_tail.float() * (32 * s))
+    q, k, v = _rows(T, 4, 2, seed=79, scale=4.0)
+    v = (v.float() * (32 * s)).bfloat16()
+    out = torch.full_like(q, 7.0)
+    bc.attend_chunk(0, q, k, v, _cu(lens), out)
+    at = 0
+    for p, (a, n) in enumerate(zip(held, lens)):
+        pages = bc.table[p, :a // N].long()
+        mask = torch.arange(a + n, device="cuda")[None] <= torch.arange(a, a + n, device="cuda")[:, None]
+        for h in range(4):
+            g = h // 2
+            kk = (bc.k_codes[0, pages, g].double() * bc.k_scale[0, pages, g].double()[:, None, None]).reshape(-1, D)
+            vv = (bc.v_codes[0, pages, g].double() * s).transpose(1, 2).reshape(-1, D)
+            kk = torch.cat([kk, bc.k_tail[0, p, g, :a % N].double(), k[at:at + n, g].double()])
+            vv = torch.cat([vv, bc.v_tail[0, p, g, :a % N].double(), v[at:at + n, g].double()])
+            w = q[at:at + n, h].double() @ kk.t().contiguous() * D ** -0.5
+            w = torch.softmax(torch.where(mask, w, -torch.inf), 1)
+            o, A = w @ vv, w @ vv.abs()
+            tol = 2.0 ** -8 * (A + o.abs()) + 2.0 ** -10 * A + (a + n) * 2.0 ** -126 / s * vv.abs().max()
+            err = (out[at:at + n, h].double() - o).abs()
+            assert bool((err <= tol).all()), (p, h, (err / tol).max().item())
+        at += n
