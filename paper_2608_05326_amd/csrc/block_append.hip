@@ -14,9 +14,12 @@ namespace qv {
 // product and one fused product, with the same roundings as k_rotate's.  The place's last, open
 // block is written by the workgroup of the first one, after it has read the old open block: both
 // are in the same rows.
-// A token and head is 512 bytes read and 256 written.  Bound by the chain of a workgroup (place,
-// positions, angles, rows, largest magnitude, codes; four workgroups of it to a unit), not yet by
-// memory: 11770 tokens of 8 heads 28 us (25 without the rotation), 18503 45 us, 2.5 TB/s.
+// A token and head is 512 bytes read and 256 written.  Not yet bound by memory: 11770 tokens of 8
+// heads 28.5 us (25 without the rotation), 18503 45.5 us, 2.5 TB/s.  What a workgroup does one after
+// the other (place, positions, angles, rows, largest magnitude, codes) is hidden by four waves a
+// SIMD only: 126 registers and 33 KB of LDS, which the angles need and which the workgroups that
+// rotate nothing have, too.  (k_block_store, the same without angles at 47 registers and eight
+// waves a SIMD, moves 5.2 TB/s.)
 namespace {
 // The angles (cosine and sine of pair i at angle_at(row, i)) are in the place of the values'
 // codes: four workgroups a compute unit.

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kThreads) void k_block_fetch(BlockArgs a, PackedRow
 // output are held in 32 bits, a block's value scale is applied to its products' fp32 sum.
 //
 // Bound by the pages' bytes: eight 8B sequences (401 MB) take 76 us, 32 ragged 70B places
-// (985 MB) 189 us, 5.3 and 5.2 TB/s where a large copy reaches 5.2; one sequence of 32K
+// (985 MB) 189 us, 5.3 and 5.2 TB/s (a large elementwise copy: 6.27); one sequence of 32K
 // (67 MB) 21 us, of which 3 go by before the first page is asked for and 5 in the join.
 namespace {
 constexpr float kLazyD = 8.f;

@@ -12,12 +12,12 @@
 // cut: qv_chunk.h), partial rows are joined by a second launch.  By the rows (position, head) of
 // a place and KV head:
 //   to 32 or 64   (drafted tokens) bound by the pages' bytes: a wave has its own pages, straight
-//                 from memory to LDS; 28 places, 113 tokens over 966 MB of cache 185 us and 6
-//                 for the join (5.2 TB/s).  64 rows a wave pair cost twice 32.
+//                 from memory to LDS; 28 places, 113 tokens over 966 MB of cache 191 us with
+//                 the join's 6 (5.1 TB/s).  64 rows a wave pair cost twice 32.
 //   more          (pieces of prompts) bound by the products and the exponentials between them:
 //                 eight waves of 32 rows share tiles that are expanded once, into LDS; 4096
-//                 tokens of 64 / 8 heads over 61440 take 7.6 to 8.0 ms (1.07 to 1.12 PFLOP/s; a
-//                 large matrix product reaches 1.39), the matrix unit busy 53% at 1.98 GHz.
+//                 tokens of 64 / 8 heads over 61440 take 7.5 to 8.1 ms by card (1.14 to 1.06 PFLOP/s;
+//                 a large matrix product reaches 1.45 to 1.35 there), the matrix unit busy 54%.
 // The reference of a row's weights is raised by whole powers of two, so that weights in bf16 that
 // are in flight scale exactly.
 //
@@ -1041,6 +1041,8 @@ __device__ __forceinline__ int join_groups(int parts) {
 }
 }  // namespace
 
+// (254 of 256 vector registers, nothing in scratch memory; 188 scalar values of the walk and of the
+// arguments are kept in lanes of vector registers.)
 __global__ __launch_bounds__(kChunkThreads, 2) void k_chunk_attend(BlockArgs a, ChunkStep s) {
   __shared__ __attribute__((aligned(128))) uint8_t lds_k[kLds], lds_v[kLds];
   const Shared sm = {lds_k, lds_v};

@@ -20,7 +20,8 @@ struct RotaryArgs {
   int64_t p_st, p_sa;
 };
 
-// cos and sin of u 2^-32 turns, to about 2^-24.  The nearest quarter turn is taken off, the
+// cos and sin of u 2^-32 turns, to 2^-23.4 (the largest error over the range; a product with a
+// bf16 value is rounded by 2^-8 in the end).  The nearest quarter turn is taken off, the
 // rest (at most pi / 4) goes into the Taylor series, whose first terms left out are
 // x^11 / 11! < 2^-29 and x^10 / 10! < 2^-25.
 __device__ __forceinline__ float2 cos_sin(uint32_t u) {

@@ -8,7 +8,8 @@
 namespace qv {
 
 // Every value is read and written once, 3 flops each: bound by memory (32K tokens of 32 + 8 heads
-// 127 us, 5.3 TB/s, a copy's rate; 5000 of 64 + 8 heads 42 us).  A thread computes the angles of
+// 127 us, 5.3 TB/s, where a copy of as many bytes takes as long and an elementwise one of 4 GB
+// reaches 6.27; 5000 of 64 + 8 heads 42 us).  A thread computes the angles of
 // eight pairs of one token once and takes them through up to eight heads (two loads of 16
 // bytes a head); eight threads a token.  The workgroups of a token's heads are neighbours, so
 // that their rows, which are, are read at about the same time (tokens as neighbours: 160 us).
